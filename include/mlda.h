@@ -228,6 +228,110 @@ void mlda_destroy(mlda_ctx* ctx);
 int mlda_philox_uniform(uint64_t seed, uint32_t iter, uint64_t token0, int64_t n,
                         double* out_dev, void* hip_stream);
 
+/*
+ * Operators on device tensors, for models that are trained and scored next to the sampled topics: a document's
+ * features or logits in, one row to a document.  They belong to no context.
+ *
+ * Common to all of them
+ *   - Pointers are DEVICE pointers unless said otherwise, aligned to their element; rows have consecutive columns and begin
+ *     `stride` elements apart (not read where there is one row), at any element.
+ *   - type: MLDA_FP32, MLDA_BF16 or MLDA_FP16.  Sums and statistics are fp32 or fp64 whatever the type, results are rounded once,
+ *     to nearest.  The order of all additions is fixed: equal inputs give equal bits.
+ *   - Kernels are launched on hip_stream, a stream of the current device, and the call returns; nothing is allocated or
+ *     synchronised, so the calls may be captured into a graph.  The workspace (the size comes from the call that is named
+ *     for it; its contents do not matter) and all tensors must stay until the stream has passed.
+ *   - What an output must not overlap with it may still equal: an output may be in the place of the input of its shape
+ *     where that is said.
+ *   - Without rows (or tensors) there is nothing to do, and the pointers may be null.
+ */
+#define MLDA_FP32 0
+#define MLDA_BF16 1
+#define MLDA_FP16 2
+
+/*
+ * Layer norm of each row of x over its cols columns (1 .. 2^30):
+ *   mean = sum x / cols, rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps), y = (x - mean) rstd weight + bias.
+ *   weight, bias   cols entries each of weight_type (the type of x, or MLDA_FP32); null: ones, zeros
+ *   y              of the type of x; may be x
+ *   mean, rstd     rows entries each, for the backward pass; null: not wanted
+ *   eps            finite, >= 0
+ */
+int mlda_layer_norm(const void* x, int64_t x_stride, const void* weight, const void* bias, void* y, int64_t y_stride,
+                    float* mean, float* rstd, int64_t rows, int32_t cols, double eps, int32_t type, int32_t weight_type,
+                    void* hip_stream);
+
+/*
+ * Its gradients, for grad_y of y: with u = (x - mean) rstd and h = grad_y weight
+ *   grad_x = rstd (h - mean over columns of h - u (mean over columns of h u)),
+ *   grad_weight = sum over rows of grad_y u, grad_bias = sum over rows of grad_y.
+ * Each of grad_x (of the type of x; may be x or grad_y), grad_weight and grad_bias (of weight_type) may be null: not wanted.  Without
+ * rows grad_weight and grad_bias are zeros.  The workspace (4-byte aligned) is for grad_weight and grad_bias.
+ */
+int mlda_layer_norm_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes);
+int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const void* x, int64_t x_stride, const float* mean,
+                             const float* rstd, const void* weight, void* grad_x, int64_t grad_x_stride, void* grad_weight,
+                             void* grad_bias, int64_t rows, int32_t cols, int32_t type, int32_t weight_type,
+                             void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
+#define MLDA_MAX_ALTERNATIVES 32
+
+/*
+ * Log-probabilities of given words under the softmax of each row of logits over vocab words (1 .. 2^30).
+ *   tokens    n_tokens (< 2^31) words.  Below zero: no word (log-probability 0, no gradient); vocab or more: NaN, no gradient.
+ *   row_ptr   rows + 1 entries as in mlda_create, here on the device: row r has the words row_ptr[r] .. row_ptr[r+1]-1 (the bounds are
+ *             clamped to 0 .. n_tokens).  Null: one word to a row, n_tokens = rows.
+ *   logprobs  n_tokens entries
+ *   stats     rows x 2: the greatest logit m and the logarithm of the sum of exp(logit - m), for the backward
+ *             pass (their sum is the logarithm of the sum of exponentials); null: not wanted
+ *   entropy   rows entries; null: not wanted
+ *   top_ids, top_logprobs   rows x alternatives (0 .. 32, at most vocab): the likeliest words in descending order, of equal logits the
+ *             lower word first, NaN after every number
+ * Words that are not allowed have a logit of minus infinity (or the type's lowest value).  A row that allows no word at all (all minus
+ * infinity) has log-probabilities of minus infinity and entropy 0; one with NaN or plus infinity has NaN.
+ * The workspace is 8-byte aligned.
+ */
+int mlda_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t alternatives, int32_t type, size_t* bytes);
+int mlda_token_logprobs(const void* logits, int64_t stride, int64_t rows, int32_t vocab, int32_t type, const int32_t* tokens,
+                        const int64_t* row_ptr, int64_t n_tokens, int32_t alternatives, float* logprobs, float* stats,
+                        float* entropy, int32_t* top_ids, float* top_logprobs, void* dev_workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
+/*
+ * The gradient with respect to the logits, for grad_logprobs (n_tokens) of the log-probabilities and grad_entropy (rows; null: zeros; with
+ * it, entropy as it came out) of the entropies.  With p the row's probabilities, l their logarithms, H the entropy:
+ *   grad_logits_v = sum over the row's tokens of word v of g  -  p_v (sum over all the row's tokens of g + grad_entropy (l_v + H)).
+ * grad_logits is of the type of the logits and may be the logits.  A row that allows no word, and one without words and
+ * without a gradient of its entropy, has zeros; a row whose words have a gradient that is not finite has NaN.
+ */
+int mlda_token_logprobs_backward(const void* logits, int64_t stride, int64_t rows, int32_t vocab, int32_t type, const int32_t* tokens,
+                                 const int64_t* row_ptr, int64_t n_tokens, const float* stats, const float* grad_logprobs,
+                                 const float* entropy, const float* grad_entropy, void* grad_logits, int64_t grad_stride,
+                                 void* hip_stream);
+
+/*
+ * Both at once, for a training step whose loss is the sum of the tokens' log-probabilities times `weights` (n_tokens, known
+ * beforehand): log-probabilities, and that sum's gradient.  grad_logits may be the logits.  The workspace is
+ * mlda_token_logprobs_workspace_bytes' for no alternatives.
+ */
+int mlda_token_logprobs_grad(const void* logits, int64_t stride, int64_t rows, int32_t vocab, int32_t type, const int32_t* tokens,
+                             const int64_t* row_ptr, int64_t n_tokens, const float* weights, float* logprobs, void* grad_logits,
+                             int64_t grad_stride, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The norm of a gradient over n_tensors tensors, the square root of the sum of all squares (summed in fp64), and the tensors
+ * scaled by max_norm / norm where the norm exceeds max_norm (>= 0; infinity: never).
+ *   tensors, out, sizes, types   HOST arrays of n_tensors entries, only read during the call: device pointers to contiguous tensors,
+ *          where each goes (its own place, or one that overlaps no tensor), numbers of elements (0 .. 2^40), types
+ *   norm   device, 1 entry, out: the norm before the scaling.  Where a tensor holds NaN or infinity it is not finite, and nothing is
+ *          scaled (one beyond fp32's range only comes out as infinity).
+ * The workspace is 8-byte aligned.
+ */
+int mlda_grad_norm_workspace_bytes(int32_t n_tensors, size_t* bytes);
+int mlda_grad_norm(const void* const* tensors, const int64_t* sizes, const int32_t* types, int32_t n_tensors, float* norm,
+                   void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+int mlda_clip_grads(const void* const* tensors, void* const* out, const int64_t* sizes, const int32_t* types, int32_t n_tensors,
+                    double max_norm, float* norm, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* mlda_strerror(int code);
 const char* mlda_last_error(void);
 

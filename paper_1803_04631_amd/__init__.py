@@ -57,6 +57,16 @@ def load_library() -> ctypes.CDLL:
         "mlda_get_timing": [p, p, i32, p],
         "mlda_get_sampler_bytes": [p, p, i32, p],
         "mlda_philox_uniform": [u64, u32, u64, i64, p, p],
+        "mlda_layer_norm": [p, i64, p, p, p, i64, p, p, i64, i32, dbl, i32, i32, p],
+        "mlda_layer_norm_workspace_bytes": [i64, i32, p],
+        "mlda_layer_norm_backward": [p, i64, p, i64, p, p, p, p, i64, p, p, i64, i32, i32, i32, p, sz, p],
+        "mlda_token_logprobs_workspace_bytes": [i64, i32, i32, i32, p],
+        "mlda_token_logprobs": [p, i64, i64, i32, i32, p, p, i64, i32, p, p, p, p, p, p, sz, p],
+        "mlda_token_logprobs_backward": [p, i64, i64, i32, i32, p, p, i64, p, p, p, p, p, i64, p],
+        "mlda_token_logprobs_grad": [p, i64, i64, i32, i32, p, p, i64, p, p, p, i64, p, sz, p],
+        "mlda_grad_norm_workspace_bytes": [i32, p],
+        "mlda_grad_norm": [p, p, p, i32, p, p, sz, p],
+        "mlda_clip_grads": [p, p, p, p, i32, dbl, p, p, sz, p],
     }
     for name, argtypes in sig.items():
         fn = getattr(lib, name)
@@ -77,7 +87,10 @@ EXPORTED = ["mlda_workspace_bytes", "mlda_create", "mlda_workspace_bytes_streame
             "mlda_step", "mlda_iteration", "mlda_get_assignments", "mlda_get_word_topic",
             "mlda_get_topic_totals", "mlda_get_doc_topic_nnz", "mlda_get_doc_topic_csr",
             "mlda_get_loglik", "mlda_get_timing", "mlda_get_sampler_bytes", "mlda_destroy",
-            "mlda_philox_uniform", "mlda_strerror", "mlda_last_error"]
+            "mlda_philox_uniform", "mlda_layer_norm", "mlda_layer_norm_workspace_bytes",
+            "mlda_layer_norm_backward", "mlda_token_logprobs_workspace_bytes", "mlda_token_logprobs",
+            "mlda_token_logprobs_backward", "mlda_token_logprobs_grad", "mlda_grad_norm_workspace_bytes",
+            "mlda_grad_norm", "mlda_clip_grads", "mlda_strerror", "mlda_last_error"]
 
 
 def _check(rc: int):

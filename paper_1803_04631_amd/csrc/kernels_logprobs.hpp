@@ -1,0 +1,609 @@
+// Log-probabilities of given words out of rows of logits, the distributions' entropies, the likeliest
+// words, and the gradient with respect to the logits.
+//
+// With m = max_v x_v, s = sum_v exp(x_v - m), p_v = exp(x_v - m) / s of a row:
+//   log p(word) = x_word - m - ln s
+//   H           = -sum_v p_v ln p_v = ln s - sum_v exp(x_v - m) (x_v - m) / s
+//   d/dx_v of  sum_t g_t log p(word_t) + h H  =  sum_{t: word_t = v} g_t  -  p_v (G + h (x_v - m - ln s + H)),  G = sum_t g_t
+//
+// One pass over a row has the maximum, both sums and the likeliest words: each lane keeps a running maximum and rescales
+// its sums when it grows; lanes, waves and segments of a row are joined at the end.  Bound by memory where the logits have 4 bytes;
+// with 2 the instructions issued (about ten an element) are not far behind.
+//
+// The statistics of a row are kept as the pair (m, ln s): their sum is the logarithm of the sum of exponentials, and
+// differences to m lose nothing where m is large.  A row whose logits are all minus infinity has (-inf, 0).
+#pragma once
+#include "vec_io.hpp"
+
+namespace mlda {
+
+constexpr int kMaxAlternatives = 32;
+constexpr int kHeld = 128;                       // candidates a wave holds before it sorts them: two a lane
+constexpr int kTilePieces = 4;                   // 16-byte pieces of a row that a lane has on their way
+constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kLowest = -3.402823466e+38f;
+constexpr float kVanished = -200.0f;             // exponentials of less are 0 in fp32: what they are multiplied with may stay finite
+constexpr int kLogprobThreads = 256;
+constexpr int kLogprobWaves = kLogprobThreads / kWave;
+
+template <class T> constexpr int kTileCols = kWave * kTilePieces * kPack<T>;    // columns of a wave's tile
+
+struct RowPart {          // what a segment of a row comes to
+    double s, u;          // sums of exp(x - m) and of exp(x - m) (x - m)
+    float m;
+    int32_t n;            // candidates
+};
+
+struct LogprobArgs {
+    const void* logits;
+    int64_t stride, rows;
+    int32_t vocab;
+    const int32_t* tokens;       // words; below zero: none
+    const int64_t* row_ptr;      // null: one word to a row
+    int64_t n_tokens;
+    int32_t top;
+    float* logprobs;
+    float* stats;                // [rows][2]
+    float* entropy;              // null: not wanted
+    int32_t* top_ids;
+    float* top_logprobs;
+    int32_t segments;            // of a row, at most a wave's lanes, of segment_cols columns each (a multiple of the workgroup's tiles)
+    int32_t segment_cols;
+    RowPart* parts;              // [rows][segments]
+    uint64_t* part_top;          // [rows][segments][top]
+};
+
+// ---------------------------------------------------------------- the order of the alternatives
+// Greater logits first, then lower words; NaN after every number.  A logit's key is a whole number in that order; 0 is kept
+// for "no word".
+__device__ __forceinline__ uint32_t order_key(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);                  // (minus zero is zero)
+    const uint32_t k = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+    return x == x ? k : 1u;
+}
+__device__ __forceinline__ float key_logit(uint32_t k) {
+    if (k == 1u) return __uint_as_float(0x7fc00000u);
+    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+__device__ __forceinline__ uint64_t candidate(uint32_t key, int32_t word) { return (uint64_t)key << 32 | (uint32_t)~word; }
+__device__ __forceinline__ int32_t candidate_word(uint64_t c) { return (int32_t)~(uint32_t)c; }
+
+// LDS of a wave that other lanes of the same wave have written: the hardware keeps a wave's LDS accesses in order, the compiler must, too.
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Puts the `n` greatest of held[0 .. count) (count <= kHeld, all different) first, in descending order.  By one wave; every lane takes
+// part.  Returns how many there are now.
+__device__ __forceinline__ int keep_greatest(uint64_t* held, int count, int n) {
+    const int lane = lane_id();
+    wave_lds_fence();
+    const uint64_t a = lane < count ? held[lane] : 0, b = lane + kWave < count ? held[lane + kWave] : 0;
+    int rank_a = 0, rank_b = 0;
+    if (count <= kWave) {
+#pragma unroll 8
+        for (int i = 0; i < count; ++i) rank_a += held[i] > a ? 1 : 0;
+    } else {
+#pragma unroll 8
+        for (int i = 0; i < count; ++i) {
+            const uint64_t c = held[i];
+            rank_a += c > a ? 1 : 0;
+            rank_b += c > b ? 1 : 0;
+        }
+    }
+    wave_lds_fence();
+    if (lane < count && rank_a < n) held[rank_a] = a;
+    if (lane + kWave < count && rank_b < n) held[rank_b] = b;
+    wave_lds_fence();
+    return min(count, n);
+}
+
+// The greatest key that at least n lanes' keys reach (0 if fewer than n have one).
+__device__ __forceinline__ uint32_t nth_key(uint32_t key, int n) {
+    uint32_t found = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t with = found | 1u << bit;
+        if (__popcll(__ballot(key >= with)) >= n) found = with;
+    }
+    return found;
+}
+
+// A wave's candidates for the alternatives of a row.
+struct Candidates {
+    uint64_t* held;        // LDS, kHeld of them
+    int n, count = 0;      // wanted; held
+    uint64_t least = 0;    // the n-th greatest so far, if there are n
+    float bar = 0.0f;      // its logit
+
+    __device__ __forceinline__ void sort() {
+        count = keep_greatest(held, count, n);
+        if (count == n) {
+            const uint64_t c = held[n - 1];
+            least = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(c >> 32)) << 32 |
+                    (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)c);
+            bar = key_logit((uint32_t)(least >> 32));
+        }
+    }
+    // Whether a tile may have something to add, by each lane's maximum of it.  Columns ascend from tile to tile, so an equal logit
+    // of a later tile comes after those held.  (A bar that is NaN lets everything through.)
+    __device__ __forceinline__ bool wants(float lane_max) const { return count < n || __ballot(!(lane_max <= bar)) != 0; }
+
+    // The tile of columns [first, first + kTileCols) of a row, those below `end`, read once more (from the caches).  At least n of its
+    // logits reach the n-th greatest of the lanes' maxima, so only those can be among the n greatest.
+    template <class T>
+    __device__ __forceinline__ void add(const T* row, int64_t first, int32_t end) {
+        constexpr int P = kPack<T>;
+        auto piece = [&](int j, float (&v)[P]) {
+            const int64_t c = first + (j * kWave + lane_id()) * P;
+            unpack(load_some(row + c, (int)max((int64_t)0, min((int64_t)P, end - c)), 0.0f), v, T());
+            return (int32_t)c;
+        };
+        uint32_t most = 0;
+#pragma unroll 1
+        for (int j = 0; j < kTilePieces; ++j) {
+            float v[P];
+            const int32_t c = piece(j, v);
+#pragma unroll
+            for (int e = 0; e < P; ++e) most = max(most, c + e < end ? order_key(v[e]) : 0u);
+        }
+        const uint32_t floor = max(nth_key(most, n), 1u);
+#pragma unroll 1
+        for (int j = 0; j < kTilePieces; ++j) {
+            float v[P];
+            const int32_t c = piece(j, v);
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const uint32_t key = c + e < end ? order_key(v[e]) : 0u;
+                const uint64_t mine = candidate(key, c + e);
+                uint64_t mask = __ballot(key >= floor && mine > least);
+                if (mask) {
+                    if (count + __popcll(mask) > kHeld) {
+                        sort();
+                        mask = __ballot(key >= floor && mine > least);
+                    }
+                    if (key >= floor && mine > least) held[count + __popcll(mask & lanes_below())] = mine;
+                    count += __popcll(mask);
+                }
+            }
+        }
+        if (count >= n) sort();
+    }
+};
+
+// ---------------------------------------------------------------- one pass over a row, or a segment
+// exp2 of a product that is at most zero: a product of the type's lowest values may overflow to minus infinity, which is meant.
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2E); }
+
+struct LaneSums {
+    float m = kLowest;        // (a finite bound: minus infinity minus it is minus infinity, whose exponential is 0)
+    float s = 0.0f, u = 0.0f;
+
+    __device__ __forceinline__ void raise(float to) {
+        if (to > m) {
+            const float d = fmaxf(m - to, kVanished);
+            const float f = exp_of(d);
+            u = f * __builtin_fmaf(d, s, u);
+            s *= f;
+            m = to;
+        }
+    }
+    template <bool kEntropy>
+    __device__ __forceinline__ void add(float x) {
+        const float d = x - m, e = exp_of(d);
+        s += e;
+        if constexpr (kEntropy) u = __builtin_fmaf(e, fmaxf(d, kVanished), u);
+    }
+};
+
+// The sums of all lanes of a wave, each relative to its own bound, as one, relative to the greatest.
+__device__ __forceinline__ void join_lanes(float& m, double& s, double& u) {
+    const float most = wave_max(m), d = fmaxf(m - most, kVanished);
+    const double f = s != 0.0 ? (double)exp_of(d) : 0.0;
+    u = wave_sum(f != 0.0 ? f * (u + (double)d * s) : 0.0);
+    s = wave_sum(f * s);
+    m = most;
+}
+
+// The parts that the waves of a workgroup have left, as one; every wave gets it.
+__device__ __forceinline__ void join_parts(const RowPart* part, int n, float& m, double& s, double& u) {
+    const int lane = lane_id();
+    m = lane < n ? part[lane].m : kLowest;
+    s = lane < n ? part[lane].s : 0.0;
+    u = lane < n ? part[lane].u : 0.0;
+    join_lanes(m, s, u);
+}
+
+// The columns [begin, end) of a row by the waves of a workgroup, `waves` of them taking tiles in turn.  `top` may be null.
+template <class T, bool kExtras>
+__device__ __forceinline__ void walk_row(const T* row, int32_t begin, int32_t end, int wave, int waves, LaneSums& sums, Candidates* top) {
+    constexpr int P = kPack<T>, kCols = kTileCols<T>;
+    const int lane = lane_id();
+    Raw next[kTilePieces];
+    auto load = [&](int64_t first) {
+        if (first + kCols <= end) {
+#pragma unroll
+            for (int j = 0; j < kTilePieces; ++j) next[j] = load_raw(row + first + (j * kWave + lane) * P);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kTilePieces; ++j) {
+                const int64_t c = first + (j * kWave + lane) * P;
+                next[j] = load_some(row + c, (int)max((int64_t)0, min((int64_t)P, end - c)), -INFINITY);
+            }
+        }
+    };
+    int64_t first = begin + (int64_t)wave * kCols;
+    if (first < end) load(first);
+    for (; first < end; first += (int64_t)waves * kCols) {
+        Raw now[kTilePieces];
+        float most = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kTilePieces; ++j) {
+            now[j] = next[j];
+            float v[P];
+            unpack(now[j], v, T());
+#pragma unroll
+            for (int e = 0; e < P; ++e) most = fmaxf(most, v[e]);
+        }
+        if (first + (int64_t)waves * kCols < end) load(first + (int64_t)waves * kCols);
+        sums.raise(most);
+#pragma unroll
+        for (int j = 0; j < kTilePieces; ++j) {
+            float v[P];
+            unpack(now[j], v, T());
+#pragma unroll
+            for (int e = 0; e < P; ++e) sums.add<kExtras>(v[e]);
+        }
+        if constexpr (kExtras) {
+            if (top->n && top->wants(most)) top->add(row, first, end);
+        }
+    }
+}
+
+// The log-probability of a word: NaN for one outside the vocabulary, 0 for none.
+template <class T>
+__device__ __forceinline__ float word_logprob(const T* row, int32_t word, int32_t vocab, float m, float log_s) {
+    if (word < 0) return 0.0f;
+    if (word >= vocab) return __uint_as_float(0x7fc00000u);
+    if (m == -INFINITY) return -INFINITY;
+    return ((float)row[word] - m) - log_s;
+}
+
+// The words of a row: [begin, end) of the tokens, whatever the bounds say.
+__device__ __forceinline__ void row_tokens(const int64_t* row_ptr, int64_t n_tokens, int64_t row, int64_t& begin, int64_t& end) {
+    if (row_ptr) {
+        begin = min(max(row_ptr[row], (int64_t)0), n_tokens);
+        end = min(max(row_ptr[row + 1], begin), n_tokens);
+    } else {
+        begin = row;
+        end = row + 1;
+    }
+}
+
+// A row's statistics out of its sums.  No logit above minus infinity: (-inf, 0), entropy 0.
+struct RowStats {
+    float m, log_s, entropy;
+    __device__ __forceinline__ RowStats(float max, double s, double u) {
+        if (s == 0.0) {
+            m = -INFINITY;
+            log_s = entropy = 0.0f;
+        } else {
+            const double l = log(s);
+            m = max;
+            log_s = (float)l;
+            entropy = (float)(l - u / s);
+        }
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, const RowStats& st, const uint64_t* top) {
+    const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+    int64_t begin, end;
+    row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
+    for (int64_t t = begin + threadIdx.x; t < end; t += kLogprobThreads)
+        a.logprobs[t] = word_logprob(logits, a.tokens[t], a.vocab, st.m, st.log_s);
+    if (threadIdx.x == 0) {
+        if (a.stats) {
+            a.stats[2 * row] = st.m;
+            a.stats[2 * row + 1] = st.log_s;
+        }
+        if (a.entropy) a.entropy[row] = st.entropy;
+    }
+    if ((int)threadIdx.x < a.top) {
+        const uint64_t c = top[threadIdx.x];
+        const float x = key_logit((uint32_t)(c >> 32));
+        a.top_ids[row * a.top + threadIdx.x] = candidate_word(c);
+        a.top_logprobs[row * a.top + threadIdx.x] = st.m == -INFINITY ? -INFINITY : (x - st.m) - st.log_s;
+    }
+}
+
+// Workgroup by workgroup a row, or a segment of one: with one segment all is done, else logprob_join_kernel goes on.
+template <class T, bool kExtras>
+__global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a) {
+    __shared__ uint64_t held[kLogprobWaves][kHeld];
+    __shared__ RowPart part[kLogprobWaves];
+    __shared__ uint64_t best[kHeld];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
+    const int64_t items = a.rows * a.segments;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t row = item / a.segments;
+        const int32_t begin = (int32_t)(item % a.segments) * a.segment_cols;
+        const int32_t end = min(a.vocab - begin, a.segment_cols) + begin;
+        LaneSums sums;
+        Candidates top{held[wave], a.top};
+        walk_row<T, kExtras>(static_cast<const T*>(a.logits) + row * a.stride, begin, end, wave, kLogprobWaves, sums, &top);
+        float m = sums.m;
+        double s = sums.s, u = sums.u;
+        join_lanes(m, s, u);
+        if (kExtras && a.top && top.count < a.top) top.sort();
+        if (lane == 0) part[wave] = RowPart{s, u, m, top.count};
+        __syncthreads();
+        join_parts(part, kLogprobWaves, m, s, u);
+        int count = 0;
+        if constexpr (kExtras) {
+            if (a.top && wave == 0) {              // the waves' lists, of kMaxAlternatives each at most, one after the other
+                for (int w = 0; w < kLogprobWaves; ++w) {
+                    const int n = part[w].n;
+                    if (lane < n) best[count + lane] = held[w][lane];
+                    count += n;
+                }
+                count = keep_greatest(best, count, a.top);
+            }
+            __syncthreads();
+        }
+        if (a.segments == 1) {
+            finish_row<T>(a, row, RowStats(m, s, u), best);
+        } else {
+            if (threadIdx.x == 0) a.parts[item] = RowPart{s, u, m, count};
+            if (kExtras && wave == 0 && lane < count) a.part_top[item * a.top + lane] = best[lane];
+        }
+        __syncthreads();                           // (the next row's parts and candidates)
+    }
+}
+
+// Joins the segments of a row.
+template <class T>
+__global__ __launch_bounds__(kLogprobThreads) void logprob_join_kernel(LogprobArgs a) {
+    __shared__ uint64_t held[kLogprobWaves][kHeld];
+    __shared__ uint64_t best[kHeld];
+    __shared__ int counts[kLogprobWaves];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const RowPart* parts = a.parts + row * a.segments;
+        // every wave the sums of all segments, of which there are at most as many as lanes
+        float m = lane < a.segments ? parts[lane].m : kLowest;
+        double s = lane < a.segments ? parts[lane].s : 0.0, u = lane < a.segments ? parts[lane].u : 0.0;
+        join_lanes(m, s, u);
+        if (a.top) {
+            // a wave's share of the segments' lists; full buffers are cut down to the wanted number
+            int count = 0;
+            for (int i = wave; i < a.segments; i += kLogprobWaves) {
+                const int n = min(__builtin_amdgcn_readfirstlane(parts[i].n), a.top);
+                if (count + n > kHeld) count = keep_greatest(held[wave], count, a.top);
+                if (lane < n) held[wave][count + lane] = a.part_top[(row * a.segments + i) * a.top + lane];
+                count += n;
+            }
+            count = keep_greatest(held[wave], count, a.top);
+            if (lane == 0) counts[wave] = count;
+            __syncthreads();
+            if (wave == 0) {
+                count = 0;
+                for (int w = 0; w < kLogprobWaves; ++w) {
+                    const int n = counts[w];
+                    if (lane < n) best[count + lane] = held[w][lane];
+                    count += n;
+                }
+                keep_greatest(best, count, a.top);
+            }
+            __syncthreads();
+        }
+        finish_row<T>(a, row, RowStats(m, s, u), best);
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------- gradient
+struct LogprobGradArgs {
+    const void* logits;
+    int64_t stride, rows;
+    int32_t vocab;
+    const int32_t* tokens;
+    const int64_t* row_ptr;
+    int64_t n_tokens;
+    const float* grad;           // of each word's log-probability
+    float* stats;                // read, or, with kLoss, written (null: not wanted)
+    const float* entropy;        // both null: no gradient of the entropy
+    const float* grad_entropy;
+    float* logprobs;             // kLoss
+    void* out;
+    int64_t out_stride;
+    int32_t segments;
+    int32_t segment_cols;
+    int32_t slots;               // of the words' table, a power of two
+};
+
+constexpr int kGradThreads = 512;
+constexpr int kGradWaves = kGradThreads / kWave;
+
+// The words' gradients of a row are summed in a table in LDS, as whole numbers: a unit is so small that n of them of the
+// greatest magnitude stay below 2^62, and whole numbers add up to the same in any order.
+struct WordTable {
+    unsigned long long* sums;    // [slots]
+    int32_t* words;              // [slots], -1: free
+    int32_t slots;
+
+    __device__ __forceinline__ void clear() const {
+        for (int i = (int)threadIdx.x; i < slots; i += kGradThreads) {
+            sums[i] = 0;
+            words[i] = -1;
+        }
+    }
+    // `direct`: the table has a slot for each column from `first` on; else a word goes to the next free slot from the one that
+    // its hash says (at most half of them are taken).
+    __device__ __forceinline__ void add(int32_t word, long long units, bool direct, int32_t first) const {
+        int i = word - first;
+        if (direct) {
+            words[i] = word;
+        } else {
+            i = (int)(((uint32_t)word * 0x9E3779B1u) >> 16) & (slots - 1);
+            for (;;) {
+                const int was = atomicCAS(&words[i], -1, word);
+                if (was == -1 || was == word) break;
+                i = (i + 1) & (slots - 1);
+            }
+        }
+        atomicAdd(&sums[i], (unsigned long long)units);
+    }
+};
+
+// What a row's gradient needs besides its logits.
+struct RowGrad {
+    float m, log_s, inv_s;       // of the row
+    float total, h, entropy;     // G, gradient of the entropy, entropy
+    // of one logit, without its own words' gradients
+    template <bool kEntropy>
+    __device__ __forceinline__ float of(float x) const {
+        const float d = x - m, p = exp_of(d) * inv_s;
+        if constexpr (kEntropy) return -p * (total + h * (fmaxf(d, kVanished) - log_s + entropy));
+        return -p * total;
+    }
+};
+
+template <class T, bool kEntropy, bool kSingle>
+__device__ __forceinline__ void stream_grad(const T* row, T* out, int32_t begin, int32_t end, const RowGrad& g, int32_t word, float word_grad) {
+    constexpr int P = kPack<T>;
+    for (int64_t c = begin + (int64_t)threadIdx.x * P; c < end; c += kGradThreads * P) {
+        const int n = (int)min((int64_t)P, end - c);
+        float v[P];
+        unpack(load_some(row + c, n, -INFINITY), v, T());
+#pragma unroll
+        for (int e = 0; e < P; ++e) v[e] = g.of<kEntropy>(v[e]);
+        if (kSingle && (uint32_t)(word - (int32_t)c) < (uint32_t)P) {
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[e] += (int32_t)c + e == word ? word_grad : 0.0f;
+        }
+        store_some(out + c, pack(v, T()), n);
+    }
+}
+
+// Rows, or segments of rows.  kLoss: the statistics and the words' log-probabilities are found first, by the same workgroup
+// (one segment).  kSingle: one word to a row.  The logits' rows may be the gradient's.
+template <class T, bool kLoss, bool kEntropy, bool kSingle>
+__global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradArgs a) {
+    extern __shared__ unsigned long long table_lds[];
+    __shared__ RowPart part[kGradWaves];
+    __shared__ double totals[kGradWaves];
+    __shared__ float largest[kGradWaves];
+    const WordTable table{table_lds, reinterpret_cast<int32_t*>(table_lds + a.slots), a.slots};
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
+    const int64_t items = a.rows * a.segments;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t row = item / a.segments;
+        const int32_t begin = (int32_t)(item % a.segments) * a.segment_cols;
+        const int32_t end = min(a.vocab - begin, a.segment_cols) + begin;
+        const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+        T* out = static_cast<T*>(a.out) + row * a.out_stride;
+        int64_t t0, t1;
+        row_tokens(a.row_ptr, a.n_tokens, row, t0, t1);
+        RowGrad g;
+        g.h = kEntropy ? a.grad_entropy[row] : 0.0f;
+        g.entropy = kEntropy ? a.entropy[row] : 0.0f;
+        if (kLoss && (t1 > t0 || a.stats)) {
+            LaneSums sums;
+            walk_row<T, false>(logits, begin, end, wave, kGradWaves, sums, nullptr);
+            float m = sums.m;
+            double s = sums.s, u = 0.0;
+            join_lanes(m, s, u);
+            if (lane == 0) part[wave] = RowPart{s, u, m, 0};
+            __syncthreads();
+            join_parts(part, kGradWaves, m, s, u);
+            const RowStats st(m, s, u);
+            g.m = st.m;
+            g.log_s = st.log_s;
+            g.inv_s = (float)(1.0 / s);
+            if (a.stats && threadIdx.x == 0) {
+                a.stats[2 * row] = st.m;
+                a.stats[2 * row + 1] = st.log_s;
+            }
+        } else if (!kLoss) {
+            g.m = a.stats[2 * row];
+            g.log_s = a.stats[2 * row + 1];
+            g.inv_s = (float)exp(-(double)g.log_s);
+        } else {
+            g.m = -INFINITY;                       // (a row without words: nothing to read it for)
+            g.log_s = g.inv_s = 0.0f;
+        }
+        // the row's total and the greatest magnitude of its words' gradients
+        double total = 0.0;
+        float most = 0.0f;
+        int32_t word = -1;
+        for (int64_t t = t0 + (kSingle ? 0 : threadIdx.x); t < t1; t += kGradThreads) {
+            word = a.tokens[t];
+            if (kLoss && (!kSingle || threadIdx.x == 0)) a.logprobs[t] = word_logprob(logits, word, a.vocab, g.m, g.log_s);
+            if (word >= 0 && word < a.vocab) {
+                total += (double)a.grad[t];
+                most = fmaxf(most, fabsf(a.grad[t]));
+            }
+        }
+        if (!kSingle) {
+            total = wave_sum(total);
+            most = wave_max(most);
+            if (lane == 0) {
+                totals[wave] = total;
+                largest[wave] = most;
+            }
+            __syncthreads();
+            total = 0.0;
+            most = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kGradWaves; ++w) {
+                total += totals[w];
+                most = fmaxf(most, largest[w]);
+            }
+        }
+        g.total = (float)total;
+        const bool finite = most < INFINITY && total == total;
+        if (!finite) g.total = __uint_as_float(0x7fc00000u);       // the whole row's gradient is NaN
+        if (g.m == -INFINITY || (most == 0.0f && total == 0.0 && g.h == 0.0f)) {
+            // nothing is allowed, or nothing is wanted: zeros
+            if (kLoss) __syncthreads();                            // (logits read above may be written here)
+            for (int64_t c = begin + (int64_t)threadIdx.x * kPack<T>; c < end; c += kGradThreads * kPack<T>)
+                store_some(out + c, Raw{0, 0, 0, 0}, (int)min((int64_t)kPack<T>, end - c));
+        } else if (kSingle) {
+            if (kLoss) __syncthreads();
+            stream_grad<T, kEntropy, true>(logits, out, begin, end, g, word < a.vocab ? word : -1, (float)total);
+        } else {
+            const int64_t n = t1 - t0;
+            const bool direct = n > a.slots / 2;
+            const int unit = 62 - (n > 1 ? 64 - __clzll(n - 1) : 0) - (finite && most > 0.0f ? ilogbf(most) + 1 : 0);
+            const double units = ldexp(1.0, unit), per_unit = ldexp(1.0, -unit);
+            for (int32_t first = begin; first < end; first += direct ? a.slots : end - begin) {
+                const int32_t last = direct ? min(end - first, a.slots) + first : end;
+                table.clear();
+                __syncthreads();
+                for (int64_t t = t0 + threadIdx.x; finite && t < t1; t += kGradThreads) {
+                    const int32_t w = a.tokens[t];
+                    if (w >= first && w < last) table.add(w, (long long)rint((double)a.grad[t] * units), direct, first);
+                }
+                __syncthreads();
+                // a word's own gradient, before the row is written over
+                for (int i = (int)threadIdx.x; i < a.slots; i += kGradThreads)
+                    if (table.words[i] >= 0) {
+                        const float own = (float)((double)(long long)table.sums[i] * per_unit);
+                        table.sums[i] = (unsigned long long)__float_as_uint(own + g.of<kEntropy>((float)logits[table.words[i]]));
+                    }
+                __syncthreads();
+                stream_grad<T, kEntropy, false>(logits, out, first, last, g, -1, 0.0f);
+                __syncthreads();
+                for (int i = (int)threadIdx.x; i < a.slots; i += kGradThreads)
+                    if (table.words[i] >= 0) out[table.words[i]] = (T)__uint_as_float((uint32_t)table.sums[i]);
+                if (direct) __syncthreads();
+            }
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace mlda

@@ -26,6 +26,7 @@
 #include <vector>
 
 #include "chunk_layout.hpp"
+#include "host_errors.hpp"
 #include "kernels_rebuild.hpp"
 #include "kernels_sample.hpp"
 #include "switches.hpp"
@@ -1862,6 +1863,15 @@ int for_each_chunk_rows(mlda_ctx* c, F&& visit) {
 }
 
 }  // namespace
+
+int mlda::set_error(int code, const char* what, const char* why) noexcept {
+    try {
+        return fail(code, why ? std::string(what) + ": " + why : std::string(what));
+    } catch (...) {                      // no memory for the message
+        g_last_error.clear();
+        return code;
+    }
+}
 
 extern "C" {
 
