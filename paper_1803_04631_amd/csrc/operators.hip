@@ -320,7 +320,8 @@ int mlda_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t alt
     if (alternatives < 0 || alternatives > MLDA_MAX_ALTERNATIVES || alternatives > vocab)
         return refuse("log-probabilities: need 0 <= alternatives <= 32, and no more than there are words");
     // (the statistics that mlda_token_logprobs_grad keeps where it works in two steps come on top)
-    *bytes = logprob_workspace(rows, vocab, alternatives, type) + (size_t)rows * 8;
+    const size_t parts = logprob_workspace(rows, vocab, alternatives, type);
+    *bytes = parts ? parts + (size_t)rows * 8 : 0;
     return MLDA_OK;
 }
 

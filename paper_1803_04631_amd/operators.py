@@ -33,129 +33,139 @@ class TokenLogprobs(NamedTuple):
     top_logprobs: Optional[torch.Tensor]       # [rows, alternatives] fp32
 
 
-def _need(ok, message):
-    if not ok:
-        raise ValueError(message)
-
-
-def _on(device):
-    """The library launches on the current device."""
-    _need(device.type == "cuda", "tensors must be on a GPU: there is no CPU path")
-    return torch.cuda.device(device)
+# On one document a call takes the GPU 4 us; what is done here for it is kept short: messages are made where one is
+# raised, sizes of workspaces are asked for once.
+def _launch(device, call, *args):
+    """The library's call on the current stream of that device, which it wants to be the current one."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        rc = call(*args, torch._C._cuda_getCurrentRawStream(index))    # current_stream().cuda_stream, which takes 2.7 us
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, torch._C._cuda_getCurrentRawStream(index))
+    if rc:
+        _check(rc)
 
 
 def _rows(t, name):
-    """A matrix's rows, consecutive columns each: (rows, cols, stride)."""
-    _need(t.dim() == 2 and t.shape[1] >= 1, f"{name} must be a matrix with at least one column")
-    _need(t.dtype in _TYPES, f"{name} must be fp32, bf16 or fp16")
+    """A matrix's rows, consecutive columns each: (rows, cols, stride, type code)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a tensor on a GPU: there is no CPU path")
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"{name} must be fp32, bf16 or fp16")
+    if t.dim() != 2 or t.shape[1] < 1:
+        raise ValueError(f"{name} must be a matrix with at least one column")
     rows, cols = t.shape
     stride, step = t.stride()
-    _need((step == 1 or cols == 1) and (rows <= 1 or stride >= cols),
-          f"{name} must have consecutive columns and rows that do not overlap")
-    return rows, cols, stride
+    if (step != 1 and cols != 1) or (rows > 1 and stride < cols):
+        raise ValueError(f"{name} must have consecutive columns and rows that do not overlap")
+    return rows, cols, stride, kind
 
 
 def _like(t, name, shape, dtype, device):
-    """A contiguous tensor of that shape, type and device; its address."""
-    _need(tuple(t.shape) == shape and t.dtype == dtype and t.device == device and t.is_contiguous(),
-          f"{name} must be a contiguous {dtype} tensor of shape {shape} on {device}")
+    """The address of a contiguous tensor of that shape, type and device."""
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
     return t.data_ptr()
 
 
-def _out_rows(out, name, like):
-    """Rows for a result of the shape and type of `like`."""
-    if out is None:
-        out = torch.empty(like.shape, dtype=like.dtype, device=like.device)
-    else:
-        _need(out.shape == like.shape and out.dtype == like.dtype and out.device == like.device,
-              f"{name} must have the shape, type and device of the input")
-    return out, _rows(out, name)[2]
+def _rows_like(t, name, like):
+    """The stride of rows of the shape, type and device of `like`."""
+    stride = _rows(t, name)[2]
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must have the shape, type and device of the input")
+    return stride
 
 
-def _workspace(size_call, args, device):
+def _fp32(shape, device):
+    return torch.empty(shape, dtype=torch.float32, device=device)
+
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(call, *sizes):
     n = ctypes.c_size_t()
-    _check(size_call(*args, ctypes.addressof(n)))
-    if not n.value:
-        return None, 0, 0
-    t = torch.empty(n.value, dtype=torch.uint8, device=device)
-    return t, t.data_ptr(), n.value
+    _check(getattr(load_library(), call)(*sizes, ctypes.addressof(n)))
+    return n.value
 
 
-def _with_device(fn):
-    """Makes the first tensor's device the current one for the call, where it is another."""
-    @functools.wraps(fn)
-    def call(first, *args, **kwargs):
-        device = first.device if isinstance(first, torch.Tensor) else None
-        if device is None:
-            raise ValueError("a tensor is wanted")
-        _need(device.type == "cuda", "tensors must be on a GPU: there is no CPU path")
-        if device.index == torch.cuda.current_device():
-            return fn(first, *args, **kwargs)
-        with torch.cuda.device(device):
-            return fn(first, *args, **kwargs)
-    return call
+def _workspace(size, device):
+    """(what holds the memory, its address)"""
+    if not size:
+        return None, 0
+    t = torch.empty(size, dtype=torch.uint8, device=device)
+    return t, t.data_ptr()
 
 
-def _weight_type(weight, bias, x, cols):
-    """The weight's type code and both addresses (0: none)."""
-    given = weight if weight is not None else bias
-    if given is None:
-        return _TYPES[x.dtype], 0, 0
-    _need(given.dtype == x.dtype or given.dtype == torch.float32, "weight and bias must have the type of x, or be fp32")
-    at = [0 if t is None else _like(t, name, (cols,), given.dtype, x.device) for t, name in ((weight, "weight"), (bias, "bias"))]
-    return _TYPES[given.dtype], at[0], at[1]
+def _columns(t, name, cols, x):
+    """The address of a weight or bias, and its type code."""
+    if not isinstance(t, torch.Tensor) or (t.dtype != x.dtype and t.dtype != torch.float32):
+        raise ValueError(f"{name} must have the type of x, or be fp32")
+    return _like(t, name, (cols,), t.dtype, x.device), _TYPES[t.dtype]
 
 
-@_with_device
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None):
     """Each row of x [rows, cols] less its mean, over its standard deviation, times weight, plus bias.
     Returns (y, mean [rows], rstd [rows]); `out` (x, for instance) takes y."""
-    rows, cols, stride = _rows(x, "x")
-    kind, at_weight, at_bias = _weight_type(weight, bias, x, cols)
-    y, y_stride = _out_rows(out, "out", x)
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
-    _check(load_library().mlda_layer_norm(
-        x.data_ptr(), stride, at_weight, at_bias, y.data_ptr(), y_stride, mean.data_ptr(), rstd.data_ptr(), rows, cols,
-        eps, _TYPES[x.dtype], kind, torch.cuda.current_stream().cuda_stream))
-    return y, mean, rstd
+    rows, cols, stride, kind = _rows(x, "x")
+    device = x.device
+    at_weight = at_bias = 0
+    weight_kind = kind
+    if weight is not None:
+        at_weight, weight_kind = _columns(weight, "weight", cols, x)
+    if bias is not None:
+        at_bias, bias_kind = _columns(bias, "bias", cols, x)
+        if weight is not None and bias_kind != weight_kind:
+            raise ValueError("bias must have the type of weight")
+        weight_kind = bias_kind
+    if out is None:
+        out = torch.empty_like(x)
+    out_stride = _rows_like(out, "out", x)
+    mean, rstd = _fp32(rows, device), _fp32(rows, device)
+    _launch(device, load_library().mlda_layer_norm, x.data_ptr(), stride, at_weight, at_bias, out.data_ptr(), out_stride,
+            mean.data_ptr(), rstd.data_ptr(), rows, cols, eps, kind, weight_kind)
+    return out, mean, rstd
 
 
-@_with_device
 def layer_norm_backward(grad_y, x, mean, rstd, weight=None, out=None):
     """(grad_x, grad_weight, grad_bias) for the gradient grad_y of layer_norm's y; the last two are of
     the weight's type (without a weight: of x's).  `out` (grad_y or x, for instance) takes grad_x."""
-    rows, cols, stride = _rows(x, "x")
-    _need(grad_y.shape == x.shape and grad_y.dtype == x.dtype and grad_y.device == x.device,
-          "grad_y must have the shape, type and device of x")
-    grad_stride = _rows(grad_y, "grad_y")[2]
-    kind, at_weight, _ = _weight_type(weight, None, x, cols)
-    at_mean = _like(mean, "mean", (rows,), torch.float32, x.device)
-    at_rstd = _like(rstd, "rstd", (rows,), torch.float32, x.device)
-    grad_x, out_stride = _out_rows(out, "out", x)
-    grad_weight, grad_bias = torch.empty((2, cols), dtype=x.dtype if weight is None else weight.dtype, device=x.device).unbind(0)
-    lib = load_library()
-    held, at, size = _workspace(lib.mlda_layer_norm_workspace_bytes, (rows, cols), x.device)
-    _check(lib.mlda_layer_norm_backward(
-        grad_y.data_ptr(), grad_stride, x.data_ptr(), stride, at_mean, at_rstd, at_weight, grad_x.data_ptr(), out_stride,
-        grad_weight.data_ptr(), grad_bias.data_ptr(), rows, cols, _TYPES[x.dtype], kind, at, size,
-        torch.cuda.current_stream().cuda_stream))
-    return grad_x, grad_weight, grad_bias
+    rows, cols, stride, kind = _rows(x, "x")
+    device = x.device
+    grad_stride = _rows_like(grad_y, "grad_y", x)
+    at_weight, weight_kind, dtype = 0, kind, x.dtype
+    if weight is not None:
+        at_weight, weight_kind = _columns(weight, "weight", cols, x)
+        dtype = weight.dtype
+    at_mean = _like(mean, "mean", (rows,), torch.float32, device)
+    at_rstd = _like(rstd, "rstd", (rows,), torch.float32, device)
+    if out is None:
+        out = torch.empty_like(x)
+    out_stride = _rows_like(out, "out", x)
+    grad_weight = torch.empty(cols, dtype=dtype, device=device)
+    grad_bias = torch.empty(cols, dtype=dtype, device=device)
+    size = _workspace_bytes("mlda_layer_norm_workspace_bytes", rows, cols)
+    held, at = _workspace(size, device)
+    _launch(device, load_library().mlda_layer_norm_backward, grad_y.data_ptr(), grad_stride, x.data_ptr(), stride, at_mean, at_rstd,
+            at_weight, out.data_ptr(), out_stride, grad_weight.data_ptr(), grad_bias.data_ptr(), rows, cols, kind, weight_kind, at, size)
+    return out, grad_weight, grad_bias
 
 
 def _documents(logits, tokens, row_ptr):
     """Checks logits, tokens and row_ptr; the arguments that the library's calls begin with."""
-    rows, vocab, stride = _rows(logits, "logits")
-    n = tokens.numel()
-    at = _like(tokens, "tokens", (n,), torch.int32, logits.device)
-    if row_ptr is None:
-        _need(n == rows, "without row_ptr there must be one token to a row")
-        at_rows = 0
+    rows, vocab, stride, kind = _rows(logits, "logits")
+    device = logits.device
+    n = tokens.numel() if isinstance(tokens, torch.Tensor) else -1
+    at = _like(tokens, "tokens", (n,), torch.int32, device)
+    if row_ptr is not None:
+        at_rows = _like(row_ptr, "row_ptr", (rows + 1,), torch.int64, device)
     else:
-        at_rows = _like(row_ptr, "row_ptr", (rows + 1,), torch.int64, logits.device)
-    return logits.data_ptr(), stride, rows, vocab, _TYPES[logits.dtype], at, at_rows, n
+        at_rows = 0
+        if n != rows:
+            raise ValueError("without row_ptr there must be one token to a row")
+    return logits.data_ptr(), stride, rows, vocab, kind, at, at_rows, n
 
 
-@_with_device
 def token_logprobs(logits, tokens, row_ptr=None, alternatives: int = 0, entropy: bool = False) -> TokenLogprobs:
     """Log-probabilities of tokens (int32 words) under the softmax of their rows of logits [rows, vocab]:
     row r has the tokens row_ptr[r] .. row_ptr[r+1]-1 (int64, on the GPU, its last entry at most the number
@@ -163,22 +173,25 @@ def token_logprobs(logits, tokens, row_ptr=None, alternatives: int = 0, entropy:
     likeliest words, ties to the lowest; with `entropy` the entropies."""
     args = _documents(logits, tokens, row_ptr)
     rows, vocab, device = args[2], args[3], logits.device
-    _need(0 <= alternatives <= min(MAX_ALTERNATIVES, vocab), f"alternatives must be in 0 .. {min(MAX_ALTERNATIVES, vocab)}")
-    logprobs = torch.empty(args[7], dtype=torch.float32, device=device)
-    stats = torch.empty((rows, 2), dtype=torch.float32, device=device)
-    entropies = torch.empty(rows, dtype=torch.float32, device=device) if entropy else None
-    top_ids = torch.empty((rows, alternatives), dtype=torch.int32, device=device) if alternatives else None
-    top_logprobs = torch.empty((rows, alternatives), dtype=torch.float32, device=device) if alternatives else None
-    lib = load_library()
-    held, at, size = _workspace(lib.mlda_token_logprobs_workspace_bytes, (rows, vocab, alternatives, args[4]), device)
-    _check(lib.mlda_token_logprobs(
-        *args, alternatives, logprobs.data_ptr(), stats.data_ptr(), entropies.data_ptr() if entropy else 0,
-        top_ids.data_ptr() if alternatives else 0, top_logprobs.data_ptr() if alternatives else 0, at, size,
-        torch.cuda.current_stream().cuda_stream))
+    if not 0 <= alternatives <= min(MAX_ALTERNATIVES, vocab):
+        raise ValueError(f"alternatives must be in 0 .. {min(MAX_ALTERNATIVES, vocab)}")
+    logprobs, stats = _fp32(args[7], device), _fp32((rows, 2), device)
+    entropies = top_ids = top_logprobs = None
+    at_entropies = at_ids = at_top = 0
+    if entropy:
+        entropies = _fp32(rows, device)
+        at_entropies = entropies.data_ptr()
+    if alternatives:
+        top_ids = torch.empty((rows, alternatives), dtype=torch.int32, device=device)
+        top_logprobs = _fp32((rows, alternatives), device)
+        at_ids, at_top = top_ids.data_ptr(), top_logprobs.data_ptr()
+    size = _workspace_bytes("mlda_token_logprobs_workspace_bytes", rows, vocab, alternatives, args[4])
+    held, at = _workspace(size, device)
+    _launch(device, load_library().mlda_token_logprobs, *args, alternatives, logprobs.data_ptr(), stats.data_ptr(), at_entropies,
+            at_ids, at_top, at, size)
     return TokenLogprobs(logprobs, stats, entropies, top_ids, top_logprobs)
 
 
-@_with_device
 def token_logprobs_backward(grad_logprobs, logits, tokens, stats, row_ptr=None, grad_entropy=None, entropy=None, out=None):
     """The gradient with respect to the logits, for gradients grad_logprobs [n_tokens] of token_logprobs'
     log-probabilities and grad_entropy [rows] (with `entropy` as it came out) of its entropies.  `out` (logits, for
@@ -189,17 +202,18 @@ def token_logprobs_backward(grad_logprobs, logits, tokens, stats, row_ptr=None, 
     at_stats = _like(stats, "stats", (rows, 2), torch.float32, device)
     at_entropy = at_grad_entropy = 0
     if grad_entropy is not None:
-        _need(entropy is not None, "a gradient of the entropy needs the entropy")
+        if entropy is None:
+            raise ValueError("a gradient of the entropy needs the entropy")
         at_grad_entropy = _like(grad_entropy, "grad_entropy", (rows,), torch.float32, device)
         at_entropy = _like(entropy, "entropy", (rows,), torch.float32, device)
-    grad_logits, out_stride = _out_rows(out, "out", logits)
-    _check(load_library().mlda_token_logprobs_backward(
-        *args, at_stats, at_grad, at_entropy, at_grad_entropy, grad_logits.data_ptr(), out_stride,
-        torch.cuda.current_stream().cuda_stream))
-    return grad_logits
+    if out is None:
+        out = torch.empty_like(logits)
+    out_stride = _rows_like(out, "out", logits)
+    _launch(device, load_library().mlda_token_logprobs_backward, *args, at_stats, at_grad, at_entropy, at_grad_entropy,
+            out.data_ptr(), out_stride)
+    return out
 
 
-@_with_device
 def token_logprobs_grad(logits, tokens, weights, row_ptr=None, out=None):
     """A training step's loss and gradient in one: (log-probabilities of the tokens, the gradient of
     sum(weights * log-probabilities) with respect to the logits), weights [n_tokens] fp32.  `out` (logits, for
@@ -207,47 +221,46 @@ def token_logprobs_grad(logits, tokens, weights, row_ptr=None, out=None):
     args = _documents(logits, tokens, row_ptr)
     device = logits.device
     at_weights = _like(weights, "weights", (args[7],), torch.float32, device)
-    logprobs = torch.empty(args[7], dtype=torch.float32, device=device)
-    grad_logits, out_stride = _out_rows(out, "out", logits)
-    lib = load_library()
-    held, at, size = _workspace(lib.mlda_token_logprobs_workspace_bytes, (args[2], args[3], 0, args[4]), device)
-    _check(lib.mlda_token_logprobs_grad(
-        *args, at_weights, logprobs.data_ptr(), grad_logits.data_ptr(), out_stride, at, size,
-        torch.cuda.current_stream().cuda_stream))
-    return logprobs, grad_logits
+    logprobs = _fp32(args[7], device)
+    if out is None:
+        out = torch.empty_like(logits)
+    out_stride = _rows_like(out, "out", logits)
+    size = _workspace_bytes("mlda_token_logprobs_workspace_bytes", args[2], args[3], 0, args[4])
+    held, at = _workspace(size, device)
+    _launch(device, load_library().mlda_token_logprobs_grad, *args, at_weights, logprobs.data_ptr(), out.data_ptr(), out_stride, at, size)
+    return logprobs, out
 
 
 def _tensor_list(tensors, name, device):
     """Addresses, sizes and type codes of contiguous tensors on the device, as host arrays."""
-    n = len(tensors)
     for t in tensors:
-        _need(t.is_contiguous() and t.device == device and t.dtype in _TYPES,
-              f"{name} must be contiguous fp32, bf16 or fp16 tensors on one GPU")
+        if not isinstance(t, torch.Tensor) or not t.is_contiguous() or t.device != device or t.dtype not in _TYPES:
+            raise ValueError(f"{name} must be contiguous fp32, bf16 or fp16 tensors on one GPU")
+    n = len(tensors)
     return ((ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors]), (ctypes.c_int64 * n)(*[t.numel() for t in tensors]),
             (ctypes.c_int32 * n)(*[_TYPES[t.dtype] for t in tensors]))
 
 
 def _grads(tensors, max_norm, out):
     tensors = list(tensors)
-    _need(len(tensors) > 0, "there must be at least one tensor")
-    device = tensors[0].device
-    with _on(device):
-        at, sizes, types = _tensor_list(tensors, "tensors", device)
-        norm = torch.empty((), dtype=torch.float32, device=device)
-        lib = load_library()
-        held, workspace, size = _workspace(lib.mlda_grad_norm_workspace_bytes, (len(tensors),), device)
-        stream = torch.cuda.current_stream().cuda_stream
-        if max_norm is None:
-            _check(lib.mlda_grad_norm(at, sizes, types, len(tensors), norm.data_ptr(), workspace, size, stream))
-            return norm
-        to = at
-        if out is not None:
-            out = list(out)
-            _need(len(out) == len(tensors) and all(o.dtype == t.dtype and o.shape == t.shape for o, t in zip(out, tensors)),
-                  "out must have a tensor of the shape and type of each of tensors")
-            to = _tensor_list(out, "out", device)[0]
-        _check(lib.mlda_clip_grads(at, to, sizes, types, len(tensors), max_norm, norm.data_ptr(), workspace, size, stream))
+    if not tensors or not isinstance(tensors[0], torch.Tensor) or not tensors[0].is_cuda:
+        raise ValueError("there must be at least one tensor, on a GPU: there is no CPU path")
+    n, device = len(tensors), tensors[0].device
+    at, sizes, types = _tensor_list(tensors, "tensors", device)
+    norm = _fp32((), device)
+    size = _workspace_bytes("mlda_grad_norm_workspace_bytes", n)
+    held, workspace = _workspace(size, device)
+    if max_norm is None:
+        _launch(device, load_library().mlda_grad_norm, at, sizes, types, n, norm.data_ptr(), workspace, size)
         return norm
+    to = at
+    if out is not None:
+        out = list(out)
+        if len(out) != n or any(o.dtype != t.dtype or o.shape != t.shape for o, t in zip(out, tensors)):
+            raise ValueError("out must have a tensor of the shape and type of each of tensors")
+        to = _tensor_list(out, "out", device)[0]
+    _launch(device, load_library().mlda_clip_grads, at, to, sizes, types, n, max_norm, norm.data_ptr(), workspace, size)
+    return norm
 
 
 def grad_norm(tensors):
