@@ -215,9 +215,10 @@ __device__ __forceinline__ void join_parts(const RowPart* part, int n, float& m,
     join_lanes(m, s, u);
 }
 
-// The columns [begin, end) of a row by the waves of a workgroup, `waves` of them taking tiles in turn.  `top` may be null.
-template <class T, bool kExtras>
-__device__ __forceinline__ void walk_row(const T* row, int32_t begin, int32_t end, int wave, int waves, LaneSums& sums, Candidates* top) {
+// f(raw pieces, first column) for the tiles of the columns [begin, end) of a row that are this wave's, where `waves` take them in turn;
+// the next tile's loads are on their way meanwhile.  Past the end there is minus infinity.
+template <class T, class F>
+__device__ __forceinline__ void for_tiles(const T* row, int32_t begin, int32_t end, int wave, int waves, F&& f) {
     constexpr int P = kPack<T>, kCols = kTileCols<T>;
     const int lane = lane_id();
     Raw next[kTilePieces];
@@ -237,28 +238,42 @@ __device__ __forceinline__ void walk_row(const T* row, int32_t begin, int32_t en
     if (first < end) load(first);
     for (; first < end; first += (int64_t)waves * kCols) {
         Raw now[kTilePieces];
-        float most = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < kTilePieces; ++j) {
-            now[j] = next[j];
-            float v[P];
-            unpack(now[j], v, T());
-#pragma unroll
-            for (int e = 0; e < P; ++e) most = fmaxf(most, v[e]);
-        }
+        for (int j = 0; j < kTilePieces; ++j) now[j] = next[j];
         if (first + (int64_t)waves * kCols < end) load(first + (int64_t)waves * kCols);
-        sums.raise(most);
+        f(now, first);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ float tile_max(const Raw (&now)[kTilePieces]) {
+    constexpr int P = kPack<T>;
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kTilePieces; ++j) {
+        float v[P];
+        unpack(now[j], v, T());
+#pragma unroll
+        for (int e = 0; e < P; ++e) most = fmaxf(most, v[e]);
+    }
+    return most;
+}
+
+template <class T, bool kEntropy>
+__device__ __forceinline__ LaneSums walk_row(const T* row, int32_t begin, int32_t end, int wave, int waves) {
+    constexpr int P = kPack<T>;
+    LaneSums sums;
+    for_tiles(row, begin, end, wave, waves, [&](const Raw (&now)[kTilePieces], int64_t) {
+        sums.raise(tile_max<T>(now));
 #pragma unroll
         for (int j = 0; j < kTilePieces; ++j) {
             float v[P];
             unpack(now[j], v, T());
 #pragma unroll
-            for (int e = 0; e < P; ++e) sums.add<kExtras>(v[e]);
+            for (int e = 0; e < P; ++e) sums.add<kEntropy>(v[e]);
         }
-        if constexpr (kExtras) {
-            if (top->n && top->wants(most)) top->add(row, first, end);
-        }
-    }
+    });
+    return sums;
 }
 
 // The log-probability of a word: NaN for one outside the vocabulary, 0 for none.
@@ -319,40 +334,101 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, co
     }
 }
 
+// LDS of the search for the likeliest words.
+struct TopLds {
+    float most[kLogprobThreads];                  // each lane's greatest logit
+    uint64_t best[kHeld];                         // candidates, then the answer
+    uint64_t held[kLogprobWaves][kHeld];          // of the waves, where every logit is looked at
+    int32_t chosen[kLogprobThreads];
+    int chosen_n, n, counts[kLogprobWaves];
+};
+
+// The `n` greatest of the columns [begin, end) of a row, in order, into lds.best; returns how many there are (to wave 0).  `most`: this
+// lane's greatest logit of those that walk_row gave it.  The n-th greatest of 64 groups of four lanes' maxima is a bound that n logits
+// reach: the few lanes that reach it (about n of 256) have their columns looked through once more, by everyone, and what
+// reaches the bound is put in order.  Where that is more than the list has room for (ties), or fewer than n lanes have a number,
+// the row is looked through from the start.  By a whole workgroup, whose earlier readers of lds are done.
+template <class T>
+__device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end, float most, int n, TopLds& lds) {
+    constexpr int P = kPack<T>, kCols = kTileCols<T>;
+    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = lane_id();
+    lds.most[tid] = most;
+    if (tid == 0) lds.chosen_n = lds.n = 0;
+    __syncthreads();
+    float group = lds.most[lane];
+#pragma unroll
+    for (int w = 1; w < kLogprobWaves; ++w) group = fmaxf(group, lds.most[w * kWave + lane]);
+    const uint32_t bound = nth_key(order_key(group), n);
+    bool all = bound <= order_key(kLowest);        // (a lane without a number starts from the lowest)
+    if (!all) {
+        if (order_key(most) >= bound) lds.chosen[atomicAdd(&lds.chosen_n, 1)] = tid;
+        __syncthreads();
+        const int tiles = (int)(((int64_t)end - begin + kLogprobWaves * kCols - 1) / (kLogprobWaves * kCols));
+        const int pieces = tiles * kTilePieces, items = lds.chosen_n * pieces;
+        for (int i = tid; i < items; i += kLogprobThreads) {
+            const int who = lds.chosen[i / pieces], piece = i % pieces;
+            const int64_t c = begin + ((int64_t)(piece / kTilePieces) * kLogprobWaves + who / kWave) * kCols +
+                              ((piece % kTilePieces) * kWave + who % kWave) * P;
+            const int there = (int)max((int64_t)0, min((int64_t)P, end - c));
+            float v[P];
+            unpack(load_some(row + c, there, 0.0f), v, T());
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const uint32_t key = order_key(v[e]);
+                if (e < there && key >= bound) {
+                    const int at = atomicAdd(&lds.n, 1);
+                    if (at < kHeld) lds.best[at] = candidate(key, (int32_t)c + e);
+                }
+            }
+        }
+        __syncthreads();
+        all = lds.n > kHeld;
+    }
+    int count = lds.n;
+    if (all) {
+        Candidates top{lds.held[wave], n};
+        for_tiles(row, begin, end, wave, kLogprobWaves, [&](const Raw (&now)[kTilePieces], int64_t first) {
+            if (top.wants(tile_max<T>(now))) top.add(row, first, end);
+        });
+        if (top.count < n) top.sort();
+        if (lane == 0) lds.counts[wave] = top.count;
+        __syncthreads();
+        count = 0;
+        if (wave == 0)                             // the waves' lists, of kMaxAlternatives each at most, one after the other
+            for (int w = 0; w < kLogprobWaves; ++w) {
+                const int held = lds.counts[w];
+                if (lane < held) lds.best[count + lane] = lds.held[w][lane];
+                count += held;
+            }
+    }
+    return wave == 0 ? keep_greatest(lds.best, count, n) : 0;
+}
+
 // Workgroup by workgroup a row, or a segment of one: with one segment all is done, else logprob_join_kernel goes on.
 template <class T, bool kExtras>
 __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a) {
-    __shared__ uint64_t held[kLogprobWaves][kHeld];
+    __shared__ std::conditional_t<kExtras, TopLds, int> lds;
     __shared__ RowPart part[kLogprobWaves];
-    __shared__ uint64_t best[kHeld];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
     const int64_t items = a.rows * a.segments;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t row = item / a.segments;
         const int32_t begin = (int32_t)(item % a.segments) * a.segment_cols;
         const int32_t end = min(a.vocab - begin, a.segment_cols) + begin;
-        LaneSums sums;
-        Candidates top{held[wave], a.top};
-        walk_row<T, kExtras>(static_cast<const T*>(a.logits) + row * a.stride, begin, end, wave, kLogprobWaves, sums, &top);
+        const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+        const LaneSums sums = walk_row<T, kExtras>(logits, begin, end, wave, kLogprobWaves);
         float m = sums.m;
         double s = sums.s, u = sums.u;
         join_lanes(m, s, u);
-        if (kExtras && a.top && top.count < a.top) top.sort();
-        if (lane == 0) part[wave] = RowPart{s, u, m, top.count};
+        if (lane == 0) part[wave] = RowPart{s, u, m, 0};
+        int count = 0;
+        const uint64_t* best = nullptr;
+        if constexpr (kExtras) {
+            if (a.top) count = find_top(logits, begin, end, sums.m, a.top, lds);
+            best = lds.best;
+        }
         __syncthreads();
         join_parts(part, kLogprobWaves, m, s, u);
-        int count = 0;
-        if constexpr (kExtras) {
-            if (a.top && wave == 0) {              // the waves' lists, of kMaxAlternatives each at most, one after the other
-                for (int w = 0; w < kLogprobWaves; ++w) {
-                    const int n = part[w].n;
-                    if (lane < n) best[count + lane] = held[w][lane];
-                    count += n;
-                }
-                count = keep_greatest(best, count, a.top);
-            }
-            __syncthreads();
-        }
         if (a.segments == 1) {
             finish_row<T>(a, row, RowStats(m, s, u), best);
         } else {
@@ -511,8 +587,7 @@ __global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradA
         g.h = kEntropy ? a.grad_entropy[row] : 0.0f;
         g.entropy = kEntropy ? a.entropy[row] : 0.0f;
         if (kLoss && (t1 > t0 || a.stats)) {
-            LaneSums sums;
-            walk_row<T, false>(logits, begin, end, wave, kGradWaves, sums, nullptr);
+            const LaneSums sums = walk_row<T, false>(logits, begin, end, wave, kGradWaves);
             float m = sums.m;
             double s = sums.s, u = 0.0;
             join_lanes(m, s, u);
