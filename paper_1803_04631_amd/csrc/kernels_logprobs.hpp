@@ -99,11 +99,11 @@ __device__ __forceinline__ int keep_greatest(uint64_t* held, int count, int n) {
     return min(count, n);
 }
 
-// The greatest key that at least n lanes' keys reach (0 if fewer than n have one).
+// The greatest key, of those that end in sixteen zeros, that at least n lanes' keys reach (0 if fewer than n have one).
 __device__ __forceinline__ uint32_t nth_key(uint32_t key, int n) {
     uint32_t found = 0;
-#pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll 4
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t with = found | 1u << bit;
         if (__popcll(__ballot(key >= with)) >= n) found = with;
     }
@@ -259,12 +259,15 @@ __device__ __forceinline__ float tile_max(const Raw (&now)[kTilePieces]) {
     return most;
 }
 
-template <class T, bool kEntropy>
-__device__ __forceinline__ LaneSums walk_row(const T* row, int32_t begin, int32_t end, int wave, int waves) {
+// `seen(greatest logit of the tile)` is called for each tile of the wave.
+template <class T, bool kEntropy, class Seen>
+__device__ __forceinline__ LaneSums walk_row(const T* row, int32_t begin, int32_t end, int wave, int waves, Seen&& seen) {
     constexpr int P = kPack<T>;
     LaneSums sums;
     for_tiles(row, begin, end, wave, waves, [&](const Raw (&now)[kTilePieces], int64_t) {
-        sums.raise(tile_max<T>(now));
+        const float most = tile_max<T>(now);
+        seen(most);
+        sums.raise(most);
 #pragma unroll
         for (int j = 0; j < kTilePieces; ++j) {
             float v[P];
@@ -335,19 +338,44 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, co
 }
 
 // LDS of the search for the likeliest words.
+constexpr int kStretches = 16;                    // a wave's tiles are grouped into as many stretches, at most
 struct TopLds {
-    float most[kLogprobThreads];                  // each lane's greatest logit
+    float stretch[kStretches][kLogprobThreads];   // each lane's greatest logit of each stretch
+    float most[kLogprobThreads];                  // and of all
     uint64_t best[kHeld];                         // candidates, then the answer
     uint64_t held[kLogprobWaves][kHeld];          // of the waves, where every logit is looked at
-    int32_t chosen[kLogprobThreads];
+    int32_t chosen[kLogprobThreads];              // lane and stretch
     int chosen_n, n, counts[kLogprobWaves];
 };
 
+// Keeps a lane's maxima by stretches of `tiles` tiles.
+struct StretchMost {
+    TopLds& lds;
+    int tiles, in = 0, at = 0;
+    float most = -INFINITY;
+
+    __device__ __forceinline__ void operator()(float tile) {
+        most = in ? fmaxf(most, tile) : tile;
+        lds.stretch[at][threadIdx.x] = most;
+        if (++in == tiles) {
+            in = 0;
+            ++at;
+        }
+    }
+};
+
+template <class T>
+__device__ __forceinline__ int stretch_tiles(int32_t begin, int32_t end) {
+    constexpr int64_t kGroupCols = (int64_t)kLogprobWaves * kTileCols<T>;
+    const int64_t tiles = ((int64_t)end - begin + kGroupCols - 1) / kGroupCols;
+    return (int)((tiles + kStretches - 1) / kStretches);
+}
+
 // The `n` greatest of the columns [begin, end) of a row, in order, into lds.best; returns how many there are (to wave 0).  `most`: this
-// lane's greatest logit of those that walk_row gave it.  The n-th greatest of 64 groups of four lanes' maxima is a bound that n logits
-// reach: the few lanes that reach it (about n of 256) have their columns looked through once more, by everyone, and what
-// reaches the bound is put in order.  Where that is more than the list has room for (ties), or fewer than n lanes have a number,
-// the row is looked through from the start.  By a whole workgroup, whose earlier readers of lds are done.
+// lane's greatest logit of those that walk_row gave it; lds.stretch is written.  The n-th greatest of 64 groups of four lanes' maxima is
+// a bound that n logits reach: the few stretches of few lanes that reach it (about n of some thousand) are looked through once
+// more, by everyone, and what reaches the bound is put in order.  Where that is more than the lists have room for (ties), or
+// fewer than n lanes have a number, the row is looked through from the start.  By a whole workgroup.
 template <class T>
 __device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end, float most, int n, TopLds& lds) {
     constexpr int P = kPack<T>, kCols = kTileCols<T>;
@@ -361,14 +389,21 @@ __device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end
     const uint32_t bound = nth_key(order_key(group), n);
     bool all = bound <= order_key(kLowest);        // (a lane without a number starts from the lowest)
     if (!all) {
-        if (order_key(most) >= bound) lds.chosen[atomicAdd(&lds.chosen_n, 1)] = tid;
+        const int tiles = stretch_tiles<T>(begin, end);
+        if (order_key(most) >= bound) {
+            const int64_t first = begin + (int64_t)wave * kCols, step = (int64_t)kLogprobWaves * kCols * tiles;
+            for (int i = 0; first + i * step < end; ++i)
+                if (order_key(lds.stretch[i][tid]) >= bound) {
+                    const int at = atomicAdd(&lds.chosen_n, 1);
+                    if (at < kLogprobThreads) lds.chosen[at] = i * kLogprobThreads + tid;
+                }
+        }
         __syncthreads();
-        const int tiles = (int)(((int64_t)end - begin + kLogprobWaves * kCols - 1) / (kLogprobWaves * kCols));
-        const int pieces = tiles * kTilePieces, items = lds.chosen_n * pieces;
+        const int pieces = tiles * kTilePieces, chosen = min(lds.chosen_n, kLogprobThreads), items = chosen * pieces;
         for (int i = tid; i < items; i += kLogprobThreads) {
-            const int who = lds.chosen[i / pieces], piece = i % pieces;
-            const int64_t c = begin + ((int64_t)(piece / kTilePieces) * kLogprobWaves + who / kWave) * kCols +
-                              ((piece % kTilePieces) * kWave + who % kWave) * P;
+            const int which = lds.chosen[i / pieces], piece = i % pieces, who = which % kLogprobThreads;
+            const int64_t tile = (int64_t)(which / kLogprobThreads) * tiles + piece / kTilePieces;
+            const int64_t c = begin + (tile * kLogprobWaves + who / kWave) * kCols + ((piece % kTilePieces) * kWave + who % kWave) * P;
             const int there = (int)max((int64_t)0, min((int64_t)P, end - c));
             float v[P];
             unpack(load_some(row + c, there, 0.0f), v, T());
@@ -382,7 +417,7 @@ __device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end
             }
         }
         __syncthreads();
-        all = lds.n > kHeld;
+        all = lds.n > kHeld || lds.chosen_n > kLogprobThreads;
     }
     int count = lds.n;
     if (all) {
@@ -416,7 +451,13 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a)
         const int32_t begin = (int32_t)(item % a.segments) * a.segment_cols;
         const int32_t end = min(a.vocab - begin, a.segment_cols) + begin;
         const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
-        const LaneSums sums = walk_row<T, kExtras>(logits, begin, end, wave, kLogprobWaves);
+        LaneSums sums;
+        if constexpr (kExtras) {
+            StretchMost seen{lds, stretch_tiles<T>(begin, end)};
+            sums = walk_row<T, true>(logits, begin, end, wave, kLogprobWaves, [&](float tile) { if (a.top) seen(tile); });
+        } else {
+            sums = walk_row<T, false>(logits, begin, end, wave, kLogprobWaves, [](float) {});
+        }
         float m = sums.m;
         double s = sums.s, u = sums.u;
         join_lanes(m, s, u);
@@ -587,7 +628,7 @@ __global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradA
         g.h = kEntropy ? a.grad_entropy[row] : 0.0f;
         g.entropy = kEntropy ? a.entropy[row] : 0.0f;
         if (kLoss && (t1 > t0 || a.stats)) {
-            const LaneSums sums = walk_row<T, false>(logits, begin, end, wave, kGradWaves);
+            const LaneSums sums = walk_row<T, false>(logits, begin, end, wave, kGradWaves, [](float) {});
             float m = sums.m;
             double s = sums.s, u = 0.0;
             join_lanes(m, s, u);
