@@ -19,12 +19,11 @@ namespace mlda {
 
 constexpr int kMaxAlternatives = 32;
 constexpr int kHeld = 128;                       // candidates a wave holds before it sorts them: two a lane
-constexpr int kTilePieces = 4;                   // 16-byte pieces of a row that a lane has on their way
+constexpr int kTilePieces = 2;                   // 16-byte pieces of a row that a lane has on their way
 constexpr float kLog2E = 1.44269504088896340736f;
 constexpr float kLowest = -3.402823466e+38f;
 constexpr float kVanished = -200.0f;             // exponentials of less are 0 in fp32: what they are multiplied with may stay finite
-constexpr int kLogprobThreads = 256;
-constexpr int kLogprobWaves = kLogprobThreads / kWave;
+constexpr int kLogprobWaves = 4;                 // of a workgroup with a row, or a segment of one; one wave for a short row
 
 template <class T> constexpr int kTileCols = kWave * kTilePieces * kPack<T>;    // columns of a wave's tile
 
@@ -320,7 +319,7 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, co
     const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
     int64_t begin, end;
     row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
-    for (int64_t t = begin + threadIdx.x; t < end; t += kLogprobThreads)
+    for (int64_t t = begin + threadIdx.x; t < end; t += blockDim.x)
         a.logprobs[t] = word_logprob(logits, a.tokens[t], a.vocab, st.m, st.log_s);
     if (threadIdx.x == 0) {
         if (a.stats) {
@@ -339,18 +338,21 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, co
 
 // LDS of the search for the likeliest words.
 constexpr int kStretches = 16;                    // a wave's tiles are grouped into as many stretches, at most
+template <int kWaves>
 struct TopLds {
-    float stretch[kStretches][kLogprobThreads];   // each lane's greatest logit of each stretch
-    float most[kLogprobThreads];                  // and of all
+    static constexpr int kLanes = kWaves * kWave;
+    float stretch[kStretches][kLanes];            // each lane's greatest logit of each stretch
+    float most[kLanes];                           // and of all
     uint64_t best[kHeld];                         // candidates, then the answer
-    uint64_t held[kLogprobWaves][kHeld];          // of the waves, where every logit is looked at
-    int32_t chosen[kLogprobThreads];              // lane and stretch
-    int chosen_n, n, counts[kLogprobWaves];
+    uint64_t held[kWaves][kHeld];                 // of the waves, where every logit is looked at
+    int32_t chosen[kLanes];                       // lane and stretch
+    int chosen_n, n, counts[kWaves];
 };
 
 // Keeps a lane's maxima by stretches of `tiles` tiles.
+template <int kWaves>
 struct StretchMost {
-    TopLds& lds;
+    TopLds<kWaves>& lds;
     int tiles, in = 0, at = 0;
     float most = -INFINITY;
 
@@ -364,46 +366,46 @@ struct StretchMost {
     }
 };
 
-template <class T>
+template <class T, int kWaves>
 __device__ __forceinline__ int stretch_tiles(int32_t begin, int32_t end) {
-    constexpr int64_t kGroupCols = (int64_t)kLogprobWaves * kTileCols<T>;
+    constexpr int64_t kGroupCols = (int64_t)kWaves * kTileCols<T>;
     const int64_t tiles = ((int64_t)end - begin + kGroupCols - 1) / kGroupCols;
     return (int)((tiles + kStretches - 1) / kStretches);
 }
 
 // The `n` greatest of the columns [begin, end) of a row, in order, into lds.best; returns how many there are (to wave 0).  `most`: this
-// lane's greatest logit of those that walk_row gave it; lds.stretch is written.  The n-th greatest of 64 groups of four lanes' maxima is
+// lane's greatest logit of those that walk_row gave it; lds.stretch is written.  The n-th greatest of the maxima of 64 groups of lanes is
 // a bound that n logits reach: the few stretches of few lanes that reach it (about n of some thousand) are looked through once
 // more, by everyone, and what reaches the bound is put in order.  Where that is more than the lists have room for (ties), or
 // fewer than n lanes have a number, the row is looked through from the start.  By a whole workgroup.
-template <class T>
-__device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end, float most, int n, TopLds& lds) {
-    constexpr int P = kPack<T>, kCols = kTileCols<T>;
+template <class T, int kWaves>
+__device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end, float most, int n, TopLds<kWaves>& lds) {
+    constexpr int P = kPack<T>, kCols = kTileCols<T>, kLanes = kWaves * kWave;
     const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = lane_id();
     lds.most[tid] = most;
     if (tid == 0) lds.chosen_n = lds.n = 0;
     __syncthreads();
     float group = lds.most[lane];
 #pragma unroll
-    for (int w = 1; w < kLogprobWaves; ++w) group = fmaxf(group, lds.most[w * kWave + lane]);
+    for (int w = 1; w < kWaves; ++w) group = fmaxf(group, lds.most[w * kWave + lane]);
     const uint32_t bound = nth_key(order_key(group), n);
     bool all = bound <= order_key(kLowest);        // (a lane without a number starts from the lowest)
     if (!all) {
-        const int tiles = stretch_tiles<T>(begin, end);
+        const int tiles = stretch_tiles<T, kWaves>(begin, end);
         if (order_key(most) >= bound) {
-            const int64_t first = begin + (int64_t)wave * kCols, step = (int64_t)kLogprobWaves * kCols * tiles;
+            const int64_t first = begin + (int64_t)wave * kCols, step = (int64_t)kWaves * kCols * tiles;
             for (int i = 0; first + i * step < end; ++i)
                 if (order_key(lds.stretch[i][tid]) >= bound) {
                     const int at = atomicAdd(&lds.chosen_n, 1);
-                    if (at < kLogprobThreads) lds.chosen[at] = i * kLogprobThreads + tid;
+                    if (at < kLanes) lds.chosen[at] = i * kLanes + tid;
                 }
         }
         __syncthreads();
-        const int pieces = tiles * kTilePieces, chosen = min(lds.chosen_n, kLogprobThreads), items = chosen * pieces;
-        for (int i = tid; i < items; i += kLogprobThreads) {
-            const int which = lds.chosen[i / pieces], piece = i % pieces, who = which % kLogprobThreads;
-            const int64_t tile = (int64_t)(which / kLogprobThreads) * tiles + piece / kTilePieces;
-            const int64_t c = begin + (tile * kLogprobWaves + who / kWave) * kCols + ((piece % kTilePieces) * kWave + who % kWave) * P;
+        const int pieces = tiles * kTilePieces, chosen = min(lds.chosen_n, kLanes), items = chosen * pieces;
+        for (int i = tid; i < items; i += kLanes) {
+            const int which = lds.chosen[i / pieces], piece = i % pieces, who = which % kLanes;
+            const int64_t tile = (int64_t)(which / kLanes) * tiles + piece / kTilePieces;
+            const int64_t c = begin + (tile * kWaves + who / kWave) * kCols + ((piece % kTilePieces) * kWave + who % kWave) * P;
             const int there = (int)max((int64_t)0, min((int64_t)P, end - c));
             float v[P];
             unpack(load_some(row + c, there, 0.0f), v, T());
@@ -417,12 +419,12 @@ __device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end
             }
         }
         __syncthreads();
-        all = lds.n > kHeld || lds.chosen_n > kLogprobThreads;
+        all = lds.n > kHeld || lds.chosen_n > kLanes;
     }
     int count = lds.n;
     if (all) {
         Candidates top{lds.held[wave], n};
-        for_tiles(row, begin, end, wave, kLogprobWaves, [&](const Raw (&now)[kTilePieces], int64_t first) {
+        for_tiles(row, begin, end, wave, kWaves, [&](const Raw (&now)[kTilePieces], int64_t first) {
             if (top.wants(tile_max<T>(now))) top.add(row, first, end);
         });
         if (top.count < n) top.sort();
@@ -430,7 +432,7 @@ __device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end
         __syncthreads();
         count = 0;
         if (wave == 0)                             // the waves' lists, of kMaxAlternatives each at most, one after the other
-            for (int w = 0; w < kLogprobWaves; ++w) {
+            for (int w = 0; w < kWaves; ++w) {
                 const int held = lds.counts[w];
                 if (lane < held) lds.best[count + lane] = lds.held[w][lane];
                 count += held;
@@ -440,10 +442,10 @@ __device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end
 }
 
 // Workgroup by workgroup a row, or a segment of one: with one segment all is done, else logprob_join_kernel goes on.
-template <class T, bool kExtras>
-__global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a) {
-    __shared__ std::conditional_t<kExtras, TopLds, int> lds;
-    __shared__ RowPart part[kLogprobWaves];
+template <class T, bool kExtras, int kWaves>
+__global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) {
+    __shared__ std::conditional_t<kExtras, TopLds<kWaves>, int> lds;
+    __shared__ RowPart part[kWaves];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
     const int64_t items = a.rows * a.segments;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -453,10 +455,10 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a)
         const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
         LaneSums sums;
         if constexpr (kExtras) {
-            StretchMost seen{lds, stretch_tiles<T>(begin, end)};
-            sums = walk_row<T, true>(logits, begin, end, wave, kLogprobWaves, [&](float tile) { if (a.top) seen(tile); });
+            StretchMost<kWaves> seen{lds, stretch_tiles<T, kWaves>(begin, end)};
+            sums = walk_row<T, true>(logits, begin, end, wave, kWaves, [&](float tile) { if (a.top) seen(tile); });
         } else {
-            sums = walk_row<T, false>(logits, begin, end, wave, kLogprobWaves, [](float) {});
+            sums = walk_row<T, false>(logits, begin, end, wave, kWaves, [](float) {});
         }
         float m = sums.m;
         double s = sums.s, u = sums.u;
@@ -469,7 +471,7 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a)
             best = lds.best;
         }
         __syncthreads();
-        join_parts(part, kLogprobWaves, m, s, u);
+        join_parts(part, kWaves, m, s, u);
         if (a.segments == 1) {
             finish_row<T>(a, row, RowStats(m, s, u), best);
         } else {
@@ -482,7 +484,7 @@ __global__ __launch_bounds__(kLogprobThreads) void logprob_kernel(LogprobArgs a)
 
 // Joins the segments of a row.
 template <class T>
-__global__ __launch_bounds__(kLogprobThreads) void logprob_join_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(kLogprobWaves * kWave) void logprob_join_kernel(LogprobArgs a) {
     __shared__ uint64_t held[kLogprobWaves][kHeld];
     __shared__ uint64_t best[kHeld];
     __shared__ int counts[kLogprobWaves];

@@ -121,6 +121,13 @@ void segments_of(int64_t rows, int32_t vocab, int32_t unit, int32_t* segments, i
     *segments = (int32_t)(((int64_t)vocab + *cols - 1) / *cols);
 }
 
+// Many short rows have a wave each instead of a workgroup of four: 4,096 rows of 12,000 bf16 with the 20 likeliest words 27 us against
+// 38, 20,000 of 3,001 49 against 110; but of 100,000 fp32 317 against 284, and 1,024 of 48,001 bf16 33 against 25.
+bool wave_rows(int64_t rows, int32_t vocab, int32_t type) {
+    const int64_t bytes = (int64_t)vocab * (int64_t)type_bytes(type);
+    return bytes <= 4096 || (bytes <= 49152 && rows >= 8 * kCus);
+}
+
 template <class T> constexpr int32_t kLogprobUnit = mlda::kLogprobWaves * mlda::kTileCols<T>;
 
 int32_t logprob_unit(int32_t type) { return type == MLDA_FP32 ? kLogprobUnit<float> : kLogprobUnit<Bf16>; }
@@ -136,11 +143,18 @@ int run_logprobs(mlda::LogprobArgs a, int32_t type, void* workspace, hipStream_t
     segments_of(a.rows, a.vocab, logprob_unit(type), &a.segments, &a.segment_cols);
     a.parts = static_cast<mlda::RowPart*>(workspace);
     a.part_top = reinterpret_cast<uint64_t*>(a.parts + a.rows * a.segments);
-    const dim3 grid((unsigned)std::min(a.rows * a.segments, kMostGroups)), threads(mlda::kLogprobThreads);
+    const dim3 grid((unsigned)std::min(a.rows * a.segments, kMostGroups)), threads(mlda::kLogprobWaves * mlda::kWave);
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        if (a.top || a.entropy) hipLaunchKernelGGL((mlda::logprob_kernel<T, true>), grid, threads, 0, stream, a);
-        else hipLaunchKernelGGL((mlda::logprob_kernel<T, false>), grid, threads, 0, stream, a);
+        constexpr int kWaves = mlda::kLogprobWaves;
+        const bool extras = a.top || a.entropy;
+        if (wave_rows(a.rows, a.vocab, type)) {
+            if (extras) hipLaunchKernelGGL((mlda::logprob_kernel<T, true, 1>), grid, dim3(mlda::kWave), 0, stream, a);
+            else hipLaunchKernelGGL((mlda::logprob_kernel<T, false, 1>), grid, dim3(mlda::kWave), 0, stream, a);
+        } else {
+            if (extras) hipLaunchKernelGGL((mlda::logprob_kernel<T, true, kWaves>), grid, threads, 0, stream, a);
+            else hipLaunchKernelGGL((mlda::logprob_kernel<T, false, kWaves>), grid, threads, 0, stream, a);
+        }
         RC_TRY(launched("logprob_kernel"));
         if (a.segments == 1) return MLDA_OK;
         hipLaunchKernelGGL((mlda::logprob_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostGroups)), threads, 0, stream, a);
