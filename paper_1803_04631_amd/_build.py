@@ -1,14 +1,17 @@
-"""Compile libmlda.so for gfx950 with hipcc (cross-compiles without a GPU)."""
+"""Compile libmlda.so for gfx950 with hipcc (cross-compiles without a GPU), and _tensors.so, the operators' calls
+on torch tensors, with the host compiler."""
 from __future__ import annotations
 
 import os
 import subprocess
+import sysconfig
 import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libmlda.so")
 SOURCES = ["mlda.hip", "operators.hip"]
+TENSORS_PATH = os.path.join(_HERE, "_tensors.so")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -20,24 +23,37 @@ HIPCC_FLAGS = [
 ]
 
 
+def _tensors_command(rocm: str) -> list[str]:
+    """_tensors.so against torch's headers and libraries, and libmlda.so beside it."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+            "-DTORCH_API_INCLUDE_EXTENSION_H", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+            "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            "-isystem", os.path.join(rocm, "include"), "-isystem", sysconfig.get_paths()["include"],
+            "-o", TENSORS_PATH, os.path.join(CSRC, "tensors.cpp"), "-L" + os.path.join(at, "lib"), "-L" + _HERE, "-l:libmlda.so",
+            "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + os.path.join(at, "lib")]
+
+
 def build(verbose: bool = False) -> str:
     """Always compiles, the sources side by side; returns the library path."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    with tempfile.TemporaryDirectory() as objects:
-        running, linked = [], []
-        for source in SOURCES:
-            linked.append(os.path.join(objects, source + ".o"))
-            cmd = [hipcc, *HIPCC_FLAGS, "-c", "-o", linked[-1], os.path.join(CSRC, source)]
+
+    def run(cmds):
+        running = []
+        for cmd in cmds:
             if verbose:
                 print(" ".join(cmd), flush=True)
             running.append((cmd, subprocess.Popen(cmd)))
+        for process in [p for _, p in running]:
+            process.wait()
         for cmd, process in running:
-            if process.wait():
-                for _, other in running:
-                    other.wait()
+            if process.returncode:
                 raise subprocess.CalledProcessError(process.returncode, cmd)
-        cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-o", LIB_PATH, *linked, "-lpthread"]
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        subprocess.check_call(cmd)
+
+    with tempfile.TemporaryDirectory() as objects:
+        linked = [os.path.join(objects, source + ".o") for source in SOURCES]
+        run([hipcc, *HIPCC_FLAGS, "-c", "-o", o, os.path.join(CSRC, source)] for o, source in zip(linked, SOURCES))
+        run([[hipcc, "--offload-arch=gfx950", "-shared", "-Wl,-soname,libmlda.so", "-o", LIB_PATH, *linked, "-lpthread"]])
+    run([_tensors_command(os.environ.get("ROCM_PATH", "/opt/rocm"))])
     return LIB_PATH
