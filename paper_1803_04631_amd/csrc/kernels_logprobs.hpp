@@ -48,6 +48,7 @@ struct LogprobArgs {
     float* top_logprobs;
     int32_t segments;            // of a row, at most a wave's lanes, of segment_cols columns each (a multiple of the workgroup's tiles)
     int32_t segment_cols;
+    bool words_apart;            // the words' log-probabilities are left to logprob_words_kernel
     RowPart* parts;              // [rows][segments]
     uint64_t* part_top;          // [rows][segments][top]
 };
@@ -298,6 +299,39 @@ __device__ __forceinline__ void row_tokens(const int64_t* row_ptr, int64_t n_tok
     }
 }
 
+constexpr int kWordBatch = 4;                     // words that a thread has on their way
+
+// f(token's number, word, is there one) for the tokens [begin, end), `threads` threads side by side; every thread calls it as often.
+template <int kThreads, class F>
+__device__ __forceinline__ void for_words(const int32_t* tokens, int64_t begin, int64_t end, int tid, F&& f) {
+    for (int64_t first = begin; first < end; first += kThreads * kWordBatch) {
+        int64_t t[kWordBatch];
+        int32_t word[kWordBatch];
+        bool there[kWordBatch];
+#pragma unroll
+        for (int k = 0; k < kWordBatch; ++k) {
+            t[k] = first + k * kThreads + tid;
+            there[k] = t[k] < end;
+            word[k] = there[k] ? tokens[t[k]] : -1;
+        }
+        f(t, word, there);
+    }
+}
+
+// Their log-probabilities.
+template <class T, int kThreads>
+__device__ __forceinline__ void word_logprobs(const T* row, const int32_t* tokens, int64_t begin, int64_t end, int tid, int32_t vocab, float m,
+                                              float log_s, float* logprobs) {
+    for_words<kThreads>(tokens, begin, end, tid, [&](const int64_t (&t)[kWordBatch], const int32_t (&word)[kWordBatch], const bool (&there)[kWordBatch]) {
+        float l[kWordBatch];
+#pragma unroll
+        for (int k = 0; k < kWordBatch; ++k) l[k] = word_logprob(row, word[k], vocab, m, log_s);
+#pragma unroll
+        for (int k = 0; k < kWordBatch; ++k)
+            if (there[k]) logprobs[t[k]] = l[k];
+    });
+}
+
 // A row's statistics out of its sums.  No logit above minus infinity: (-inf, 0), entropy 0.
 struct RowStats {
     float m, log_s, entropy;
@@ -314,13 +348,14 @@ struct RowStats {
     }
 };
 
-template <class T>
+template <class T, int kThreads>
 __device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, const RowStats& st, const uint64_t* top) {
-    const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
-    int64_t begin, end;
-    row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
-    for (int64_t t = begin + threadIdx.x; t < end; t += blockDim.x)
-        a.logprobs[t] = word_logprob(logits, a.tokens[t], a.vocab, st.m, st.log_s);
+    if (!a.words_apart) {
+        int64_t begin, end;
+        row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
+        word_logprobs<T, kThreads>(static_cast<const T*>(a.logits) + row * a.stride, a.tokens, begin, end, (int)threadIdx.x, a.vocab, st.m, st.log_s,
+                                   a.logprobs);
+    }
     if (threadIdx.x == 0) {
         if (a.stats) {
             a.stats[2 * row] = st.m;
@@ -333,6 +368,21 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, co
         const float x = key_logit((uint32_t)(c >> 32));
         a.top_ids[row * a.top + threadIdx.x] = candidate_word(c);
         a.top_logprobs[row * a.top + threadIdx.x] = st.m == -INFINITY ? -INFINITY : (x - st.m) - st.log_s;
+    }
+}
+
+// The words of long documents, whose rows' statistics are known: `split` workgroups a row.
+template <class T>
+__global__ __launch_bounds__(kLogprobWaves * kWave) void logprob_words_kernel(LogprobArgs a, int split) {
+    constexpr int kThreads = kLogprobWaves * kWave;
+    for (int64_t item = blockIdx.x; item < a.rows * split; item += gridDim.x) {
+        const int64_t row = item / split;
+        int64_t begin, end;
+        row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
+        const int64_t each = (end - begin + split - 1) / split;
+        begin = min(begin + item % split * each, end);
+        word_logprobs<T, kThreads>(static_cast<const T*>(a.logits) + row * a.stride, a.tokens, begin, min(begin + each, end), (int)threadIdx.x,
+                                   a.vocab, a.stats[2 * row], a.stats[2 * row + 1], a.logprobs);
     }
 }
 
@@ -473,7 +523,7 @@ __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) 
         __syncthreads();
         join_parts(part, kWaves, m, s, u);
         if (a.segments == 1) {
-            finish_row<T>(a, row, RowStats(m, s, u), best);
+            finish_row<T, kWaves * kWave>(a, row, RowStats(m, s, u), best);
         } else {
             if (threadIdx.x == 0) a.parts[item] = RowPart{s, u, m, count};
             if (kExtras && wave == 0 && lane < count) a.part_top[item * a.top + lane] = best[lane];
@@ -518,7 +568,7 @@ __global__ __launch_bounds__(kLogprobWaves * kWave) void logprob_join_kernel(Log
             }
             __syncthreads();
         }
-        finish_row<T>(a, row, RowStats(m, s, u), best);
+        finish_row<T, kLogprobWaves * kWave>(a, row, RowStats(m, s, u), best);
         __syncthreads();
     }
 }
@@ -540,38 +590,29 @@ struct LogprobGradArgs {
     int64_t out_stride;
     int32_t segments;
     int32_t segment_cols;
-    int32_t slots;               // of the words' table, a power of two
+    int32_t slots;               // of the words' table, a power of two, or 0
+    int32_t columns;             // of a range, where each column has a sum
 };
 
-constexpr int kGradThreads = 512;
-constexpr int kGradWaves = kGradThreads / kWave;
+constexpr int kSlotBytes = 12;
 
-// The words' gradients of a row are summed in a table in LDS, as whole numbers: a unit is so small that n of them of the
-// greatest magnitude stay below 2^62, and whole numbers add up to the same in any order.
+// The words' gradients of a row are summed in LDS, as whole numbers: a unit is so small that n of them of the greatest magnitude stay
+// below 2^62, and whole numbers add up to the same in any order.  A word's slot is the next free one from the one that its
+// hash says (at most seven of eight are taken); a row of more words has a sum for each column, range by range.
 struct WordTable {
-    unsigned long long* sums;    // [slots]
+    unsigned long long* sums;    // [slots]; a column each: [columns]
     int32_t* words;              // [slots], -1: free
-    int32_t slots;
+    int32_t slots, shift;
 
-    __device__ __forceinline__ void clear() const {
-        for (int i = (int)threadIdx.x; i < slots; i += kGradThreads) {
-            sums[i] = 0;
-            words[i] = -1;
-        }
-    }
-    // `direct`: the table has a slot for each column from `first` on; else a word goes to the next free slot from the one that
-    // its hash says (at most half of them are taken).
-    __device__ __forceinline__ void add(int32_t word, long long units, bool direct, int32_t first) const {
-        int i = word - first;
-        if (direct) {
-            words[i] = word;
-        } else {
-            i = (int)(((uint32_t)word * 0x9E3779B1u) >> 16) & (slots - 1);
-            for (;;) {
-                const int was = atomicCAS(&words[i], -1, word);
-                if (was == -1 || was == word) break;
-                i = (i + 1) & (slots - 1);
-            }
+    __device__ __forceinline__ WordTable(unsigned long long* lds, int32_t n)
+        : sums(lds), words(reinterpret_cast<int32_t*>(lds + n)), slots(n), shift(__clz(n) + 1) {}
+
+    __device__ __forceinline__ void add(int32_t word, long long units) const {
+        int i = (int)(((uint32_t)word * 0x9E3779B1u) >> shift);
+        for (;;) {
+            const int was = atomicCAS(&words[i], -1, word);
+            if (was == -1 || was == word) break;
+            i = (i + 1) & (slots - 1);
         }
         atomicAdd(&sums[i], (unsigned long long)units);
     }
@@ -590,33 +631,31 @@ struct RowGrad {
     }
 };
 
-template <class T, bool kEntropy, bool kSingle>
-__device__ __forceinline__ void stream_grad(const T* row, T* out, int32_t begin, int32_t end, const RowGrad& g, int32_t word, float word_grad) {
+// The gradient of the columns [begin, end); own(values, first column) adds what a column's own words give.
+template <class T, int kThreads, bool kEntropy, class Own>
+__device__ __forceinline__ void stream_grad(const T* row, T* out, int32_t begin, int32_t end, const RowGrad& g, Own&& own) {
     constexpr int P = kPack<T>;
-    for (int64_t c = begin + (int64_t)threadIdx.x * P; c < end; c += kGradThreads * P) {
+    for (int64_t c = begin + (int64_t)threadIdx.x * P; c < end; c += kThreads * P) {
         const int n = (int)min((int64_t)P, end - c);
         float v[P];
         unpack(load_some(row + c, n, -INFINITY), v, T());
 #pragma unroll
-        for (int e = 0; e < P; ++e) v[e] = g.of<kEntropy>(v[e]);
-        if (kSingle && (uint32_t)(word - (int32_t)c) < (uint32_t)P) {
-#pragma unroll
-            for (int e = 0; e < P; ++e) v[e] += (int32_t)c + e == word ? word_grad : 0.0f;
-        }
+        for (int e = 0; e < P; ++e) v[e] = g.template of<kEntropy>(v[e]);
+        own(v, (int32_t)c, n);
         store_some(out + c, pack(v, T()), n);
     }
 }
 
 // Rows, or segments of rows.  kLoss: the statistics and the words' log-probabilities are found first, by the same workgroup
 // (one segment).  kSingle: one word to a row.  The logits' rows may be the gradient's.
-template <class T, bool kLoss, bool kEntropy, bool kSingle>
-__global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradArgs a) {
+template <class T, int kThreads, bool kLoss, bool kEntropy, bool kSingle>
+__global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs a) {
+    constexpr int P = kPack<T>, kWaves = kThreads / kWave;
     extern __shared__ unsigned long long table_lds[];
-    __shared__ RowPart part[kGradWaves];
-    __shared__ double totals[kGradWaves];
-    __shared__ float largest[kGradWaves];
-    const WordTable table{table_lds, reinterpret_cast<int32_t*>(table_lds + a.slots), a.slots};
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
+    __shared__ RowPart part[kWaves];
+    __shared__ double totals[kWaves];
+    __shared__ float largest[kWaves];
+    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = lane_id();
     const int64_t items = a.rows * a.segments;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t row = item / a.segments;
@@ -629,22 +668,20 @@ __global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradA
         RowGrad g;
         g.h = kEntropy ? a.grad_entropy[row] : 0.0f;
         g.entropy = kEntropy ? a.entropy[row] : 0.0f;
-        if (kLoss && (t1 > t0 || a.stats)) {
-            const LaneSums sums = walk_row<T, false>(logits, begin, end, wave, kGradWaves, [](float) {});
+        if (kLoss && t1 > t0) {
+            const LaneSums sums = walk_row<T, false>(logits, begin, end, wave, kWaves, [](float) {});
             float m = sums.m;
             double s = sums.s, u = 0.0;
             join_lanes(m, s, u);
-            if (lane == 0) part[wave] = RowPart{s, u, m, 0};
-            __syncthreads();
-            join_parts(part, kGradWaves, m, s, u);
+            if (kWaves > 1) {
+                if (lane == 0) part[wave] = RowPart{s, u, m, 0};
+                __syncthreads();
+                join_parts(part, kWaves, m, s, u);
+            }
             const RowStats st(m, s, u);
             g.m = st.m;
             g.log_s = st.log_s;
             g.inv_s = (float)(1.0 / s);
-            if (a.stats && threadIdx.x == 0) {
-                a.stats[2 * row] = st.m;
-                a.stats[2 * row + 1] = st.log_s;
-            }
         } else if (!kLoss) {
             g.m = a.stats[2 * row];
             g.log_s = a.stats[2 * row + 1];
@@ -657,28 +694,41 @@ __global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradA
         double total = 0.0;
         float most = 0.0f;
         int32_t word = -1;
-        for (int64_t t = t0 + (kSingle ? 0 : threadIdx.x); t < t1; t += kGradThreads) {
-            word = a.tokens[t];
-            if (kLoss && (!kSingle || threadIdx.x == 0)) a.logprobs[t] = word_logprob(logits, word, a.vocab, g.m, g.log_s);
-            if (word >= 0 && word < a.vocab) {
-                total += (double)a.grad[t];
-                most = fmaxf(most, fabsf(a.grad[t]));
+        if (kSingle) {
+            word = a.tokens[row];
+            if (kLoss && tid == 0) a.logprobs[row] = word_logprob(logits, word, a.vocab, g.m, g.log_s);
+            if (word >= a.vocab) word = -1;
+            if (word >= 0) {
+                total = (double)a.grad[row];
+                most = fabsf(a.grad[row]);
             }
-        }
-        if (!kSingle) {
+        } else {
+            if (kLoss) word_logprobs<T, kThreads>(logits, a.tokens, t0, t1, tid, a.vocab, g.m, g.log_s, a.logprobs);
+            for_words<kThreads>(a.tokens, t0, t1, tid, [&](const int64_t (&t)[kWordBatch], const int32_t (&w)[kWordBatch], const bool (&)[kWordBatch]) {
+                float own[kWordBatch];
+#pragma unroll
+                for (int k = 0; k < kWordBatch; ++k) own[k] = w[k] >= 0 && w[k] < a.vocab ? a.grad[t[k]] : 0.0f;
+#pragma unroll
+                for (int k = 0; k < kWordBatch; ++k) {
+                    total += (double)own[k];
+                    most = fmaxf(most, fabsf(own[k]));
+                }
+            });
             total = wave_sum(total);
             most = wave_max(most);
-            if (lane == 0) {
-                totals[wave] = total;
-                largest[wave] = most;
-            }
-            __syncthreads();
-            total = 0.0;
-            most = 0.0f;
+            if (kWaves > 1) {
+                if (lane == 0) {
+                    totals[wave] = total;
+                    largest[wave] = most;
+                }
+                __syncthreads();
+                total = 0.0;
+                most = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kGradWaves; ++w) {
-                total += totals[w];
-                most = fmaxf(most, largest[w]);
+                for (int w = 0; w < kWaves; ++w) {
+                    total += totals[w];
+                    most = fmaxf(most, largest[w]);
+                }
             }
         }
         g.total = (float)total;
@@ -687,37 +737,65 @@ __global__ __launch_bounds__(kGradThreads) void logprob_grad_kernel(LogprobGradA
         if (g.m == -INFINITY || (most == 0.0f && total == 0.0 && g.h == 0.0f)) {
             // nothing is allowed, or nothing is wanted: zeros
             if (kLoss) __syncthreads();                            // (logits read above may be written here)
-            for (int64_t c = begin + (int64_t)threadIdx.x * kPack<T>; c < end; c += kGradThreads * kPack<T>)
-                store_some(out + c, Raw{0, 0, 0, 0}, (int)min((int64_t)kPack<T>, end - c));
+            for (int64_t c = begin + (int64_t)tid * P; c < end; c += kThreads * P) store_some(out + c, Raw{0, 0, 0, 0}, (int)min((int64_t)P, end - c));
         } else if (kSingle) {
             if (kLoss) __syncthreads();
-            stream_grad<T, kEntropy, true>(logits, out, begin, end, g, word < a.vocab ? word : -1, (float)total);
+            stream_grad<T, kThreads, kEntropy>(logits, out, begin, end, g, [&](float (&v)[P], int32_t c, int) {
+                if ((uint32_t)(word - c) < (uint32_t)P) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) v[e] += c + e == word ? (float)total : 0.0f;
+                }
+            });
         } else {
+            const WordTable table(table_lds, a.slots);
             const int64_t n = t1 - t0;
-            const bool direct = n > a.slots / 2;
             const int unit = 62 - (n > 1 ? 64 - __clzll(n - 1) : 0) - (finite && most > 0.0f ? ilogbf(most) + 1 : 0);
             const double units = ldexp(1.0, unit), per_unit = ldexp(1.0, -unit);
-            for (int32_t first = begin; first < end; first += direct ? a.slots : end - begin) {
-                const int32_t last = direct ? min(end - first, a.slots) + first : end;
-                table.clear();
-                __syncthreads();
-                for (int64_t t = t0 + threadIdx.x; finite && t < t1; t += kGradThreads) {
-                    const int32_t w = a.tokens[t];
-                    if (w >= first && w < last) table.add(w, (long long)rint((double)a.grad[t] * units), direct, first);
+            // put(word, units) for the words of the columns [first, last)
+            auto each = [&](int32_t first, int32_t last, auto&& put) {
+                if (!finite) return;
+                for_words<kThreads>(a.tokens, t0, t1, tid, [&](const int64_t (&t)[kWordBatch], const int32_t (&w)[kWordBatch], const bool (&)[kWordBatch]) {
+                    float own[kWordBatch];
+#pragma unroll
+                    for (int k = 0; k < kWordBatch; ++k) own[k] = w[k] >= first && w[k] < last ? a.grad[t[k]] : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < kWordBatch; ++k)
+                        if (w[k] >= first && w[k] < last) put(w[k], (long long)rint((double)own[k] * units));
+                });
+            };
+            auto value = [&](unsigned long long sum) { return (float)((double)(long long)sum * per_unit); };
+            if (n <= table.slots / 8 * 7) {
+                for (int i = tid; i < table.slots; i += kThreads) {
+                    table.sums[i] = 0;
+                    table.words[i] = -1;
                 }
                 __syncthreads();
-                // a word's own gradient, before the row is written over
-                for (int i = (int)threadIdx.x; i < a.slots; i += kGradThreads)
-                    if (table.words[i] >= 0) {
-                        const float own = (float)((double)(long long)table.sums[i] * per_unit);
-                        table.sums[i] = (unsigned long long)__float_as_uint(own + g.of<kEntropy>((float)logits[table.words[i]]));
-                    }
+                each(begin, end, [&](int32_t w, long long v) { table.add(w, v); });
                 __syncthreads();
-                stream_grad<T, kEntropy, false>(logits, out, first, last, g, -1, 0.0f);
+                // the words' columns are worked out before the row is written over, and written last
+                for (int i = tid; i < table.slots; i += kThreads) {
+                    const int32_t w = table.words[i];
+                    if (w >= 0) table.sums[i] = (unsigned long long)__float_as_uint(value(table.sums[i]) + g.template of<kEntropy>((float)logits[w]));
+                }
                 __syncthreads();
-                for (int i = (int)threadIdx.x; i < a.slots; i += kGradThreads)
+                stream_grad<T, kThreads, kEntropy>(logits, out, begin, end, g, [](float (&)[P], int32_t, int) {});
+                __syncthreads();
+                for (int i = tid; i < table.slots; i += kThreads)
                     if (table.words[i] >= 0) out[table.words[i]] = (T)__uint_as_float((uint32_t)table.sums[i]);
-                if (direct) __syncthreads();
+            } else {
+                for (int32_t first = begin; first < end; first += a.columns) {
+                    const int32_t last = min(end - first, a.columns) + first;
+                    for (int i = tid; i < last - first; i += kThreads) table.sums[i] = 0;
+                    __syncthreads();
+                    each(first, last, [&](int32_t w, long long v) { atomicAdd(&table.sums[w - first], (unsigned long long)v); });
+                    __syncthreads();
+                    stream_grad<T, kThreads, kEntropy>(logits, out, first, last, g, [&](float (&v)[P], int32_t c, int there) {
+#pragma unroll
+                        for (int e = 0; e < P; ++e)
+                            if (e < there) v[e] += value(table.sums[c + e - first]);
+                    });
+                    __syncthreads();
+                }
             }
         }
         __syncthreads();

@@ -27,6 +27,7 @@ int launched(const char* what) {
 
 constexpr int32_t kMostCols = 1 << 30;        // columns and words are 32-bit in the kernels, with room for a tile past the end
 constexpr int kCus = 256;
+constexpr int64_t kWaveRowBytes = 16384, kGroupRowBytes = 65536;
 constexpr int64_t kMostGroups = 1 << 20;      // of a launch: rows beyond are taken in turn
 
 bool known_type(int32_t t) { return t == MLDA_FP32 || t == MLDA_BF16 || t == MLDA_FP16; }
@@ -121,6 +122,9 @@ void segments_of(int64_t rows, int32_t vocab, int32_t unit, int32_t* segments, i
     *segments = (int32_t)(((int64_t)vocab + *cols - 1) / *cols);
 }
 
+// Where documents are this long on average, their words are looked up by more workgroups than there are rows.
+constexpr int64_t kLongDocument = 2048;
+
 // Many short rows have a wave each instead of a workgroup of four: 4,096 rows of 12,000 bf16 with the 20 likeliest words 27 us against
 // 38, 20,000 of 3,001 49 against 110; but of 100,000 fp32 317 against 284, and 1,024 of 48,001 bf16 33 against 25.
 bool wave_rows(int64_t rows, int32_t vocab, int32_t type) {
@@ -140,6 +144,8 @@ size_t logprob_workspace(int64_t rows, int32_t vocab, int32_t top, int32_t type)
 }
 
 int run_logprobs(mlda::LogprobArgs a, int32_t type, void* workspace, hipStream_t stream) {
+    const int64_t mean_len = a.n_tokens / a.rows;
+    a.words_apart = a.stats && mean_len >= kLongDocument && a.rows < 4 * kCus;
     segments_of(a.rows, a.vocab, logprob_unit(type), &a.segments, &a.segment_cols);
     a.parts = static_cast<mlda::RowPart*>(workspace);
     a.part_top = reinterpret_cast<uint64_t*>(a.parts + a.rows * a.segments);
@@ -148,7 +154,7 @@ int run_logprobs(mlda::LogprobArgs a, int32_t type, void* workspace, hipStream_t
         typedef decltype(t) T;
         constexpr int kWaves = mlda::kLogprobWaves;
         const bool extras = a.top || a.entropy;
-        if (wave_rows(a.rows, a.vocab, type)) {
+        if (wave_rows(a.rows, a.vocab, type) && (mean_len < 512 || a.words_apart)) {
             if (extras) hipLaunchKernelGGL((mlda::logprob_kernel<T, true, 1>), grid, dim3(mlda::kWave), 0, stream, a);
             else hipLaunchKernelGGL((mlda::logprob_kernel<T, false, 1>), grid, dim3(mlda::kWave), 0, stream, a);
         } else {
@@ -156,32 +162,65 @@ int run_logprobs(mlda::LogprobArgs a, int32_t type, void* workspace, hipStream_t
             else hipLaunchKernelGGL((mlda::logprob_kernel<T, false, kWaves>), grid, threads, 0, stream, a);
         }
         RC_TRY(launched("logprob_kernel"));
-        if (a.segments == 1) return MLDA_OK;
-        hipLaunchKernelGGL((mlda::logprob_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostGroups)), threads, 0, stream, a);
-        return launched("logprob_join_kernel");
+        if (a.segments > 1) {
+            hipLaunchKernelGGL((mlda::logprob_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostGroups)), threads, 0, stream, a);
+            RC_TRY(launched("logprob_join_kernel"));
+        }
+        if (!a.words_apart) return MLDA_OK;
+        const int split = (int)std::min<int64_t>(mean_len / 1024, 64);
+        hipLaunchKernelGGL((mlda::logprob_words_kernel<T>), dim3((unsigned)std::min(a.rows * split, kMostGroups)), threads, 0, stream, a, split);
+        return launched("logprob_words_kernel");
     });
 }
 
-// The words' table holds 1,024 words of short documents, 4,096 of long ones (a document with more than half as many is
-// done by ranges of columns).
-int32_t table_slots(int64_t rows, int64_t n_tokens) { return n_tokens <= 128 * rows ? 1024 : 4096; }
+// The words' table has eight slots for each word of a document of mean length (longer ones fit up to seven times that), and so many that
+// a document of more words, done by ranges of columns, has at most some sixty ranges.  Where sums for all columns take no
+// more room there is no table (0 slots); *columns: of a range.  (With four slots a word 1,024 documents of 330 words over 102,000 columns
+// took 182 us, as the few that were too long held up the end; so 143.)
+int32_t table_slots(int64_t rows, int64_t n_tokens, int32_t cols, int32_t* columns) {
+    constexpr int32_t kMostSlots = 8192;
+    int32_t slots = 64;
+    while (slots < kMostSlots && ((int64_t)slots * rows < 8 * n_tokens || slots < cols / 96)) slots *= 2;
+    *columns = slots * mlda::kSlotBytes / 8;
+    if (cols > *columns) return slots;
+    *columns = cols;
+    return 0;
+}
+
+// Threads that share a row.
+int grad_threads(int64_t cols, int32_t type) {
+    const int64_t bytes = cols * (int64_t)type_bytes(type);
+    return bytes <= kWaveRowBytes ? 64 : bytes <= kGroupRowBytes ? 256 : 512;
+}
 
 template <bool kLoss>
 int run_grad(mlda::LogprobGradArgs a, int32_t type, hipStream_t stream) {
     const bool single = !a.row_ptr;
-    a.slots = single ? 0 : table_slots(a.rows, a.n_tokens);
-    const unsigned lds = (unsigned)a.slots * 12u;
-    const dim3 grid((unsigned)std::min(a.rows * a.segments, kMostGroups)), threads(mlda::kGradThreads);
+    a.slots = a.columns = 0;
+    if (!single) a.slots = table_slots(a.rows, a.n_tokens, a.segment_cols, &a.columns);
+    const unsigned lds = (unsigned)std::max(a.slots * mlda::kSlotBytes, a.columns * 8);
+    const dim3 grid((unsigned)std::min(a.rows * a.segments, kMostGroups));
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        if (kLoss || !a.grad_entropy) {
-            if (single) hipLaunchKernelGGL((mlda::logprob_grad_kernel<T, kLoss, false, true>), grid, threads, lds, stream, a);
-            else hipLaunchKernelGGL((mlda::logprob_grad_kernel<T, kLoss, false, false>), grid, threads, lds, stream, a);
-        } else {
-            if (single) hipLaunchKernelGGL((mlda::logprob_grad_kernel<T, false, true, true>), grid, threads, lds, stream, a);
-            else hipLaunchKernelGGL((mlda::logprob_grad_kernel<T, false, true, false>), grid, threads, lds, stream, a);
+        auto launch = [&](auto threads) {
+            constexpr int kThreads = decltype(threads)::value;
+            void (*kernel)(mlda::LogprobGradArgs);
+            if (kLoss || !a.grad_entropy)
+                kernel = single ? mlda::logprob_grad_kernel<T, kThreads, kLoss, false, true> : mlda::logprob_grad_kernel<T, kThreads, kLoss, false, false>;
+            else
+                kernel = single ? mlda::logprob_grad_kernel<T, kThreads, false, true, true> : mlda::logprob_grad_kernel<T, kThreads, false, true, false>;
+            if (lds > 48 * 1024) {
+                const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                if (e != hipSuccess) return set_error(MLDA_EHIP, "logprob_grad_kernel's LDS", hipGetErrorString(e));
+            }
+            hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, stream, a);
+            return launched("logprob_grad_kernel");
+        };
+        switch (a.n_tokens / a.rows > 512 ? 512 : grad_threads(a.segment_cols, type)) {
+        case 64: return launch(std::integral_constant<int, 64>());
+        case 256: return launch(std::integral_constant<int, 256>());
+        default: return launch(std::integral_constant<int, 512>());
         }
-        return launched("logprob_grad_kernel");
     });
 }
 
@@ -353,7 +392,7 @@ int mlda_token_logprobs(const void* logits, int64_t stride, int64_t rows, int32_
     if (need && (!dev_workspace || !aligned(dev_workspace, 8))) return refuse("log-probabilities: the workspace is null or not aligned");
     if (workspace_bytes < need) return set_error(MLDA_ENOMEM, "log-probabilities: the workspace is smaller than mlda_token_logprobs_workspace_bytes");
     const mlda::LogprobArgs a{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, alternatives, logprobs, stats, entropy,
-                              top_ids, top_logprobs, 1, vocab, nullptr, nullptr};
+                              top_ids, top_logprobs, 1, vocab, false, nullptr, nullptr};
     return run_logprobs(a, type, dev_workspace, (hipStream_t)hip_stream);
 }
 
@@ -367,8 +406,8 @@ int mlda_token_logprobs_backward(const void* logits, int64_t stride, int64_t row
     if (!stats || (n_tokens > 0 && !grad_logprobs)) return refuse("log-probabilities: stats or grad_logprobs are null");
     if (grad_entropy && !entropy) return refuse("log-probabilities: a gradient of the entropy needs the entropy");
     mlda::LogprobGradArgs a{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, grad_logprobs, const_cast<float*>(stats), entropy,
-                            grad_entropy, nullptr, grad_logits, grad_stride, 1, vocab, 0};
-    segments_of(rows, vocab, 2 * mlda::kGradThreads * (int32_t)(16 / type_bytes(type)), &a.segments, &a.segment_cols);
+                            grad_entropy, nullptr, grad_logits, grad_stride, 1, vocab, 0, 0};
+    segments_of(rows, vocab, 1024 * (int32_t)(16 / type_bytes(type)), &a.segments, &a.segment_cols);
     return run_grad<false>(a, type, (hipStream_t)hip_stream);
 }
 
@@ -388,13 +427,13 @@ int mlda_token_logprobs_grad(const void* logits, int64_t stride, int64_t rows, i
             return set_error(MLDA_ENOMEM, "log-probabilities: the workspace is smaller than mlda_token_logprobs_workspace_bytes");
         float* stats = reinterpret_cast<float*>(static_cast<char*>(dev_workspace) + parts);
         const mlda::LogprobArgs f{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, 0, logprobs, stats, nullptr,
-                                  nullptr, nullptr, 1, vocab, nullptr, nullptr};
+                                  nullptr, nullptr, 1, vocab, false, nullptr, nullptr};
         RC_TRY(run_logprobs(f, type, dev_workspace, stream));
         return mlda_token_logprobs_backward(logits, stride, rows, vocab, type, tokens, row_ptr, n_tokens, stats, weights, nullptr,
                                             nullptr, grad_logits, grad_stride, hip_stream);
     }
     const mlda::LogprobGradArgs a{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, weights, nullptr, nullptr, nullptr, logprobs,
-                                  grad_logits, grad_stride, 1, vocab, 0};
+                                  grad_logits, grad_stride, 1, vocab, 0, 0};
     return run_grad<true>(a, type, stream);
 }
 
