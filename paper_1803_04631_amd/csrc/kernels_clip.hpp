@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kClipThreads) void square_sums_kernel(ClipArgs a) {
 #pragma unroll
             for (int j = 0; j < kClipUnit / (kClipThreads * P); ++j) take(r[j]);
         } else {
-            for (int c = (int)threadIdx.x * P; c < n; c += kClipThreads * P) take(load_some(in + c, min(P, n - c), 0.0f));
+            for (int c = (int)threadIdx.x * P; c < n; c += kClipThreads * P) take(load_some(in + c, min(P, n - c), 0.0f, c));
         }
     });
     sum = clip_group_sum(sum, slots);
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kClipThreads) void clip_kernel(ClipArgs a, const do
             for (int j = 0; j < kClipUnit / (kClipThreads * P); ++j) store_raw(out + (j * kClipThreads + (int)threadIdx.x) * P, times(r[j]));
         } else {
             for (int c = (int)threadIdx.x * P; c < n; c += kClipThreads * P)
-                store_some(out + c, times(load_some(in + c, min(P, n - c), 0.0f)), min(P, n - c));
+                store_some(out + c, times(load_some(in + c, min(P, n - c), 0.0f, c)), min(P, n - c));
         }
     });
 }

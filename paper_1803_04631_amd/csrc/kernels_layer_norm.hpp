@@ -3,11 +3,10 @@
 //   mean = sum x / C,  var = sum (x - mean)^2 / C,  rstd = 1 / sqrt(var + eps),  y = (x - mean) rstd w + b
 //   u = (x - mean) rstd,  h = g w:   dx = rstd (h - sum h / C - u sum(h u) / C),  dw = sum_rows g u,  db = sum_rows g
 //
-// Bound by memory (7 and 13 operations an element).  Up to 16,384 columns a row stays in the registers of a team of lanes
-// from its one read to its one write: 16 lanes, a wave, or a workgroup, by the number of columns.  Teams take row after row, so
-// that weight and bias are read once and the weight's gradient is summed in registers; the next row's loads are
-// on their way while a row is worked on.  Sums are fp32 in a fixed order, the deviations' squares are taken
-// after the mean is known.
+// Bound by memory (7 and 13 operations an element).  A row is held by a team of lanes, so many 16-byte pieces each, from its one read
+// to its one write: four or sixteen lanes, a wave, or a workgroup, by the bytes of a row.  Teams take row after row, so that
+// weight and bias are read once and the weight's gradient is summed in registers; the next row's loads are on their way
+// while a row is worked on.  Sums are fp32 in a fixed order, the deviations' squares are taken after the mean is known.
 #pragma once
 #include "vec_io.hpp"
 
@@ -42,76 +41,112 @@ struct LayerNormGradArgs {
     int32_t cols;
 };
 
-// P elements of a vector of type W (P of another type make up 16 bytes) from column c on; `fill` past the end.
+// P columns of a vector of type W, as they are loaded: P elements of another type make up 16 bytes.
 template <class W, int P>
-__device__ __forceinline__ void load_columns(const void* at, int32_t c, int32_t cols, float fill, float (&out)[P]) {
-    const W* p = static_cast<const W*>(at);
-#pragma unroll
-    for (int e = 0; e < P; ++e) out[e] = p && c + e < cols ? (float)p[c + e] : fill;
-}
+struct Columns {
+    static constexpr int kRaw = P / kPack<W>;
+    Raw raw[kRaw];
 
-template <class T, class W, int kTeam, int kE>
-__global__ __launch_bounds__(kTeam < 256 ? 256 : kTeam) void layer_norm_kernel(LayerNormArgs a) {
-    constexpr int P = kPack<T>, kPieces = kE / P, kThreads = kTeam < 256 ? 256 : kTeam, kTeams = kThreads / kTeam;
+    // `fill` past the end, and everywhere where there is no vector
+    __device__ __forceinline__ void load(const void* at, int32_t c, int32_t cols, float fill) {
+        const W* p = static_cast<const W*>(at);
+#pragma unroll
+        for (int i = 0; i < kRaw; ++i) raw[i] = load_some(p + c + i * kPack<W>, p ? cols - c - i * kPack<W> : 0, fill, c + i * kPack<W>);
+    }
+    __device__ __forceinline__ void get(float (&out)[P]) const {
+#pragma unroll
+        for (int i = 0; i < kRaw; ++i) {
+            float v[kPack<W>];
+            unpack(raw[i], v, W());
+#pragma unroll
+            for (int e = 0; e < kPack<W>; ++e) out[i * kPack<W> + e] = v[e];
+        }
+    }
+};
+
+constexpr int team_threads(int team) { return team < 256 ? 256 : team; }
+
+// kHeld: weight and bias are kept, and the next row's pieces are loaded ahead.
+template <class T, class W, int kTeam, int kPieces, bool kHeld>
+__global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNormArgs a) {
+    constexpr int P = kPack<T>, kThreads = team_threads(kTeam), kTeams = kThreads / kTeam;
     __shared__ float slots[2][kThreads / kWave];
     const int lane = (int)threadIdx.x % kTeam;
     const int32_t cols = a.cols;
     const float n_cols = (float)cols;              // (a quotient is right where the sum is: a row of equal numbers has no variance)
-    float w[kE], b[kE];
+    Columns<W, P> w[kHeld ? kPieces : 1], b[kHeld ? kPieces : 1];
+    if constexpr (kHeld) {
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-        float v[P];
-        load_columns<W, P>(a.weight, (j * kTeam + lane) * P, cols, 1.0f, v);
-#pragma unroll
-        for (int e = 0; e < P; ++e) w[j * P + e] = v[e];
-        load_columns<W, P>(a.bias, (j * kTeam + lane) * P, cols, 0.0f, v);
-#pragma unroll
-        for (int e = 0; e < P; ++e) b[j * P + e] = v[e];
+        for (int j = 0; j < kPieces; ++j) {
+            w[j].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
+            b[j].load(a.bias, (j * kTeam + lane) * P, cols, 0.0f);
+        }
     }
     const int64_t step = (int64_t)gridDim.x * kTeams;
     int64_t row = (int64_t)blockIdx.x * kTeams + (int)threadIdx.x / kTeam;
-    // (the sums want every lane of a wave: teams of 16 whose rows have run out go on beside the others with a row of zeros)
+    // (the sums want every lane of a wave: teams of fewer whose rows have run out go on beside the others with a row of zeros)
     const int64_t rounds = (a.rows - (int64_t)blockIdx.x * kTeams + step - 1) / step;
-    Raw next[kPieces];
-    auto load_row = [&](int64_t r) {
+    auto load_row = [&](int64_t r, Raw (&to)[kPieces]) {
         const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             const int32_t c = (j * kTeam + lane) * P;
-            next[j] = r < a.rows ? load_some(x + c, min(max(cols - c, 0), P), 0.0f) : Raw{0, 0, 0, 0};
+            to[j] = load_some(x + c, r < a.rows ? cols - c : 0, 0.0f, c);
         }
     };
-    load_row(row);
+    Raw x[kPieces], next[kPieces];
+    if (kHeld) load_row(row, next);
     for (int64_t i = 0; i < rounds; ++i, row += step) {
-        float x[kE];
+        if constexpr (kHeld) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) x[j] = next[j];
+            if (i + 1 < rounds) load_row(row + step, next);
+        } else {
+            load_row(row, x);
+        }
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             float v[P];
-            unpack(next[j], v, T());
+            unpack(x[j], v, T());
 #pragma unroll
-            for (int e = 0; e < P; ++e) { x[j * P + e] = v[e]; sum += v[e]; }
+            for (int e = 0; e < P; ++e) sum += v[e];
         }
-        if (i + 1 < rounds) load_row(row + step);
         const float mean = team_sum<kTeam>(sum, slots[0]) / n_cols;
+        forget(x);
         float squares = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j)
+        for (int j = 0; j < kPieces; ++j) {
+            const int32_t c = (j * kTeam + lane) * P;
+            float v[P];
+            unpack(x[j], v, T());
+            if (c + P <= cols) {
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const float d = x[j * P + e] - mean;
-                x[j * P + e] = d;
-                squares += (j * kTeam + lane) * P + e < cols ? d * d : 0.0f;
+                for (int e = 0; e < P; ++e) squares = __builtin_fmaf(v[e] - mean, v[e] - mean, squares);
+            } else {
+#pragma unroll
+                for (int e = 0; e < P; ++e) squares += c + e < cols ? (v[e] - mean) * (v[e] - mean) : 0.0f;
             }
+        }
         const float rstd = 1.0f / sqrtf(team_sum<kTeam>(squares, slots[1]) / n_cols + a.eps);
+        forget(x);
         if (row < a.rows) {
             T* y = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
-                float v[P];
-#pragma unroll
-                for (int e = 0; e < P; ++e) v[e] = __builtin_fmaf(x[j * P + e] * rstd, w[j * P + e], b[j * P + e]);
                 const int32_t c = (j * kTeam + lane) * P;
+                if constexpr (!kHeld) {
+                    w[0].load(a.weight, c, cols, 1.0f);
+                    b[0].load(a.bias, c, cols, 0.0f);
+                }
+                float v[P], vw[P], vb[P];
+                unpack(x[j], v, T());
+                forget(w[kHeld ? j : 0].raw);
+                forget(b[kHeld ? j : 0].raw);
+                w[kHeld ? j : 0].get(vw);
+                b[kHeld ? j : 0].get(vb);
+#pragma unroll
+                for (int e = 0; e < P; ++e) v[e] = __builtin_fmaf((v[e] - mean) * rstd, vw[e], vb[e]);
                 store_some(y + c, pack(v, T()), min(max(cols - c, 0), P));
             }
             if (lane == 0) {
@@ -135,7 +170,7 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a) 
         float sum = 0.0f;
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             float v[P];
-            unpack(load_some(x + c, (int)min((int64_t)P, cols - c), 0.0f), v, T());
+            unpack(load_some(x + c, (int)min((int64_t)P, cols - c), 0.0f, c), v, T());
 #pragma unroll
             for (int e = 0; e < P; ++e) sum += v[e];
         }
@@ -144,7 +179,7 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a) 
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             const int n = (int)min((int64_t)P, cols - c);
             float v[P];
-            unpack(load_some(x + c, n, 0.0f), v, T());
+            unpack(load_some(x + c, n, 0.0f, c), v, T());
 #pragma unroll
             for (int e = 0; e < P; ++e) squares += e < n ? (v[e] - mean) * (v[e] - mean) : 0.0f;
         }
@@ -152,12 +187,15 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a) 
         // (x and y may be the same rows: what is written below is read by the same thread only)
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             const int n = (int)min((int64_t)P, cols - c);
-            float v[P], w[P], b[P];
-            unpack(load_some(x + c, n, 0.0f), v, T());
-            load_columns<W, P>(a.weight, (int32_t)c, cols, 1.0f, w);
-            load_columns<W, P>(a.bias, (int32_t)c, cols, 0.0f, b);
+            float v[P], vw[P], vb[P];
+            Columns<W, P> w, b;
+            unpack(load_some(x + c, n, 0.0f, c), v, T());
+            w.load(a.weight, (int32_t)c, cols, 1.0f);
+            b.load(a.bias, (int32_t)c, cols, 0.0f);
+            w.get(vw);
+            b.get(vb);
 #pragma unroll
-            for (int e = 0; e < P; ++e) v[e] = __builtin_fmaf((v[e] - mean) * rstd, w[e], b[e]);
+            for (int e = 0; e < P; ++e) v[e] = __builtin_fmaf((v[e] - mean) * rstd, vw[e], vb[e]);
             store_some(y + c, pack(v, T()), n);
         }
         if (threadIdx.x == 0) {
@@ -167,135 +205,156 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a) 
     }
 }
 
-template <class T, class W, int kTeam, int kE>
-__global__ __launch_bounds__(kTeam < 256 ? 256 : kTeam) void layer_norm_grad_kernel(LayerNormGradArgs a) {
-    constexpr int P = kPack<T>, kPieces = kE / P, kThreads = kTeam < 256 ? 256 : kTeam, kTeams = kThreads / kTeam;
-    __shared__ float slots[4][kThreads / kWave];
+// One row's part in the gradient: u and h of a piece.
+template <class T, class W>
+__device__ __forceinline__ void grad_piece(Raw x, Raw g, const Columns<W, kPack<T>>& w, float mean, float rstd, float (&u)[kPack<T>],
+                                           float (&h)[kPack<T>], float (&grad)[kPack<T>]) {
+    unpack(x, u, T());
+    unpack(g, grad, T());
+    w.get(h);
+#pragma unroll
+    for (int e = 0; e < kPack<T>; ++e) {
+        u[e] = (u[e] - mean) * rstd;
+        h[e] *= grad[e];
+    }
+}
+
+// kSums: the weight's and bias' gradients are summed here (kHeld too: the weight is kept, the next row's pieces are loaded ahead).
+template <class T, class W, int kTeam, int kPieces, bool kSums>
+__global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(LayerNormGradArgs a) {
+    constexpr int P = kPack<T>, kThreads = team_threads(kTeam), kTeams = kThreads / kTeam;
+    __shared__ float slots[2][2 * (kThreads / kWave)];
     // sums over the workgroup's teams: [dw or db][column]
-    __shared__ float joined[kTeams > 1 ? 2 * kTeam * kE : 1];
+    __shared__ float joined[kSums && kTeams > 1 ? 2 * kTeam * kPieces * P : 1];
     const int lane = (int)threadIdx.x % kTeam;
     const int32_t cols = a.cols;
     const float n_cols = (float)cols;
-    // (a thousand threads of sixteen columns have no registers left for the weight and the next row)
-    constexpr bool kTight = kTeam == 1024 && kE > 8;
-    float w[kTight ? 1 : kE], dw[kE], db[kE];
+    Columns<W, P> w[kSums ? kPieces : 1];
+    float dw[kSums ? kPieces * P : 1], db[kSums ? kPieces * P : 1];
+    if constexpr (kSums) {
 #pragma unroll
-    for (int j = 0; j < kPieces; ++j) {
-        float v[P];
-        if constexpr (!kTight) load_columns<W, P>(a.weight, (j * kTeam + lane) * P, cols, 1.0f, v);
+        for (int j = 0; j < kPieces; ++j) w[j].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            if constexpr (!kTight) w[j * P + e] = v[e];
-            dw[j * P + e] = db[j * P + e] = 0.0f;
-        }
+        for (int k = 0; k < kPieces * P; ++k) dw[k] = db[k] = 0.0f;
     }
     const int64_t step = (int64_t)gridDim.x * kTeams;
     int64_t row = (int64_t)blockIdx.x * kTeams + (int)threadIdx.x / kTeam;
     const int64_t rounds = (a.rows - (int64_t)blockIdx.x * kTeams + step - 1) / step;
-    Raw next_x[kPieces], next_g[kPieces];
-    float next_mean, next_rstd;
-    auto load_row = [&](int64_t r) {
-        const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
-        const T* g = static_cast<const T*>(a.grad) + r * a.grad_stride;
+    Raw x[kPieces], g[kPieces], next_x[kPieces], next_g[kPieces];
+    float mean, rstd, next_mean, next_rstd;
+    // (columns past the end: the gradient is zero there, and what comes out is not stored)
+    auto load_row = [&](int64_t r, Raw (&to_x)[kPieces], Raw (&to_g)[kPieces], float& to_mean, float& to_rstd) {
+        const T* at_x = static_cast<const T*>(a.x) + r * a.x_stride;
+        const T* at_g = static_cast<const T*>(a.grad) + r * a.grad_stride;
         const bool there = r < a.rows;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             const int32_t c = (j * kTeam + lane) * P;
-            const int n = min(max(cols - c, 0), P);
-            next_x[j] = there ? load_some(x + c, n, 0.0f) : Raw{0, 0, 0, 0};
-            next_g[j] = there ? load_some(g + c, n, 0.0f) : Raw{0, 0, 0, 0};
+            const int n = there ? cols - c : 0;
+            to_x[j] = load_some(at_x + c, n, 0.0f, c);
+            to_g[j] = load_some(at_g + c, n, 0.0f, c);
         }
-        next_mean = there ? a.mean[r] : 0.0f;
-        next_rstd = there ? a.rstd[r] : 0.0f;
+        to_mean = there ? a.mean[r] : 0.0f;
+        to_rstd = there ? a.rstd[r] : 0.0f;
     };
-    if (!kTight) load_row(row);
+    if (kSums) load_row(row, next_x, next_g, next_mean, next_rstd);
     for (int64_t i = 0; i < rounds; ++i, row += step) {
-        if (kTight) load_row(row);
-        float u[kE], h[kE];
-        const float mean = next_mean, rstd = next_rstd;
+        if constexpr (kSums) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                x[j] = next_x[j];
+                g[j] = next_g[j];
+            }
+            mean = next_mean;
+            rstd = next_rstd;
+            if (i + 1 < rounds) load_row(row + step, next_x, next_g, next_mean, next_rstd);
+        } else {
+            load_row(row, x, g, mean, rstd);
+        }
         float sum_h = 0.0f, sum_hu = 0.0f;
-        // (columns past the end: the gradient is zero there, and what comes out is not stored)
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-            float x[P], g[P], here[P];
-            unpack(next_x[j], x, T());
-            unpack(next_g[j], g, T());
-            if constexpr (kTight) load_columns<W, P>(a.weight, (j * kTeam + lane) * P, cols, 1.0f, here);
+            float u[P], h[P], grad[P];
+            if constexpr (!kSums) w[0].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
+            forget(w[kSums ? j : 0].raw);
+            grad_piece<T, W>(x[j], g[j], w[kSums ? j : 0], mean, rstd, u, h, grad);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                const int k = j * P + e;
-                u[k] = (x[e] - mean) * rstd;
-                h[k] = g[e] * (kTight ? here[e] : w[kTight ? 0 : k]);
-                dw[k] = __builtin_fmaf(g[e], u[k], dw[k]);
-                db[k] += g[e];
-                sum_h += h[k];
-                sum_hu = __builtin_fmaf(h[k], u[k], sum_hu);
+                sum_h += h[e];
+                sum_hu = __builtin_fmaf(h[e], u[e], sum_hu);
             }
         }
-        if (!kTight && i + 1 < rounds) load_row(row + step);
-        if (a.grad_x) {
-            // two sums a row, and the barrier of the second parts the first's readers from the next row's writers
-            const float mean_h = team_sum<kTeam>(sum_h, slots[0]) / n_cols;
-            const float mean_hu = team_sum<kTeam>(sum_hu, slots[1]) / n_cols;
-            if (row < a.rows) {
-                T* dx = static_cast<T*>(a.grad_x) + row * a.grad_x_stride;
+        team_sums<kTeam>(sum_h, sum_hu, slots[i & 1]);
+        const float mean_h = sum_h / n_cols, mean_hu = sum_hu / n_cols;
+        forget(x);
+        forget(g);
+        T* dx = row < a.rows && a.grad_x ? static_cast<T*>(a.grad_x) + row * a.grad_x_stride : nullptr;
 #pragma unroll
-                for (int j = 0; j < kPieces; ++j) {
-                    float v[P];
+        for (int j = 0; j < kPieces; ++j) {
+            const int32_t c = (j * kTeam + lane) * P;
+            float u[P], h[P], v[P];
+            if constexpr (!kSums) w[0].load(a.weight, c, cols, 1.0f);
+            forget(w[kSums ? j : 0].raw);
+            grad_piece<T, W>(x[j], g[j], w[kSums ? j : 0], mean, rstd, u, h, v);
+            if constexpr (kSums) {                 // (not beside the sums above: what that needs would be kept until here)
 #pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        const int k = j * P + e;
-                        v[e] = rstd * (h[k] - mean_h - u[k] * mean_hu);
-                    }
-                    const int32_t c = (j * kTeam + lane) * P;
-                    store_some(dx + c, pack(v, T()), min(max(cols - c, 0), P));
+                for (int e = 0; e < P; ++e) {
+                    dw[j * P + e] = __builtin_fmaf(v[e], u[e], dw[j * P + e]);
+                    db[j * P + e] += v[e];
                 }
             }
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[e] = rstd * ((h[e] - mean_h) - u[e] * mean_hu);
+            if (dx) store_some(dx + c, pack(v, T()), min(max(cols - c, 0), P));
         }
     }
-    if (!a.partial) return;
-    float* out = a.partial + (int64_t)blockIdx.x * 2 * cols;
-    if constexpr (kTeams > 1) {
-        // one team after the other, so that the order of the additions is fixed
-        for (int t = 0; t < kTeams; ++t) {
-            if ((int)threadIdx.x / kTeam == t) {
+    if constexpr (kSums) {
+        if (!a.partial) return;
+        float* out = a.partial + (int64_t)blockIdx.x * 2 * cols;
+        if constexpr (kTeams > 1) {
+            // one team after the other, so that the order of the additions is fixed
+            constexpr int kCols = kTeam * kPieces * P;
+            for (int t = 0; t < kTeams; ++t) {
+                if ((int)threadIdx.x / kTeam == t) {
 #pragma unroll
-                for (int j = 0; j < kPieces; ++j)
+                    for (int j = 0; j < kPieces; ++j)
 #pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        const int c = (j * kTeam + lane) * P + e, k = j * P + e;
-                        joined[c] = t ? joined[c] + dw[k] : dw[k];
-                        joined[kTeam * kE + c] = t ? joined[kTeam * kE + c] + db[k] : db[k];
-                    }
-            }
-            __syncthreads();
-        }
-        for (int c = (int)threadIdx.x; c < cols; c += kThreads) {
-            out[c] = joined[c];
-            out[cols + c] = joined[kTeam * kE + c];
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kPieces; ++j)
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const int c = (j * kTeam + lane) * P + e, k = j * P + e;
-                if (c < cols) {
-                    out[c] = dw[k];
-                    out[cols + c] = db[k];
+                        for (int e = 0; e < P; ++e) {
+                            const int c = (j * kTeam + lane) * P + e, k = j * P + e;
+                            joined[c] = t ? joined[c] + dw[k] : dw[k];
+                            joined[kCols + c] = t ? joined[kCols + c] + db[k] : db[k];
+                        }
                 }
+                __syncthreads();
             }
+            for (int c = (int)threadIdx.x; c < cols; c += kThreads) {
+                out[c] = joined[c];
+                out[cols + c] = joined[kCols + c];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const int c = (j * kTeam + lane) * P + e, k = j * P + e;
+                    if (c < cols) {
+                        out[c] = dw[k];
+                        out[cols + c] = db[k];
+                    }
+                }
+        }
     }
 }
 
-// Rows without room in registers: the gradient of x by a workgroup a row, which reads the row twice ...
+// Rows without room in registers: the gradient of x by a workgroup a row, which reads the row twice.
 template <class T, class W>
 __global__ __launch_bounds__(1024) void layer_norm_grad_long_kernel(LayerNormGradArgs a) {
     constexpr int P = kPack<T>;
-    __shared__ float slots[2][16];
+    __shared__ float slots[2][32];
     const int32_t cols = a.cols;
     const float n_cols = (float)cols;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
         const T* grad = static_cast<const T*>(a.grad) + row * a.grad_stride;
         T* dx = static_cast<T*>(a.grad_x) + row * a.grad_x_stride;
@@ -303,15 +362,10 @@ __global__ __launch_bounds__(1024) void layer_norm_grad_long_kernel(LayerNormGra
         float sum_h = 0.0f, sum_hu = 0.0f;
         auto piece = [&](int64_t c, float (&u)[P], float (&h)[P]) {
             const int n = (int)min((int64_t)P, cols - c);
-            float w[P];
-            unpack(load_some(x + c, n, 0.0f), u, T());
-            unpack(load_some(grad + c, n, 0.0f), h, T());
-            load_columns<W, P>(a.weight, (int32_t)c, cols, 1.0f, w);
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-                u[e] = (u[e] - mean) * rstd;
-                h[e] *= w[e];
-            }
+            Columns<W, P> w;
+            float unused[P];
+            w.load(a.weight, (int32_t)c, cols, 1.0f);
+            grad_piece<T, W>(load_some(x + c, n, 0.0f, c), load_some(grad + c, n, 0.0f, c), w, mean, rstd, u, h, unused);
             return n;
         };
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
@@ -323,22 +377,23 @@ __global__ __launch_bounds__(1024) void layer_norm_grad_long_kernel(LayerNormGra
                 sum_hu = __builtin_fmaf(h[e], u[e], sum_hu);
             }
         }
-        const float mean_h = team_sum<1024>(sum_h, slots[0]) / n_cols;
-        const float mean_hu = team_sum<1024>(sum_hu, slots[1]) / n_cols;
+        team_sums<1024>(sum_h, sum_hu, slots[turn]);
+        const float mean_h = sum_h / n_cols, mean_hu = sum_hu / n_cols;
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             float u[P], h[P], v[P];
             const int n = piece(c, u, h);
 #pragma unroll
-            for (int e = 0; e < P; ++e) v[e] = rstd * (h[e] - mean_h - u[e] * mean_hu);
+            for (int e = 0; e < P; ++e) v[e] = rstd * ((h[e] - mean_h) - u[e] * mean_hu);
             store_some(dx + c, pack(v, T()), n);
         }
     }
 }
 
-// ... and the sums over rows by tiles of 64 x kPack columns: workgroup (tile, slab) sums its slab's rows, wave by wave.
+// The sums over rows on their own, by tiles of 64 x kPack columns: workgroup (tile, slab) sums its slab's rows, four to a wave at
+// once.
 template <class T>
 __global__ __launch_bounds__(256) void layer_norm_grad_columns_kernel(LayerNormGradArgs a) {
-    constexpr int P = kPack<T>;
+    constexpr int P = kPack<T>, kAtOnce = 4;
     __shared__ float joined[4][2 * kWave * P];
     const int wave = (int)threadIdx.x / kWave, lane = lane_id();
     const int32_t c = ((int32_t)blockIdx.x * kWave + lane) * P;
@@ -346,15 +401,28 @@ __global__ __launch_bounds__(256) void layer_norm_grad_columns_kernel(LayerNormG
     float dw[P], db[P];
 #pragma unroll
     for (int e = 0; e < P; ++e) dw[e] = db[e] = 0.0f;
-    for (int64_t row = (int64_t)blockIdx.y * 4 + wave; row < a.rows; row += (int64_t)gridDim.y * 4) {
-        float x[P], g[P];
-        unpack(load_some(static_cast<const T*>(a.x) + row * a.x_stride + c, n, 0.0f), x, T());
-        unpack(load_some(static_cast<const T*>(a.grad) + row * a.grad_stride + c, n, 0.0f), g, T());
-        const float mean = a.mean[row], rstd = a.rstd[row];
+    for (int64_t first = ((int64_t)blockIdx.y * 4 + wave) * kAtOnce; first < a.rows; first += (int64_t)gridDim.y * 4 * kAtOnce) {
+        Raw x[kAtOnce], g[kAtOnce];
+        float mean[kAtOnce], rstd[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            dw[e] = __builtin_fmaf(g[e], (x[e] - mean) * rstd, dw[e]);
-            db[e] += g[e];
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int64_t row = first + k;
+            const int there = row < a.rows ? n : 0;
+            x[k] = load_some(static_cast<const T*>(a.x) + row * a.x_stride + c, there, 0.0f, c);
+            g[k] = load_some(static_cast<const T*>(a.grad) + row * a.grad_stride + c, there, 0.0f, c);
+            mean[k] = row < a.rows ? a.mean[row] : 0.0f;
+            rstd[k] = row < a.rows ? a.rstd[row] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            float vx[P], vg[P];
+            unpack(x[k], vx, T());
+            unpack(g[k], vg, T());
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                dw[e] = __builtin_fmaf(vg[e], (vx[e] - mean[k]) * rstd[k], dw[e]);
+                db[e] += vg[e];
+            }
         }
     }
 #pragma unroll
@@ -371,27 +439,32 @@ __global__ __launch_bounds__(256) void layer_norm_grad_columns_kernel(LayerNormG
     }
 }
 
-// The workgroups' sums added up, in their order, and rounded to the weight's type: 64 columns of [dw, db] a workgroup.
+// The workgroups' sums added up, in their order, and rounded to the weight's type: 16 columns of [dw, db] a workgroup, by 64
+// slices of the workgroups.
 template <class W>
 __global__ __launch_bounds__(1024) void layer_norm_grad_final_kernel(const float* partial, int32_t partials, int32_t cols,
                                                                      W* grad_weight, W* grad_bias) {
-    __shared__ float joined[16][kWave];
-    const int slice = (int)threadIdx.x / kWave, lane = lane_id();
-    const int64_t i = (int64_t)blockIdx.x * kWave + lane;
+    constexpr int kCols = 16, kSlices = 64;
+    __shared__ float joined[kSlices][kCols + 1];
+    const int slice = (int)threadIdx.x / kCols, lane = (int)threadIdx.x % kCols;
+    const int64_t i = (int64_t)blockIdx.x * kCols + lane;
     float sum = 0.0f;
     if (i < 2 * (int64_t)cols)
 #pragma unroll 4
-        for (int p = slice; p < partials; p += 16) sum += partial[(int64_t)p * 2 * cols + i];
+        for (int p = slice; p < partials; p += kSlices) sum += partial[(int64_t)p * 2 * cols + i];
     joined[slice][lane] = sum;
     __syncthreads();
-    if (slice != 0 || i >= 2 * (int64_t)cols) return;
-    sum = 0.0f;
-#pragma unroll
-    for (int s = 0; s < 16; ++s) sum += joined[s][lane];
-    if (i < cols) {
-        if (grad_weight) grad_weight[i] = (W)sum;
+    // a column to each group of 16 lanes: four slices a lane, then the lanes
+    const int column = (int)threadIdx.x / 16, part = (int)threadIdx.x % 16;
+    if (threadIdx.x >= kCols * 16) return;
+    sum = (joined[part][column] + joined[part + 16][column]) + (joined[part + 32][column] + joined[part + 48][column]);
+    sum = row16_sum(sum);
+    const int64_t at = (int64_t)blockIdx.x * kCols + column;
+    if (part != 0 || at >= 2 * (int64_t)cols) return;
+    if (at < cols) {
+        if (grad_weight) grad_weight[at] = (W)sum;
     } else if (grad_bias) {
-        grad_bias[i - cols] = (W)sum;
+        grad_bias[at - cols] = (W)sum;
     }
 }
 

@@ -137,7 +137,7 @@ struct Candidates {
         constexpr int P = kPack<T>;
         auto piece = [&](int j, float (&v)[P]) {
             const int64_t c = first + (j * kWave + lane_id()) * P;
-            unpack(load_some(row + c, (int)max((int64_t)0, min((int64_t)P, end - c)), 0.0f), v, T());
+            unpack(load_some(row + c, (int)max((int64_t)0, min((int64_t)P, end - c)), 0.0f, c), v, T());
             return (int32_t)c;
         };
         uint32_t most = 0;
@@ -230,7 +230,7 @@ __device__ __forceinline__ void for_tiles(const T* row, int32_t begin, int32_t e
 #pragma unroll
             for (int j = 0; j < kTilePieces; ++j) {
                 const int64_t c = first + (j * kWave + lane) * P;
-                next[j] = load_some(row + c, (int)max((int64_t)0, min((int64_t)P, end - c)), -INFINITY);
+                next[j] = load_some(row + c, (int)max((int64_t)0, min((int64_t)P, end - c)), -INFINITY, c);
             }
         }
     };
@@ -458,7 +458,7 @@ __device__ __forceinline__ int find_top(const T* row, int32_t begin, int32_t end
             const int64_t c = begin + (tile * kWaves + who / kWave) * kCols + ((piece % kTilePieces) * kWave + who % kWave) * P;
             const int there = (int)max((int64_t)0, min((int64_t)P, end - c));
             float v[P];
-            unpack(load_some(row + c, there, 0.0f), v, T());
+            unpack(load_some(row + c, there, 0.0f, c), v, T());
 #pragma unroll
             for (int e = 0; e < P; ++e) {
                 const uint32_t key = order_key(v[e]);
@@ -638,7 +638,7 @@ __device__ __forceinline__ void stream_grad(const T* row, T* out, int32_t begin,
     for (int64_t c = begin + (int64_t)threadIdx.x * P; c < end; c += kThreads * P) {
         const int n = (int)min((int64_t)P, end - c);
         float v[P];
-        unpack(load_some(row + c, n, -INFINITY), v, T());
+        unpack(load_some(row + c, n, -INFINITY, c), v, T());
 #pragma unroll
         for (int e = 0; e < P; ++e) v[e] = g.template of<kEntropy>(v[e]);
         own(v, (int32_t)c, n);

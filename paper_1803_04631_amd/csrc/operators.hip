@@ -70,29 +70,51 @@ int check_layer_norm(int64_t rows, int32_t cols, int32_t type, int32_t weight_ty
     return MLDA_OK;
 }
 
-// How many lanes share a row, and how many of its elements each holds.  Rows of up to 128 columns are taken four to a
-// wave; beyond 16,384 columns they do not stay in registers.
-template <class F>
-void with_team(int32_t cols, F&& f) {
-    if (cols <= 128) f(std::integral_constant<int, 16>(), std::integral_constant<int, 8>());
-    else if (cols <= 512) f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
-    else if (cols <= 1024) f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
-    else if (cols <= 2048) f(std::integral_constant<int, 256>(), std::integral_constant<int, 8>());
-    else if (cols <= 4096) f(std::integral_constant<int, 256>(), std::integral_constant<int, 16>());
-    else if (cols <= 8192) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
-    else f(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
-}
-constexpr int32_t kHeldCols = 16384;
+template <int kTeam, int kPieces>
+struct Team {
+    static constexpr int team = kTeam, pieces = kPieces;
+};
 
-int team_threads(int32_t cols) { return cols <= 4096 ? 256 : 1024; }
-int team_lanes(int32_t cols) { return cols <= 128 ? 16 : cols <= 1024 ? 64 : team_threads(cols); }
+// f(team) for the lanes that share a row and the 16-byte pieces that each holds.
+template <class F>
+void with_team(int64_t row_bytes, F&& f) {
+    if (row_bytes <= 64) f(Team<4, 1>());
+    else if (row_bytes <= 256) f(Team<16, 1>());
+    else if (row_bytes <= 1024) f(Team<64, 1>());
+    else if (row_bytes <= 2048) f(Team<64, 2>());
+    else if (row_bytes <= 4096) f(Team<64, 4>());
+    else if (row_bytes <= 8192) f(Team<256, 2>());
+    else if (row_bytes <= 16384) f(Team<256, 4>());
+    else if (row_bytes <= 32768) f(Team<1024, 2>());
+    else if (row_bytes <= 65536) f(Team<1024, 4>());
+    else f(Team<1024, 8>());
+}
+constexpr int64_t kHeldBytes = 131072;            // of a row that a team holds
+constexpr int64_t kSummedBytes = 32768;           // of one beside whose gradient there is room for the weight's
+
+// The same for the gradient, where a column takes four times the registers; f(team, workgroups that fit a CU).
+template <class F>
+void with_grad_team(int64_t row_bytes, F&& f) {
+    if (row_bytes <= 64) f(Team<4, 1>(), 5);
+    else if (row_bytes <= 256) f(Team<16, 1>(), 5);
+    else if (row_bytes <= 1024) f(Team<64, 1>(), 5);
+    else if (row_bytes <= 2048) f(Team<64, 2>(), 4);
+    else if (row_bytes <= 4096) f(Team<128, 2>(), 4);
+    else if (row_bytes <= 8192) f(Team<256, 2>(), 4);
+    else if (row_bytes <= 16384) f(Team<512, 2>(), 2);
+    else f(Team<1024, 2>(), 1);
+}
 
 // Workgroups of the gradient's kernel, each of which leaves sums over its rows.
-int32_t norm_grad_groups(int64_t rows, int32_t cols) {
-    if (cols > kHeldCols) return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + 63) / 64, 64));      // slabs
-    const int teams = team_threads(cols) / team_lanes(cols);
-    const int64_t per_cu = team_threads(cols) == 256 ? 4 : 2;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + teams - 1) / teams, per_cu * kCus));
+int32_t norm_grad_groups(int64_t rows, int32_t cols, int32_t type) {
+    const int64_t bytes = cols * (int64_t)type_bytes(type);
+    if (bytes > kSummedBytes) return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + 63) / 64, 64));      // slabs
+    int64_t groups = 1;
+    with_grad_team(bytes, [&](auto t, int per_cu) {
+        constexpr int kThreads = mlda::team_threads(t.team), kTeams = kThreads / t.team;
+        groups = std::min<int64_t>((rows + kTeams - 1) / kTeams, per_cu * kCus);
+    });
+    return (int32_t)std::max<int64_t>(1, groups);
 }
 
 // ---------------------------------------------------------------- log-probabilities
@@ -291,13 +313,15 @@ int mlda_layer_norm(const void* x, int64_t x_stride, const void* weight, const v
     return with_types(type, weight_type, [&](auto t, auto w) {
         typedef decltype(t) T;
         typedef decltype(w) W;
-        if (cols > kHeldCols) {
+        const int64_t bytes = cols * (int64_t)sizeof(T);
+        if (bytes > kHeldBytes) {
             hipLaunchKernelGGL((mlda::layer_norm_long_kernel<T, W>), dim3((unsigned)std::min(rows, kMostGroups)), dim3(1024), 0, stream, a);
         } else {
-            with_team(cols, [&](auto team, auto held) {
-                constexpr int kTeam = decltype(team)::value, kThreads = kTeam < 256 ? 256 : kTeam, kTeams = kThreads / kTeam;
+            with_team(bytes, [&](auto t) {
+                constexpr int kThreads = mlda::team_threads(t.team), kTeams = kThreads / t.team;
+                constexpr bool kHeld = t.pieces * t.team < 8192;
                 const int64_t groups = std::min<int64_t>((rows + kTeams - 1) / kTeams, kThreads == 256 ? 8 * kCus : 2 * kCus);
-                hipLaunchKernelGGL((mlda::layer_norm_kernel<T, W, kTeam, decltype(held)::value>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
+                hipLaunchKernelGGL((mlda::layer_norm_kernel<T, W, t.team, t.pieces, kHeld>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
             });
         }
         return launched("layer_norm_kernel");
@@ -307,7 +331,7 @@ int mlda_layer_norm(const void* x, int64_t x_stride, const void* weight, const v
 int mlda_layer_norm_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes) {
     if (!bytes) return refuse("bytes is null");
     RC_TRY(check_layer_norm(rows, cols, MLDA_FP32, MLDA_FP32));
-    *bytes = rows == 0 ? 0 : (size_t)norm_grad_groups(rows, cols) * 2 * (size_t)cols * 4;
+    *bytes = rows == 0 ? 0 : (size_t)std::max(norm_grad_groups(rows, cols, MLDA_FP32), norm_grad_groups(rows, cols, MLDA_BF16)) * 2 * (size_t)cols * 4;
     return MLDA_OK;
 }
 
@@ -320,7 +344,7 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
     if (!aligned(weight, type_bytes(weight_type)) || !aligned(grad_weight, type_bytes(weight_type)) || !aligned(grad_bias, type_bytes(weight_type)))
         return refuse("layer norm: weight or its gradient is not aligned to its type");
     mlda::LayerNormGradArgs a{grad_y, grad_y_stride, x, x_stride, mean, rstd, weight, grad_x, grad_x_stride, nullptr, rows, cols};
-    const int32_t groups = norm_grad_groups(rows, cols);
+    const int32_t groups = norm_grad_groups(rows, cols, type);
     if (rows > 0) {
         RC_TRY(check_rows(x, x_stride, rows, cols, type, "layer norm: x is null", "layer norm: rows of x overlap or are not aligned to their type"));
         RC_TRY(check_rows(grad_y, grad_y_stride, rows, cols, type, "layer norm: grad_y is null", "layer norm: rows of grad_y overlap or are not aligned to their type"));
@@ -342,7 +366,8 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
     return with_types(type, weight_type, [&](auto t, auto w) {
         typedef decltype(t) T;
         typedef decltype(w) W;
-        if (rows > 0 && cols > kHeldCols) {
+        const int64_t bytes = cols * (int64_t)sizeof(T);
+        if (rows > 0 && bytes > kSummedBytes) {
             // (the sums first: grad_x may be written over what they read)
             if (a.partial) {
                 const int32_t tile = mlda::kWave * mlda::kPack<T>;
@@ -350,17 +375,19 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
                                    dim3(256), 0, stream, a);
                 RC_TRY(launched("layer_norm_grad_columns_kernel"));
             }
-            if (grad_x)
-                hipLaunchKernelGGL((mlda::layer_norm_grad_long_kernel<T, W>), dim3((unsigned)std::min(rows, kMostGroups)), dim3(1024), 0, stream, a);
+            const dim3 grid((unsigned)std::min(rows, kMostGroups));
+            if (!grad_x) {}
+            else if (bytes <= 65536) hipLaunchKernelGGL((mlda::layer_norm_grad_kernel<T, W, 1024, 4, false>), grid, dim3(1024), 0, stream, a);
+            else hipLaunchKernelGGL((mlda::layer_norm_grad_long_kernel<T, W>), grid, dim3(1024), 0, stream, a);
         } else if (rows > 0) {
-            with_team(cols, [&](auto team, auto held) {
-                constexpr int kTeam = decltype(team)::value, kThreads = kTeam < 256 ? 256 : kTeam;
-                hipLaunchKernelGGL((mlda::layer_norm_grad_kernel<T, W, kTeam, decltype(held)::value>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
+            with_grad_team(bytes, [&](auto t, int) {
+                constexpr int kThreads = mlda::team_threads(t.team);
+                hipLaunchKernelGGL((mlda::layer_norm_grad_kernel<T, W, t.team, t.pieces, true>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
             });
         }
         RC_TRY(launched("layer_norm_grad_kernel"));
         if (!sums) return MLDA_OK;
-        hipLaunchKernelGGL((mlda::layer_norm_grad_final_kernel<W>), dim3((unsigned)((2 * (int64_t)cols + 63) / 64)), dim3(1024), 0, stream,
+        hipLaunchKernelGGL((mlda::layer_norm_grad_final_kernel<W>), dim3((unsigned)((2 * (int64_t)cols + 15) / 16)), dim3(1024), 0, stream,
                            a.partial, rows > 0 ? groups : 0, cols, static_cast<W*>(grad_weight), static_cast<W*>(grad_bias));
         return launched("layer_norm_grad_final_kernel");
     });

@@ -54,14 +54,56 @@ __device__ __forceinline__ Raw pack(const float (&in)[8], H) {
     return __builtin_bit_cast(Raw, h);
 }
 
-// `n` (0 .. kPack) elements from p on, `fill` behind them; never reads past the n-th.
-template <class T>
-__device__ __forceinline__ Raw load_some(const T* p, int n, float fill) {
-    if (n >= kPack<T>) return load_raw(p);
-    float v[kPack<T>];
+// What was made of these pieces before is not kept in registers for what is made of them next: unpacking again takes one
+// instruction an element, keeping it a register.
+template <int N>
+__device__ __forceinline__ void forget(Raw (&r)[N]) {
 #pragma unroll
-    for (int e = 0; e < kPack<T>; ++e) v[e] = e < n ? (float)p[e] : fill;
-    return pack(v, T());
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(r[i]));
+}
+
+// Moves a piece's elements `by` (0 .. kPack - 1) places down, and puts `fill` behind the first `n` of what results.
+template <class T>
+__device__ __forceinline__ Raw move_down(Raw r, int by, int n, T fill) {
+    if constexpr (sizeof(T) == 4) {
+        const uint32_t f = __builtin_bit_cast(uint32_t, fill);
+        if (by & 2) { r[0] = r[2]; r[1] = r[3]; }
+        if (by & 1) { r[0] = r[1]; r[1] = r[2]; r[2] = r[3]; }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = i < n ? r[i] : f;
+    } else {
+        const uint32_t f = __builtin_bit_cast(uint16_t, fill);
+        if (by & 4) { r[0] = r[2]; r[1] = r[3]; }
+        if (by & 2) { r[0] = r[1]; r[1] = r[2]; r[2] = r[3]; }
+        if (by & 1) {
+            r[0] = r[0] >> 16 | r[1] << 16;
+            r[1] = r[1] >> 16 | r[2] << 16;
+            r[2] = r[2] >> 16 | r[3] << 16;
+            r[3] = r[3] >> 16;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = 2 * i + 1 < n ? r[i] : 2 * i < n ? (r[i] & 0xffffu) | f << 16 : f << 16 | f;
+    }
+    return r;
+}
+
+// `n` (at most kPack) elements from p on, `fill` behind them; never reads past the n-th, nor more than `before` elements before
+// p.  The end of a row is the piece that ends there, moved down: one load, whatever is left.
+template <class T>
+__device__ __forceinline__ Raw load_some(const T* p, int n, float fill, int64_t before) {
+    constexpr int P = kPack<T>;
+    if (n >= P) return load_raw(p);
+    Raw r = {0, 0, 0, 0};
+    if (n <= 0) return move_down(r, 0, 0, (T)fill);
+    if (before >= P - n) return move_down(load_raw(p - (P - n)), P - n, n, (T)fill);
+#pragma unroll 1
+    for (int e = n; e-- > 0;) {                       // a row shorter than a piece
+        typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Bits;
+        const uint32_t bits = *reinterpret_cast<const Bits*>(p + e);
+        if constexpr (sizeof(T) == 4) r = Raw{bits, r[0], r[1], r[2]};
+        else r = Raw{r[0] << 16 | bits, r[1] << 16 | r[0] >> 16, r[2] << 16 | r[1] >> 16, r[3] << 16 | r[2] >> 16};
+    }
+    return move_down(r, 0, n, (T)fill);
 }
 
 template <class T>
@@ -105,22 +147,53 @@ __device__ __forceinline__ float wave_max(float v) {
     return fmaxf(a, b);
 }
 
-// Sum over a team of kTeam lanes (16, 64, or a whole workgroup of more), which every lane of the team gets.  `slots`: LDS of
-// kTeam / 64 floats that no earlier sum uses whose readers may still be reading: two taken in turn do, as each sum has one
-// barrier.  The order of the additions is fixed.
+// Sum over a team of kTeam lanes (4, 16, or whole waves: then all of the workgroup's teams take part at once), which every lane of the
+// team gets.  `slots`: LDS of a float for each of the workgroup's waves that no earlier sum uses whose readers may still be
+// reading: two taken in turn do, as each sum has one barrier.  The order of the additions is fixed.
+template <int kTeam>
+__device__ __forceinline__ float lanes_sum(float v) {
+    if constexpr (kTeam == 4) {
+        v += dpp_all<0xb1>(v);       // quad_perm: 1 0 3 2, then 2 3 0 1
+        return v + dpp_all<0x4e>(v);
+    }
+    return kTeam == 16 ? row16_sum(v) : wave_sum(v);
+}
+
 template <int kTeam>
 __device__ __forceinline__ float team_sum(float v, float* slots) {
-    if constexpr (kTeam == 16) return row16_sum(v);
-    v = wave_sum(v);
+    v = lanes_sum<kTeam>(v);
     if constexpr (kTeam > kWave) {
         constexpr int kWaves = kTeam / kWave;
-        if (lane_id() == 0) slots[threadIdx.x / kWave] = v;
+        slots += (int)threadIdx.x / kTeam * kWaves;
+        if (lane_id() == 0) slots[(int)threadIdx.x % kTeam / kWave] = v;
         __syncthreads();
         v = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) v += slots[w];
     }
     return v;
+}
+
+// Two sums with one barrier; slots of twice the size.
+template <int kTeam>
+__device__ __forceinline__ void team_sums(float& a, float& b, float* slots) {
+    a = lanes_sum<kTeam>(a);
+    b = lanes_sum<kTeam>(b);
+    if constexpr (kTeam > kWave) {
+        constexpr int kWaves = kTeam / kWave;
+        slots += (int)threadIdx.x / kTeam * 2 * kWaves;
+        if (lane_id() == 0) {
+            slots[(int)threadIdx.x % kTeam / kWave] = a;
+            slots[kWaves + (int)threadIdx.x % kTeam / kWave] = b;
+        }
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            a += slots[w];
+            b += slots[kWaves + w];
+        }
+    }
 }
 
 }  // namespace mlda
