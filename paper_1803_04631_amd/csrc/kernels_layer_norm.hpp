@@ -219,8 +219,8 @@ __device__ __forceinline__ void grad_piece(Raw x, Raw g, const Columns<W, kPack<
     }
 }
 
-// kSums: the weight's and bias' gradients are summed here (kHeld too: the weight is kept, the next row's pieces are loaded ahead).
-template <class T, class W, int kTeam, int kPieces, bool kSums>
+// kSums: the weight's and bias' gradients are summed here.  kHeld: the weight is kept, and the next row's pieces are loaded ahead.
+template <class T, class W, int kTeam, int kPieces, bool kSums, bool kHeld = kSums>
 __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(LayerNormGradArgs a) {
     constexpr int P = kPack<T>, kThreads = team_threads(kTeam), kTeams = kThreads / kTeam;
     __shared__ float slots[2][2 * (kThreads / kWave)];
@@ -229,11 +229,13 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(La
     const int lane = (int)threadIdx.x % kTeam;
     const int32_t cols = a.cols;
     const float n_cols = (float)cols;
-    Columns<W, P> w[kSums ? kPieces : 1];
+    Columns<W, P> w[kHeld ? kPieces : 1];
     float dw[kSums ? kPieces * P : 1], db[kSums ? kPieces * P : 1];
-    if constexpr (kSums) {
+    if constexpr (kHeld) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) w[j].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
+    }
+    if constexpr (kSums) {
 #pragma unroll
         for (int k = 0; k < kPieces * P; ++k) dw[k] = db[k] = 0.0f;
     }
@@ -257,9 +259,9 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(La
         to_mean = there ? a.mean[r] : 0.0f;
         to_rstd = there ? a.rstd[r] : 0.0f;
     };
-    if (kSums) load_row(row, next_x, next_g, next_mean, next_rstd);
+    if (kHeld) load_row(row, next_x, next_g, next_mean, next_rstd);
     for (int64_t i = 0; i < rounds; ++i, row += step) {
-        if constexpr (kSums) {
+        if constexpr (kHeld) {
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
                 x[j] = next_x[j];
@@ -275,9 +277,9 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(La
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             float u[P], h[P], grad[P];
-            if constexpr (!kSums) w[0].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
-            forget(w[kSums ? j : 0].raw);
-            grad_piece<T, W>(x[j], g[j], w[kSums ? j : 0], mean, rstd, u, h, grad);
+            if constexpr (!kHeld) w[0].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
+            forget(w[kHeld ? j : 0].raw);
+            grad_piece<T, W>(x[j], g[j], w[kHeld ? j : 0], mean, rstd, u, h, grad);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
                 sum_h += h[e];
@@ -293,9 +295,9 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(La
         for (int j = 0; j < kPieces; ++j) {
             const int32_t c = (j * kTeam + lane) * P;
             float u[P], h[P], v[P];
-            if constexpr (!kSums) w[0].load(a.weight, c, cols, 1.0f);
-            forget(w[kSums ? j : 0].raw);
-            grad_piece<T, W>(x[j], g[j], w[kSums ? j : 0], mean, rstd, u, h, v);
+            if constexpr (!kHeld) w[0].load(a.weight, c, cols, 1.0f);
+            forget(w[kHeld ? j : 0].raw);
+            grad_piece<T, W>(x[j], g[j], w[kHeld ? j : 0], mean, rstd, u, h, v);
             if constexpr (kSums) {                 // (not beside the sums above: what that needs would be kept until here)
 #pragma unroll
                 for (int e = 0; e < P; ++e) {

@@ -90,7 +90,8 @@ void with_team(int64_t row_bytes, F&& f) {
     else f(Team<1024, 8>());
 }
 constexpr int64_t kHeldBytes = 131072;            // of a row that a team holds
-constexpr int64_t kSummedBytes = 32768;           // of one beside whose gradient there is room for the weight's
+// of one beside whose gradient there is room for the weight's (two sums a column; 8,009 x 10,000 fp32 with the sums on their own 333 us, so 215)
+constexpr int64_t summed_bytes(int64_t type_bytes) { return type_bytes == 4 ? 65536 : 32768; }
 
 // The same for the gradient, where a column takes four times the registers; f(team, workgroups that fit a CU).
 template <class F>
@@ -102,13 +103,14 @@ void with_grad_team(int64_t row_bytes, F&& f) {
     else if (row_bytes <= 4096) f(Team<128, 2>(), 4);
     else if (row_bytes <= 8192) f(Team<256, 2>(), 4);
     else if (row_bytes <= 16384) f(Team<512, 2>(), 2);
-    else f(Team<1024, 2>(), 1);
+    else if (row_bytes <= 32768) f(Team<1024, 2>(), 1);
+    else f(Team<1024, 4>(), 1);
 }
 
 // Workgroups of the gradient's kernel, each of which leaves sums over its rows.
 int32_t norm_grad_groups(int64_t rows, int32_t cols, int32_t type) {
     const int64_t bytes = cols * (int64_t)type_bytes(type);
-    if (bytes > kSummedBytes) return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + 63) / 64, 64));      // slabs
+    if (bytes > summed_bytes((int64_t)type_bytes(type))) return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + 63) / 64, 64));      // slabs
     int64_t groups = 1;
     with_grad_team(bytes, [&](auto t, int per_cu) {
         constexpr int kThreads = mlda::team_threads(t.team), kTeams = kThreads / t.team;
@@ -367,7 +369,7 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
         typedef decltype(t) T;
         typedef decltype(w) W;
         const int64_t bytes = cols * (int64_t)sizeof(T);
-        if (rows > 0 && bytes > kSummedBytes) {
+        if (rows > 0 && bytes > summed_bytes(sizeof(T))) {
             // (the sums first: grad_x may be written over what they read)
             if (a.partial) {
                 const int32_t tile = mlda::kWave * mlda::kPack<T>;
@@ -382,7 +384,8 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
         } else if (rows > 0) {
             with_grad_team(bytes, [&](auto t, int) {
                 constexpr int kThreads = mlda::team_threads(t.team);
-                hipLaunchKernelGGL((mlda::layer_norm_grad_kernel<T, W, t.team, t.pieces, true>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
+                if constexpr (sizeof(T) == 4 || t.pieces < 4)
+                    hipLaunchKernelGGL((mlda::layer_norm_grad_kernel<T, W, t.team, t.pieces, true, (t.pieces < 4)>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
             });
         }
         RC_TRY(launched("layer_norm_grad_kernel"));

@@ -17,6 +17,9 @@ template <class T> constexpr int kPack = 16 / (int)sizeof(T);                   
 // Rows start wherever their stride puts them: 16 bytes are read and written at the alignment of an element.
 template <class T> __device__ __forceinline__ Raw load_raw(const T* p) { return *reinterpret_cast<const RawAnywhere*>(p); }
 template <class T> __device__ __forceinline__ void store_raw(T* p, Raw r) { *reinterpret_cast<RawAnywhere*>(p) = r; }
+// The same for what is not read again soon: it does not take the place in the caches of what is.
+template <class T> __device__ __forceinline__ Raw load_raw_once(const T* p) { return __builtin_nontemporal_load(reinterpret_cast<const RawAnywhere*>(p)); }
+template <class T> __device__ __forceinline__ void store_raw_once(T* p, Raw r) { __builtin_nontemporal_store(r, reinterpret_cast<RawAnywhere*>(p)); }
 
 __device__ __forceinline__ void unpack(Raw r, float (&out)[4], float) {
 #pragma unroll
