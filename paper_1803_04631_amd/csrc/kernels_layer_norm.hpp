@@ -24,6 +24,7 @@ struct LayerNormArgs {
     int64_t rows;
     int32_t cols;
     float eps;
+    bool once;                   // x and y are more than the caches hold
 };
 
 struct LayerNormGradArgs {
@@ -39,6 +40,7 @@ struct LayerNormGradArgs {
     float* partial;              // [workgroups][2][cols], null: the sums over rows are not wanted
     int64_t rows;
     int32_t cols;
+    bool once;                   // x, grad and grad_x are more than the caches hold
 };
 
 // P columns of a vector of type W, as they are loaded: P elements of another type make up 16 bytes.
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNo
                 b[kHeld ? j : 0].get(vb);
 #pragma unroll
                 for (int e = 0; e < P; ++e) v[e] = __builtin_fmaf((v[e] - mean) * rstd, vw[e], vb[e]);
-                store_some(y + c, pack(v, T()), min(max(cols - c, 0), P));
+                store_piece(y, c, 0, cols, pack(v, T()), a.once);
             }
             if (lane == 0) {
                 if (a.mean) a.mean[row] = mean;
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a) 
             b.get(vb);
 #pragma unroll
             for (int e = 0; e < P; ++e) v[e] = __builtin_fmaf((v[e] - mean) * rstd, vw[e], vb[e]);
-            store_some(y + c, pack(v, T()), n);
+            store_piece(y, c, 0, cols, pack(v, T()), a.once);
         }
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -307,7 +309,7 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(La
             }
 #pragma unroll
             for (int e = 0; e < P; ++e) v[e] = rstd * ((h[e] - mean_h) - u[e] * mean_hu);
-            if (dx) store_some(dx + c, pack(v, T()), min(max(cols - c, 0), P));
+            if (dx) store_piece(dx, c, 0, cols, pack(v, T()), a.once);
         }
     }
     if constexpr (kSums) {
@@ -386,7 +388,7 @@ __global__ __launch_bounds__(1024) void layer_norm_grad_long_kernel(LayerNormGra
             const int n = piece(c, u, h);
 #pragma unroll
             for (int e = 0; e < P; ++e) v[e] = rstd * ((h[e] - mean_h) - u[e] * mean_hu);
-            store_some(dx + c, pack(v, T()), n);
+            store_piece(dx, c, 0, cols, pack(v, T()), a.once);
         }
     }
 }

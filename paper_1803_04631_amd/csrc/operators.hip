@@ -34,6 +34,10 @@ bool known_type(int32_t t) { return t == MLDA_FP32 || t == MLDA_BF16 || t == MLD
 size_t type_bytes(int32_t t) { return t == MLDA_FP32 ? 4 : 2; }
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+// Whether a call that reads and writes so many bytes leaves them out of the caches (256 MB on the way to memory): what is written then
+// does not push out what is still to be read.  Below, the next call finds the results there.
+bool passes_caches(double bytes) { return bytes > 192e6; }
+
 // f(tag) for the type; the type is known.
 template <class F>
 int with_type(int32_t type, F&& f) {
@@ -221,6 +225,7 @@ template <bool kLoss>
 int run_grad(mlda::LogprobGradArgs a, int32_t type, hipStream_t stream) {
     const bool single = !a.row_ptr;
     a.slots = a.columns = 0;
+    a.once = passes_caches(2.0 * a.rows * a.vocab * type_bytes(type));
     if (!single) a.slots = table_slots(a.rows, a.n_tokens, a.segment_cols, &a.columns);
     const unsigned lds = (unsigned)std::max(a.slots * mlda::kSlotBytes, a.columns * 8);
     const dim3 grid((unsigned)std::min(a.rows * a.segments, kMostGroups));
@@ -310,7 +315,8 @@ int mlda_layer_norm(const void* x, int64_t x_stride, const void* weight, const v
     if (x == y && x_stride != y_stride && rows > 1) return refuse("layer norm: y in the place of x has its stride");
     if (!aligned(weight, type_bytes(weight_type)) || !aligned(bias, type_bytes(weight_type)) || !aligned(mean, 4) || !aligned(rstd, 4))
         return refuse("layer norm: weight, bias, mean or rstd is not aligned to its type");
-    const mlda::LayerNormArgs a{x, x_stride, weight, bias, y, y_stride, mean, rstd, rows, cols, (float)eps};
+    const mlda::LayerNormArgs a{x, x_stride, weight, bias, y, y_stride, mean, rstd, rows, cols, (float)eps,
+                                passes_caches(2.0 * rows * cols * type_bytes(type))};
     const hipStream_t stream = (hipStream_t)hip_stream;
     return with_types(type, weight_type, [&](auto t, auto w) {
         typedef decltype(t) T;
@@ -345,7 +351,8 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
     const bool sums = grad_weight || grad_bias;
     if (!aligned(weight, type_bytes(weight_type)) || !aligned(grad_weight, type_bytes(weight_type)) || !aligned(grad_bias, type_bytes(weight_type)))
         return refuse("layer norm: weight or its gradient is not aligned to its type");
-    mlda::LayerNormGradArgs a{grad_y, grad_y_stride, x, x_stride, mean, rstd, weight, grad_x, grad_x_stride, nullptr, rows, cols};
+    mlda::LayerNormGradArgs a{grad_y, grad_y_stride, x, x_stride, mean, rstd, weight, grad_x, grad_x_stride, nullptr, rows, cols,
+                              passes_caches(3.0 * rows * cols * type_bytes(type))};
     const int32_t groups = norm_grad_groups(rows, cols, type);
     if (rows > 0) {
         RC_TRY(check_rows(x, x_stride, rows, cols, type, "layer norm: x is null", "layer norm: rows of x overlap or are not aligned to their type"));
@@ -436,7 +443,7 @@ int mlda_token_logprobs_backward(const void* logits, int64_t stride, int64_t row
     if (!stats || (n_tokens > 0 && !grad_logprobs)) return refuse("log-probabilities: stats or grad_logprobs are null");
     if (grad_entropy && !entropy) return refuse("log-probabilities: a gradient of the entropy needs the entropy");
     mlda::LogprobGradArgs a{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, grad_logprobs, const_cast<float*>(stats), entropy,
-                            grad_entropy, nullptr, grad_logits, grad_stride, 1, vocab, 0, 0};
+                            grad_entropy, nullptr, grad_logits, grad_stride, 1, vocab, 0, 0, false};
     segments_of(rows, vocab, 1024 * (int32_t)(16 / type_bytes(type)), &a.segments, &a.segment_cols);
     return run_grad<false>(a, type, (hipStream_t)hip_stream);
 }
@@ -463,7 +470,7 @@ int mlda_token_logprobs_grad(const void* logits, int64_t stride, int64_t rows, i
                                             nullptr, grad_logits, grad_stride, hip_stream);
     }
     const mlda::LogprobGradArgs a{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, weights, nullptr, nullptr, nullptr, logprobs,
-                                  grad_logits, grad_stride, 1, vocab, 0, 0};
+                                  grad_logits, grad_stride, 1, vocab, 0, 0, false};
     return run_grad<true>(a, type, stream);
 }
 

@@ -90,6 +90,96 @@ __device__ __forceinline__ Raw move_down(Raw r, int by, int n, T fill) {
     return r;
 }
 
+// Moves a piece's elements `by` (0 .. kPack - 1) places up.
+template <class T>
+__device__ __forceinline__ Raw move_up(Raw r, int by) {
+    if constexpr (sizeof(T) == 4) {
+        if (by & 2) { r[3] = r[1]; r[2] = r[0]; }
+        if (by & 1) { r[3] = r[2]; r[2] = r[1]; r[1] = r[0]; }
+    } else {
+        if (by & 4) { r[3] = r[1]; r[2] = r[0]; }
+        if (by & 2) { r[3] = r[2]; r[2] = r[1]; r[1] = r[0]; }
+        if (by & 1) {
+            r[3] = r[3] << 16 | r[2] >> 16;
+            r[2] = r[2] << 16 | r[1] >> 16;
+            r[1] = r[1] << 16 | r[0] >> 16;
+            r[0] = r[0] << 16;
+        }
+    }
+    return r;
+}
+
+// The elements [from, to) of a piece, `fill` in the others' places.
+template <class T>
+__device__ __forceinline__ Raw keep(Raw r, int from, int to, T fill) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            r[i] = i >= from && i < to ? r[i] : __builtin_bit_cast(uint32_t, fill);
+        } else {
+            const uint32_t f = __builtin_bit_cast(uint16_t, fill);
+            const uint32_t mask = (2 * i >= from && 2 * i < to ? 0xffffu : 0u) | (2 * i + 1 >= from && 2 * i + 1 < to ? 0xffff0000u : 0u);
+            r[i] = (r[i] & mask) | ((f << 16 | f) & ~mask);
+        }
+    }
+    return r;
+}
+
+// The piece of columns [c, c + kPack) of which [lo, hi) are there, `fill` in the others' places; reads nothing outside [lo, hi).
+template <class T>
+__device__ __forceinline__ Raw load_piece(const T* base, int64_t c, int64_t lo, int64_t hi, float fill, bool once) {
+    constexpr int P = kPack<T>;
+    if (c >= lo && c + P <= hi) {
+        Raw r;
+        if (once) {
+            asm volatile("" ::: "memory");              // (or both loads become one, the second)
+            r = load_raw_once(base + c);
+            asm volatile("" ::: "memory");
+        } else {
+            r = load_raw(base + c);
+        }
+        return r;
+    }
+    const int from = (int)max((int64_t)0, min((int64_t)P, lo - c)), to = (int)max((int64_t)0, min((int64_t)P, hi - c));
+    Raw r = {0, 0, 0, 0};
+    if (from >= to) return keep(r, 0, 0, (T)fill);
+    if (hi - lo >= P) {
+        const int64_t at = max(lo, min(c, hi - P));     // a whole piece nearby
+        r = load_raw(base + at);
+        r = at > c ? move_up<T>(r, (int)(at - c)) : move_down(r, (int)(c - at), P, (T)fill);
+    } else {
+        typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Bits;
+#pragma unroll 1
+        for (int e = to; e-- > 0;) {                    // a row shorter than a piece
+            const uint32_t bits = e >= from ? *reinterpret_cast<const Bits*>(base + c + e) : 0;
+            if constexpr (sizeof(T) == 4) r = Raw{bits, r[0], r[1], r[2]};
+            else r = Raw{r[0] << 16 | bits, r[1] << 16 | r[0] >> 16, r[2] << 16 | r[1] >> 16, r[3] << 16 | r[2] >> 16};
+        }
+    }
+    return keep(r, from, to, (T)fill);
+}
+
+template <class T>
+__device__ __forceinline__ void store_piece(T* base, int64_t c, int64_t lo, int64_t hi, Raw r, bool once) {
+    constexpr int P = kPack<T>;
+    if (c >= lo && c + P <= hi) {
+        if (once) {
+            asm volatile("" ::: "memory");              // (or both stores become one, the second)
+            store_raw_once(base + c, r);
+            asm volatile("" ::: "memory");
+        } else {
+            store_raw(base + c, r);
+        }
+        return;
+    }
+    typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Bits;
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        const uint32_t bits = sizeof(T) == 4 ? r[e % 4] : r[e / 2] >> (e % 2 * 16);
+        if (c + e >= lo && c + e < hi) *reinterpret_cast<Bits*>(base + c + e) = (Bits)bits;
+    }
+}
+
 // `n` (at most kPack) elements from p on, `fill` behind them; never reads past the n-th, nor more than `before` elements before
 // p.  The end of a row is the piece that ends there, moved down: one load, whatever is left.
 template <class T>
