@@ -223,7 +223,7 @@ __device__ __forceinline__ void grad_piece(Raw x, Raw g, const Columns<W, kPack<
 
 // kSums: the weight's and bias' gradients are summed here.  kHeld: the weight is kept, and the next row's pieces are loaded ahead.
 template <class T, class W, int kTeam, int kPieces, bool kSums, bool kHeld = kSums>
-__global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_grad_kernel(LayerNormGradArgs a) {
+__global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ? 4 : 1) void layer_norm_grad_kernel(LayerNormGradArgs a) {
     constexpr int P = kPack<T>, kThreads = team_threads(kTeam), kTeams = kThreads / kTeam;
     __shared__ float slots[2][2 * (kThreads / kWave)];
     // sums over the workgroup's teams: [dw or db][column]
