@@ -37,7 +37,9 @@ struct LayerNormGradArgs {
     const void* weight;          // null: ones
     void* grad_x;                // null: not wanted
     int64_t grad_x_stride;
-    float* partial;              // [workgroups][2][cols], null: the sums over rows are not wanted
+    float* partial;              // [workgroups][2][cols]; null: the sums over rows are not wanted, or the one workgroup's are the whole
+    void* grad_weight;           // then: null: not wanted
+    void* grad_bias;
     int64_t rows;
     int32_t cols;
     bool once;                   // x, grad and grad_x are more than the caches hold
@@ -313,13 +315,31 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
         }
     }
     if constexpr (kSums) {
-        if (!a.partial) return;
-        float* out = a.partial + (int64_t)blockIdx.x * 2 * cols;
+        if (!a.partial && !a.grad_weight && !a.grad_bias) return;
+        // a sum of this thread's: to the workgroup's, or, where there is only one, to where it is wanted
+        auto put = [&](int c, float w_sum, float b_sum) {
+            if (c >= cols) return;
+            if (a.partial) {
+                float* out = a.partial + (int64_t)blockIdx.x * 2 * cols;
+                out[c] = w_sum;
+                out[cols + c] = b_sum;
+            } else {
+                if (a.grad_weight) static_cast<W*>(a.grad_weight)[c] = (W)w_sum;
+                if (a.grad_bias) static_cast<W*>(a.grad_bias)[c] = (W)b_sum;
+            }
+        };
         if constexpr (kTeams > 1) {
-            // one team after the other, so that the order of the additions is fixed
-            constexpr int kCols = kTeam * kPieces * P;
-            for (int t = 0; t < kTeams; ++t) {
-                if ((int)threadIdx.x / kTeam == t) {
+            // the teams of a wave by its lanes, then one wave or team after the other: the order of the additions is fixed
+            constexpr int kCols = kTeam * kPieces * P, kLanes = kTeam < kWave ? kWave : kTeam;
+#pragma unroll
+            for (int k = 0; k < kPieces * P; ++k)
+#pragma unroll
+                for (int off = kTeam; off < kWave; off *= 2) {
+                    dw[k] += __shfl_xor(dw[k], off, kWave);
+                    db[k] += __shfl_xor(db[k], off, kWave);
+                }
+            for (int t = 0; t < kThreads / kLanes; ++t) {
+                if ((int)threadIdx.x / kLanes == t && (int)threadIdx.x % kLanes < kTeam) {
 #pragma unroll
                     for (int j = 0; j < kPieces; ++j)
 #pragma unroll
@@ -331,21 +351,12 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
                 }
                 __syncthreads();
             }
-            for (int c = (int)threadIdx.x; c < cols; c += kThreads) {
-                out[c] = joined[c];
-                out[cols + c] = joined[kCols + c];
-            }
+            for (int c = (int)threadIdx.x; c < min(cols, kCols); c += kThreads) put(c, joined[c], joined[kCols + c]);
         } else {
 #pragma unroll
             for (int j = 0; j < kPieces; ++j)
 #pragma unroll
-                for (int e = 0; e < P; ++e) {
-                    const int c = (j * kTeam + lane) * P + e, k = j * P + e;
-                    if (c < cols) {
-                        out[c] = dw[k];
-                        out[cols + c] = db[k];
-                    }
-                }
+                for (int e = 0; e < P; ++e) put((j * kTeam + lane) * P + e, dw[j * P + e], db[j * P + e]);
         }
     }
 }

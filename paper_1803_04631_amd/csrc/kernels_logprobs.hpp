@@ -285,13 +285,16 @@ __device__ __forceinline__ LaneSums walk_row(const Span<T>& span, int wave, int 
     return sums;
 }
 
-// The log-probability of a word: NaN for one outside the vocabulary, 0 for none.
-template <class T>
-__device__ __forceinline__ float word_logprob(const T* row, int32_t word, int32_t vocab, float m, float log_s) {
+// The log-probability of a word of that logit: NaN for one outside the vocabulary, 0 for none.
+__device__ __forceinline__ float logprob_of(float logit, int32_t word, int32_t vocab, float m, float log_s) {
     if (word < 0) return 0.0f;
     if (word >= vocab) return __uint_as_float(0x7fc00000u);
     if (m == -INFINITY) return -INFINITY;
-    return ((float)row[word] - m) - log_s;
+    return (logit - m) - log_s;
+}
+template <class T>
+__device__ __forceinline__ float word_logprob(const T* row, int32_t word, int32_t vocab, float m, float log_s) {
+    return logprob_of(word >= 0 && word < vocab ? (float)row[word] : 0.0f, word, vocab, m, log_s);
 }
 
 // The words of a row: [begin, end) of the tokens, whatever the bounds say.
@@ -354,12 +357,13 @@ struct RowStats {
     }
 };
 
+// What a row comes to is written, with its words from the `done`-th on.
 template <class T, int kThreads>
-__device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, const RowStats& st, const uint64_t* top) {
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, const RowStats& st, const uint64_t* top, int done = 0) {
     if (!a.words_apart) {
         int64_t begin, end;
         row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
-        word_logprobs<T, kThreads>(static_cast<const T*>(a.logits) + row * a.stride, a.tokens, begin, end, (int)threadIdx.x, a.vocab, st.m, st.log_s,
+        word_logprobs<T, kThreads>(static_cast<const T*>(a.logits) + row * a.stride, a.tokens, min(begin + done, end), end, (int)threadIdx.x, a.vocab, st.m, st.log_s,
                                    a.logprobs);
     }
     if (threadIdx.x == 0) {
@@ -531,7 +535,7 @@ __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) 
             finish_row<T, kWaves * kWave>(a, row, RowStats(m, s, u), best);
         } else {
             if (threadIdx.x == 0) a.parts[item] = RowPart{s, u, m, count};
-            if (kExtras && wave == 0 && lane < count) a.part_top[item * a.top + lane] = best[lane];
+            if (kExtras && wave == 0 && lane < a.top) a.part_top[item * a.top + lane] = lane < count ? best[lane] : 0;
         }
         __syncthreads();                           // (the next row's parts and candidates)
     }
@@ -542,38 +546,74 @@ template <class T>
 __global__ __launch_bounds__(kLogprobWaves * kWave) void logprob_join_kernel(LogprobArgs a) {
     __shared__ uint64_t held[kLogprobWaves][kHeld];
     __shared__ uint64_t best[kHeld];
-    __shared__ int counts[kLogprobWaves];
+    __shared__ uint32_t most[kLogprobWaves * kWave];
+    __shared__ int found, counts[kLogprobWaves];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const RowPart* parts = a.parts + row * a.segments;
+        // the first words' logits are on their way meanwhile
+        const T* logits = static_cast<const T*>(a.logits) + row * a.stride;
+        int64_t begin = 0, end = 0;
+        if (!a.words_apart) row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
+        const int64_t t = begin + threadIdx.x;
+        const int32_t word = t < end ? a.tokens[t] : -1;
+        const float logit = word >= 0 && word < a.vocab ? (float)logits[word] : 0.0f;
         // every wave the sums of all segments, of which there are at most as many as lanes
         float m = lane < a.segments ? parts[lane].m : kLowest;
         double s = lane < a.segments ? parts[lane].s : 0.0, u = lane < a.segments ? parts[lane].u : 0.0;
         join_lanes(m, s, u);
         if (a.top) {
-            // a wave's share of the segments' lists; full buffers are cut down to the wanted number
-            int count = 0;
-            for (int i = wave; i < a.segments; i += kLogprobWaves) {
-                const int n = min(__builtin_amdgcn_readfirstlane(parts[i].n), a.top);
-                if (count + n > kHeld) count = keep_greatest(held[wave], count, a.top);
-                if (lane < n) held[wave][count + lane] = a.part_top[(row * a.segments + i) * a.top + lane];
-                count += n;
+            // the segments' lists, a few entries a thread; as in find_top a bound that enough of them reach leaves few to put in order
+            constexpr int kThreads = kLogprobWaves * kWave, kMine = kWave * kMaxAlternatives / kThreads;
+            const uint64_t* lists = a.part_top + row * a.segments * a.top;
+            uint64_t mine[kMine], greatest = 0;
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int i = k * kThreads + (int)threadIdx.x;
+                mine[k] = i < a.segments * a.top ? lists[i] : 0;
+                greatest = max(greatest, mine[k]);
             }
-            count = keep_greatest(held[wave], count, a.top);
-            if (lane == 0) counts[wave] = count;
+            most[threadIdx.x] = (uint32_t)(greatest >> 32);
+            if (threadIdx.x == 0) found = 0;
             __syncthreads();
-            if (wave == 0) {
+            uint32_t group = most[lane];
+#pragma unroll
+            for (int w = 1; w < kLogprobWaves; ++w) group = max(group, most[w * kWave + lane]);
+            const uint32_t bound = max(nth_key(group, a.top), 1u);
+#pragma unroll
+            for (int k = 0; k < kMine; ++k)
+                if ((uint32_t)(mine[k] >> 32) >= bound) {
+                    const int at = atomicAdd(&found, 1);
+                    if (at < kHeld) best[at] = mine[k];
+                }
+            __syncthreads();
+            int count = found;
+            if (count > kHeld) {
+                // many equal ones: a wave's share of the lists; full buffers are cut down to the wanted number
                 count = 0;
-                for (int w = 0; w < kLogprobWaves; ++w) {
-                    const int n = counts[w];
-                    if (lane < n) best[count + lane] = held[w][lane];
+                for (int i = wave; i < a.segments; i += kLogprobWaves) {
+                    const int n = min(__builtin_amdgcn_readfirstlane(parts[i].n), a.top);
+                    if (count + n > kHeld) count = keep_greatest(held[wave], count, a.top);
+                    if (lane < n) held[wave][count + lane] = lists[i * a.top + lane];
                     count += n;
                 }
-                keep_greatest(best, count, a.top);
+                count = keep_greatest(held[wave], count, a.top);
+                if (lane == 0) counts[wave] = count;
+                __syncthreads();
+                count = 0;
+                if (wave == 0)
+                    for (int w = 0; w < kLogprobWaves; ++w) {
+                        const int n = counts[w];
+                        if (lane < n) best[count + lane] = held[w][lane];
+                        count += n;
+                    }
             }
+            if (wave == 0) keep_greatest(best, count, a.top);
             __syncthreads();
         }
-        finish_row<T, kLogprobWaves * kWave>(a, row, RowStats(m, s, u), best);
+        const RowStats st(m, s, u);
+        if (t < end) a.logprobs[t] = logprob_of(logit, word, a.vocab, st.m, st.log_s);
+        finish_row<T, kLogprobWaves * kWave>(a, row, st, best, kLogprobWaves * kWave);
         __syncthreads();
     }
 }

@@ -351,7 +351,7 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
     const bool sums = grad_weight || grad_bias;
     if (!aligned(weight, type_bytes(weight_type)) || !aligned(grad_weight, type_bytes(weight_type)) || !aligned(grad_bias, type_bytes(weight_type)))
         return refuse("layer norm: weight or its gradient is not aligned to its type");
-    mlda::LayerNormGradArgs a{grad_y, grad_y_stride, x, x_stride, mean, rstd, weight, grad_x, grad_x_stride, nullptr, rows, cols,
+    mlda::LayerNormGradArgs a{grad_y, grad_y_stride, x, x_stride, mean, rstd, weight, grad_x, grad_x_stride, nullptr, nullptr, nullptr, rows, cols,
                               passes_caches(3.0 * rows * cols * type_bytes(type))};
     const int32_t groups = norm_grad_groups(rows, cols, type);
     if (rows > 0) {
@@ -367,7 +367,12 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
             if (!dev_workspace || !aligned(dev_workspace, 4)) return refuse("layer norm: the workspace is null or not aligned");
             if (workspace_bytes < (size_t)groups * 2 * (size_t)cols * 4)
                 return set_error(MLDA_ENOMEM, "layer norm: the workspace is smaller than mlda_layer_norm_workspace_bytes");
-            a.partial = static_cast<float*>(dev_workspace);
+            if (groups > 1 || cols * (int64_t)type_bytes(type) > summed_bytes((int64_t)type_bytes(type))) {
+                a.partial = static_cast<float*>(dev_workspace);
+            } else {
+                a.grad_weight = grad_weight;
+                a.grad_bias = grad_bias;
+            }
         }
     }
     if (!sums && (!grad_x || rows == 0)) return MLDA_OK;
@@ -396,7 +401,7 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
             });
         }
         RC_TRY(launched("layer_norm_grad_kernel"));
-        if (!sums) return MLDA_OK;
+        if (!sums || (rows > 0 && !a.partial)) return MLDA_OK;
         hipLaunchKernelGGL((mlda::layer_norm_grad_final_kernel<W>), dim3((unsigned)((2 * (int64_t)cols + 15) / 16)), dim3(1024), 0, stream,
                            a.partial, rows > 0 ? groups : 0, cols, static_cast<W*>(grad_weight), static_cast<W*>(grad_bias));
         return launched("layer_norm_grad_final_kernel");
