@@ -653,14 +653,23 @@ struct WordTable {
     __device__ __forceinline__ WordTable(unsigned long long* lds, int32_t n)
         : sums(lds), words(reinterpret_cast<int32_t*>(lds + n)), slots(n), shift(__clz(n) + 1) {}
 
-    __device__ __forceinline__ void add(int32_t word, long long units) const {
-        int i = (int)(((uint32_t)word * 0x9E3779B1u) >> shift);
+    template <int kThreads>
+    __device__ __forceinline__ void clear(int tid) const {
+        for (int i = tid; i < slots; i += kThreads) {
+            sums[i] = 0;
+            words[i] = -1;
+        }
+    }
+    // The slot, if the word is new to the table, else -1.
+    __device__ __forceinline__ int add(int32_t word, long long units) const {
+        int i = (int)(((uint32_t)word * 0x9E3779B1u) >> shift), was;
         for (;;) {
-            const int was = atomicCAS(&words[i], -1, word);
+            was = atomicCAS(&words[i], -1, word);
             if (was == -1 || was == word) break;
             i = (i + 1) & (slots - 1);
         }
         atomicAdd(&sums[i], (unsigned long long)units);
+        return was == -1 ? i : -1;
     }
 };
 
@@ -740,7 +749,12 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
             g.m = -INFINITY;                       // (a row without words: nothing to read it for)
             g.log_s = g.inv_s = 0.0f;
         }
-        // the row's total and the greatest magnitude of its words' gradients
+        // the row's total and the greatest magnitude of its words' gradients; of a document that is no longer than the workgroup has
+        // room for, words, gradients and logits stay in registers
+        const int64_t n = t1 - t0;
+        const bool brief = !kSingle && n <= min(kThreads * kWordBatch, a.slots / 8 * 7);
+        int32_t words[kWordBatch];
+        float owns[kWordBatch], xs[kWordBatch];
         double total = 0.0;
         float most = 0.0f;
         int32_t word = -1;
@@ -753,17 +767,37 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
                 most = fabsf(a.grad[row]);
             }
         } else {
-            if (kLoss) word_logprobs<T, kThreads>(logits, a.tokens, t0, t1, tid, a.vocab, g.m, g.log_s, a.logprobs);
-            for_words<kThreads>(a.tokens, t0, t1, tid, [&](const int64_t (&t)[kWordBatch], const int32_t (&w)[kWordBatch], const bool (&)[kWordBatch]) {
-                float own[kWordBatch];
-#pragma unroll
-                for (int k = 0; k < kWordBatch; ++k) own[k] = w[k] >= 0 && w[k] < a.vocab ? a.grad[t[k]] : 0.0f;
+            if (brief) {
 #pragma unroll
                 for (int k = 0; k < kWordBatch; ++k) {
-                    total += (double)own[k];
-                    most = fmaxf(most, fabsf(own[k]));
+                    const int64_t t = t0 + k * kThreads + tid;
+                    words[k] = t < t1 ? a.tokens[t] : -1;
                 }
-            });
+                WordTable(table_lds, a.slots).template clear<kThreads>(tid);
+#pragma unroll
+                for (int k = 0; k < kWordBatch; ++k) {
+                    const int64_t t = t0 + k * kThreads + tid;
+                    const bool known = words[k] >= 0 && words[k] < a.vocab;
+                    owns[k] = known ? a.grad[t] : 0.0f;
+                    xs[k] = known ? (float)logits[words[k]] : 0.0f;
+                    if (kLoss && t < t1) a.logprobs[t] = logprob_of(xs[k], words[k], a.vocab, g.m, g.log_s);
+                    if (!known) words[k] = -1;
+                    total += (double)owns[k];
+                    most = fmaxf(most, fabsf(owns[k]));
+                }
+            } else {
+                if (kLoss) word_logprobs<T, kThreads>(logits, a.tokens, t0, t1, tid, a.vocab, g.m, g.log_s, a.logprobs);
+                for_words<kThreads>(a.tokens, t0, t1, tid, [&](const int64_t (&t)[kWordBatch], const int32_t (&w)[kWordBatch], const bool (&)[kWordBatch]) {
+                    float own[kWordBatch];
+#pragma unroll
+                    for (int k = 0; k < kWordBatch; ++k) own[k] = w[k] >= 0 && w[k] < a.vocab ? a.grad[t[k]] : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < kWordBatch; ++k) {
+                        total += (double)own[k];
+                        most = fmaxf(most, fabsf(own[k]));
+                    }
+                });
+            }
             total = wave_sum(total);
             most = wave_max(most);
             if (kWaves > 1) {
@@ -779,6 +813,8 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
                     total += totals[w];
                     most = fmaxf(most, largest[w]);
                 }
+            } else {
+                __syncthreads();
             }
         }
         g.total = (float)total;
@@ -798,9 +834,9 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
             });
         } else {
             const WordTable table(table_lds, a.slots);
-            const int64_t n = t1 - t0;
             const int unit = 62 - (n > 1 ? 64 - __clzll(n - 1) : 0) - (finite && most > 0.0f ? ilogbf(most) + 1 : 0);
             const double units = ldexp(1.0, unit), per_unit = ldexp(1.0, -unit);
+            auto value = [&](unsigned long long sum) { return (float)((double)(long long)sum * per_unit); };
             // put(word, units) for the words of the columns [first, last)
             auto each = [&](int32_t first, int32_t last, auto&& put) {
                 if (!finite) return;
@@ -813,12 +849,23 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
                         if (w[k] >= first && w[k] < last) put(w[k], (long long)rint((double)own[k] * units));
                 });
             };
-            auto value = [&](unsigned long long sum) { return (float)((double)(long long)sum * per_unit); };
-            if (n <= table.slots / 8 * 7) {
-                for (int i = tid; i < table.slots; i += kThreads) {
-                    table.sums[i] = 0;
-                    table.words[i] = -1;
-                }
+            if (brief) {
+                // the thread that brings a word first works out its column, and writes it last
+                int slot[kWordBatch];
+#pragma unroll
+                for (int k = 0; k < kWordBatch; ++k)
+                    slot[k] = finite && words[k] >= begin && words[k] < end ? table.add(words[k], (long long)rint((double)owns[k] * units)) : -1;
+                __syncthreads();
+#pragma unroll
+                for (int k = 0; k < kWordBatch; ++k)
+                    if (slot[k] >= 0) xs[k] = value(table.sums[slot[k]]) + g.template of<kEntropy>(xs[k]);
+                stream_grad<T, kThreads, kLoss, kEntropy>(logits, out, begin, end, g, a.once, [](float (&)[P], int32_t) {});
+                __syncthreads();
+#pragma unroll
+                for (int k = 0; k < kWordBatch; ++k)
+                    if (slot[k] >= 0) out[words[k]] = (T)xs[k];
+            } else if (n <= table.slots / 8 * 7) {
+                table.template clear<kThreads>(tid);
                 __syncthreads();
                 each(begin, end, [&](int32_t w, long long v) { table.add(w, v); });
                 __syncthreads();

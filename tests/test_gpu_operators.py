@@ -402,6 +402,28 @@ def test_logprobs_gradients(ops, rows, vocab, total, dtype):
     assert torch.equal(again[0], logprobs) and torch.equal(held, grad)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,usual", [(30000, 300), (900, 40), (7001, 9)])
+def test_logprobs_gradients_of_documents_of_very_different_lengths(ops, vocab, usual, dtype):
+    """Documents that fit a workgroup's registers, its table, and neither, in one batch."""
+    g = gen(vocab)
+    lengths = torch.full((520,), usual, device="cuda")
+    lengths[:7] = torch.tensor([8 * usual, 12 * usual, 20 * usual, 0, 1, 7 * usual, 3000], device="cuda")
+    row_ptr = torch.cat([lengths.new_zeros(1), lengths.cumsum(0)])
+    total = int(row_ptr[-1])
+    logits = (2 * randn(g, 520, vocab)).to(dtype)
+    tokens = torch.randint(vocab, (total,), generator=g, device="cuda", dtype=torch.int32)
+    weights, h = randn(g, total), randn(g, 520)
+    got, want = check_logprobs(ops, logits, tokens, row_ptr, 3)
+    close(ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr, grad_entropy=h, entropy=got.entropy), *want.grad(weights, h))
+    grad = ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr)
+    close(grad, *want.grad(weights))
+    held = logits.clone()
+    logprobs, _ = ops.token_logprobs_grad(held, tokens, weights, row_ptr, out=held)
+    close(logprobs, want.logprobs, want.off_logp[want.row, want.tokens])
+    close(held, *want.grad(weights))
+
+
 @pytest.mark.parametrize("rows", [5, 700])
 def test_logprobs_gradients_of_one_word_a_row(ops, rows):
     g = gen(rows)
