@@ -108,6 +108,10 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNo
         } else {
             load_row(row, x);
         }
+        // (where they are not held, the loads of weight and bias are to stay in the loop: outside it they are held after all)
+        const void* weight = a.weight;
+        const void* bias = a.bias;
+        if constexpr (!kHeld) asm volatile("" : "+s"(weight), "+s"(bias));
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
@@ -140,8 +144,8 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNo
             for (int j = 0; j < kPieces; ++j) {
                 const int32_t c = (j * kTeam + lane) * P;
                 if constexpr (!kHeld) {
-                    w[0].load(a.weight, c, cols, 1.0f);
-                    b[0].load(a.bias, c, cols, 0.0f);
+                    w[0].load(weight, c, cols, 1.0f);
+                    b[0].load(bias, c, cols, 0.0f);
                 }
                 float v[P], vw[P], vb[P];
                 unpack(x[j], v, T());
@@ -152,6 +156,7 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNo
 #pragma unroll
                 for (int e = 0; e < P; ++e) v[e] = __builtin_fmaf((v[e] - mean) * rstd, vw[e], vb[e]);
                 store_piece(y, c, 0, cols, pack(v, T()), a.once);
+                if constexpr (!kHeld) __builtin_amdgcn_sched_barrier(0);      // (a piece at a time: more have no registers)
             }
             if (lane == 0) {
                 if (a.mean) a.mean[row] = mean;
@@ -277,11 +282,13 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
         } else {
             load_row(row, x, g, mean, rstd);
         }
+        const void* weight = a.weight;             // (as in layer_norm_kernel)
+        if constexpr (!kHeld && !kSums) asm volatile("" : "+s"(weight));
         float sum_h = 0.0f, sum_hu = 0.0f;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             float u[P], h[P], grad[P];
-            if constexpr (!kHeld) w[0].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
+            if constexpr (!kHeld) w[0].load(weight, (j * kTeam + lane) * P, cols, 1.0f);
             forget(w[kHeld ? j : 0].raw);
             grad_piece<T, W>(x[j], g[j], w[kHeld ? j : 0], mean, rstd, u, h, grad);
 #pragma unroll
@@ -299,7 +306,7 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
         for (int j = 0; j < kPieces; ++j) {
             const int32_t c = (j * kTeam + lane) * P;
             float u[P], h[P], v[P];
-            if constexpr (!kHeld) w[0].load(a.weight, c, cols, 1.0f);
+            if constexpr (!kHeld) w[0].load(weight, c, cols, 1.0f);
             forget(w[kHeld ? j : 0].raw);
             grad_piece<T, W>(x[j], g[j], w[kHeld ? j : 0], mean, rstd, u, h, v);
             if constexpr (kSums) {                 // (not beside the sums above: what that needs would be kept until here)
@@ -354,9 +361,21 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
             for (int c = (int)threadIdx.x; c < min(cols, kCols); c += kThreads) put(c, joined[c], joined[kCols + c]);
         } else {
 #pragma unroll
-            for (int j = 0; j < kPieces; ++j)
+            for (int j = 0; j < kPieces; ++j) {
+                const int c = (j * kTeam + lane) * P;
+                if (a.partial && c + P <= cols) {
+                    float* out = a.partial + (int64_t)blockIdx.x * 2 * cols + c;
 #pragma unroll
-                for (int e = 0; e < P; ++e) put((j * kTeam + lane) * P + e, dw[j * P + e], db[j * P + e]);
+                    for (int e = 0; e < P; e += 4) {
+                        const int k = j * P + e;
+                        store_raw(out + e, pack({dw[k], dw[k + 1], dw[k + 2], dw[k + 3]}, 0.0f));
+                        store_raw(out + cols + e, pack({db[k], db[k + 1], db[k + 2], db[k + 3]}, 0.0f));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) put(c + e, dw[j * P + e], db[j * P + e]);
+                }
+            }
         }
     }
 }

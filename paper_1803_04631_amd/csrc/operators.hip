@@ -100,9 +100,9 @@ constexpr int64_t summed_bytes(int64_t type_bytes) { return type_bytes == 4 ? 65
 // The same for the gradient, where a column takes four times the registers; f(team, workgroups that fit a CU).
 template <class F>
 void with_grad_team(int64_t row_bytes, F&& f) {
-    if (row_bytes <= 64) f(Team<4, 1>(), 5);
-    else if (row_bytes <= 256) f(Team<16, 1>(), 5);
-    else if (row_bytes <= 1024) f(Team<64, 1>(), 5);
+    if (row_bytes <= 64) f(Team<4, 1>(), 4);
+    else if (row_bytes <= 256) f(Team<16, 1>(), 4);
+    else if (row_bytes <= 1024) f(Team<64, 1>(), 4);
     else if (row_bytes <= 2048) f(Team<64, 2>(), 4);
     else if (row_bytes <= 4096) f(Team<128, 2>(), 4);
     else if (row_bytes <= 8192) f(Team<256, 2>(), 4);
@@ -114,12 +114,15 @@ void with_grad_team(int64_t row_bytes, F&& f) {
 // Workgroups of the gradient's kernel, each of which leaves sums over its rows.
 int32_t norm_grad_groups(int64_t rows, int32_t cols, int32_t type) {
     const int64_t bytes = cols * (int64_t)type_bytes(type);
-    if (bytes > summed_bytes((int64_t)type_bytes(type))) return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + 63) / 64, 64));      // slabs
+    if (bytes > summed_bytes((int64_t)type_bytes(type))) return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + 15) / 16, 64));      // slabs
     int64_t groups = 1;
     with_grad_team(bytes, [&](auto t, int per_cu) {
         constexpr int kThreads = mlda::team_threads(t.team), kTeams = kThreads / t.team;
         groups = std::min<int64_t>((rows + kTeams - 1) / kTeams, per_cu * kCus);
     });
+    // their sums, written and read, are to be no more than what the rows are, unless they are less than 1 MB: 247 x 14,375 bf16 with a
+    // workgroup a row 31 us, so 27
+    groups = std::min(groups, std::max<int64_t>(rows * (int64_t)type_bytes(type) * 3 / 16, (1 << 20) / (8 * (int64_t)cols)));
     return (int32_t)std::max<int64_t>(1, groups);
 }
 
