@@ -240,14 +240,14 @@ __device__ __forceinline__ void for_tiles(const Span<T>& span, int wave, int wav
             for (int j = 0; j < kTilePieces; ++j) next[j] = span.load(first + (j * kWave + lane) * P, -INFINITY);
         }
     };
-    int64_t first = span.first + (int64_t)wave * kCols;
-    if (first < span.end) load(first);
-    for (; first < span.end; first += (int64_t)waves * kCols) {
+    // (the first round only loads)
+    const int64_t start = span.first + (int64_t)wave * kCols, step = (int64_t)waves * kCols;
+    for (int64_t first = start - step; first < span.end; first += step) {
         Raw now[kTilePieces];
 #pragma unroll
         for (int j = 0; j < kTilePieces; ++j) now[j] = next[j];
-        if (first + (int64_t)waves * kCols < span.end) load(first + (int64_t)waves * kCols);
-        f(now, first);
+        if (first + step < span.end) load(first + step);
+        if (first >= start) f(now, first);
     }
 }
 
@@ -483,9 +483,17 @@ __device__ __forceinline__ int find_top(const Span<T>& span, float most, int n, 
     int count = lds.n;
     if (all) {
         Candidates top{lds.held[wave], n};
-        for_tiles(span, wave, kWaves, [&](const Raw (&now)[kTilePieces], int64_t first) {
-            if (top.wants(tile_max<T>(now))) top.add(span, first);
-        });
+        for (int64_t first = span.first + (int64_t)wave * kCols; first < span.end; first += (int64_t)kWaves * kCols) {
+            float tile = -INFINITY;
+#pragma unroll 1
+            for (int j = 0; j < kTilePieces; ++j) {
+                float v[P];
+                unpack(span.load(first + (j * kWave + lane) * P, -INFINITY), v, T());
+#pragma unroll
+                for (int e = 0; e < P; ++e) tile = fmaxf(tile, v[e]);
+            }
+            if (top.wants(tile)) top.add(span, first);
+        }
         if (top.count < n) top.sort();
         if (lane == 0) lds.counts[wave] = top.count;
         __syncthreads();
