@@ -14,7 +14,7 @@ SOURCES = ["mlda.hip", "operators.hip"]
 TENSORS_PATH = os.path.join(_HERE, "_tensors.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # every fp64 product and sum rounds as written (parity with the fp64 definition)
     "-ffp-contract=off",
     # no packed-fp32 instruction forms
@@ -53,7 +53,8 @@ def build(verbose: bool = False) -> str:
 
     with tempfile.TemporaryDirectory() as objects:
         linked = [os.path.join(objects, source + ".o") for source in SOURCES]
-        run([hipcc, *HIPCC_FLAGS, "-c", "-o", o, os.path.join(CSRC, source)] for o, source in zip(linked, SOURCES))
+        compiled = [flag for flag in HIPCC_FLAGS if flag != "-shared"]
+        run([hipcc, *compiled, "-c", "-o", o, os.path.join(CSRC, source)] for o, source in zip(linked, SOURCES))
         run([[hipcc, "--offload-arch=gfx950", "-shared", "-Wl,-soname,libmlda.so", "-o", LIB_PATH, *linked, "-lpthread"]])
     run([_tensors_command(os.environ.get("ROCM_PATH", "/opt/rocm"))])
     return LIB_PATH
