@@ -509,9 +509,9 @@ __device__ __forceinline__ int find_top(const Span<T>& span, float most, int n, 
 }
 
 // Workgroup by workgroup a row, or a segment of one: with one segment all is done, else logprob_join_kernel goes on.
-template <class T, bool kExtras, int kWaves>
+template <class T, bool kEntropy, bool kTop, int kWaves>
 __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) {
-    __shared__ std::conditional_t<kExtras, TopLds<kWaves>, int> lds;
+    __shared__ std::conditional_t<kTop, TopLds<kWaves>, int> lds;
     __shared__ RowPart part[kWaves];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
     const int64_t items = a.rows * a.segments;
@@ -521,11 +521,11 @@ __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) 
         const int32_t end = min(a.vocab - begin, a.segment_cols) + begin;
         const Span<T> span{static_cast<const T*>(a.logits) + row * a.stride, begin, end};
         LaneSums sums;
-        if constexpr (kExtras) {
+        if constexpr (kTop) {
             StretchMost<kWaves> seen{lds, stretch_tiles<T, kWaves>(span)};
-            sums = walk_row<T, true>(span, wave, kWaves, [&](float tile) { if (a.top) seen(tile); });
+            sums = walk_row<T, kEntropy>(span, wave, kWaves, seen);
         } else {
-            sums = walk_row<T, false>(span, wave, kWaves, [](float) {});
+            sums = walk_row<T, kEntropy>(span, wave, kWaves, [](float) {});
         }
         float m = sums.m;
         double s = sums.s, u = sums.u;
@@ -533,8 +533,8 @@ __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) 
         if (lane == 0) part[wave] = RowPart{s, u, m, 0};
         int count = 0;
         const uint64_t* best = nullptr;
-        if constexpr (kExtras) {
-            if (a.top) count = find_top(span, sums.m, a.top, lds);
+        if constexpr (kTop) {
+            count = find_top(span, sums.m, a.top, lds);
             best = lds.best;
         }
         __syncthreads();
@@ -543,7 +543,7 @@ __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) 
             finish_row<T, kWaves * kWave>(a, row, RowStats(m, s, u), best);
         } else {
             if (threadIdx.x == 0) a.parts[item] = RowPart{s, u, m, count};
-            if (kExtras && wave == 0 && lane < a.top) a.part_top[item * a.top + lane] = lane < count ? best[lane] : 0;
+            if (kTop && wave == 0 && lane < a.top) a.part_top[item * a.top + lane] = lane < count ? best[lane] : 0;
         }
         __syncthreads();                           // (the next row's parts and candidates)
     }

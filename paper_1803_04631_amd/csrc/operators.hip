@@ -183,15 +183,14 @@ int run_logprobs(mlda::LogprobArgs a, int32_t type, void* workspace, hipStream_t
     const dim3 grid((unsigned)std::min(a.rows * a.segments, kMostGroups)), threads(mlda::kLogprobWaves * mlda::kWave);
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        constexpr int kWaves = mlda::kLogprobWaves;
-        const bool extras = a.top || a.entropy;
-        if (wave_rows(a.rows, a.vocab, type) && (mean_len < 512 || a.words_apart)) {
-            if (extras) hipLaunchKernelGGL((mlda::logprob_kernel<T, true, 1>), grid, dim3(mlda::kWave), 0, stream, a);
-            else hipLaunchKernelGGL((mlda::logprob_kernel<T, false, 1>), grid, dim3(mlda::kWave), 0, stream, a);
-        } else {
-            if (extras) hipLaunchKernelGGL((mlda::logprob_kernel<T, true, kWaves>), grid, threads, 0, stream, a);
-            else hipLaunchKernelGGL((mlda::logprob_kernel<T, false, kWaves>), grid, threads, 0, stream, a);
-        }
+        auto launch = [&](auto waves) {
+            constexpr int kWaves = decltype(waves)::value;
+            if (a.top) hipLaunchKernelGGL((mlda::logprob_kernel<T, true, true, kWaves>), grid, dim3(kWaves * mlda::kWave), 0, stream, a);
+            else if (a.entropy) hipLaunchKernelGGL((mlda::logprob_kernel<T, true, false, kWaves>), grid, dim3(kWaves * mlda::kWave), 0, stream, a);
+            else hipLaunchKernelGGL((mlda::logprob_kernel<T, false, false, kWaves>), grid, dim3(kWaves * mlda::kWave), 0, stream, a);
+        };
+        if (wave_rows(a.rows, a.vocab, type) && (mean_len < 512 || a.words_apart)) launch(std::integral_constant<int, 1>());
+        else launch(std::integral_constant<int, mlda::kLogprobWaves>());
         RC_TRY(launched("logprob_kernel"));
         if (a.segments > 1) {
             hipLaunchKernelGGL((mlda::logprob_join_kernel<T>), dim3((unsigned)std::min(a.rows, kMostGroups)), threads, 0, stream, a);
