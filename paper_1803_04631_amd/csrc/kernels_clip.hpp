@@ -14,9 +14,9 @@
 namespace mlda {
 
 constexpr int kClipThreads = 256;
-constexpr int kClipUnit = 4096;              // elements
+constexpr int kClipUnit = 8192;              // elements
 constexpr int kClipTensors = 120;            // of one launch: their table is a kernel argument
-constexpr int kClipGroups = 2048;            // workgroups of one launch at most
+constexpr int kClipGroups = 1024;            // workgroups of one launch at most: four to a CU (142e6 bf16 elements read in 47 us, with twice as many of half the unit 54)
 
 struct ClipTensor {
     const void* in;

@@ -657,3 +657,10 @@ def test_refusals(ops):
     for call in (lambda: ops.layer_norm(x, eps=-1.0), lambda: ops.layer_norm(x, eps=NAN), lambda: ops.clip_grads([x], -1.0), lambda: ops.clip_grads([x], NAN)):
         with pytest.raises(mlda.MldaError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_clip_at_the_edges_of_its_units(ops, dtype):
+    g = gen(21)
+    for n in (8191, 8192, 8193, 16384, 16391, 8192 * 1024, 8192 * 1024 + 1):
+        check_clip(ops, [randn(g, n, dtype=dtype), randn(g, 3, dtype=dtype)], 0.5)
