@@ -664,3 +664,33 @@ def test_clip_at_the_edges_of_its_units(ops, dtype):
     g = gen(21)
     for n in (8191, 8192, 8193, 16384, 16391, 8192 * 1024, 8192 * 1024 + 1):
         check_clip(ops, [randn(g, n, dtype=dtype), randn(g, 3, dtype=dtype)], 0.5)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [24001, 33001, 70001, 300001])
+def test_layer_norm_of_very_long_rows(ops, cols, dtype):
+    g = gen(cols)
+    x = (randn(g, 3, cols) + randn(g, 3, 1)).to(dtype)
+    weight, bias, grad = randn(g, cols, dtype=dtype), randn(g, cols, dtype=dtype), randn(g, 3, cols, dtype=dtype)
+    got = ops.layer_norm(x, weight, bias)
+    check_norm(x, weight, bias, 1e-5, got)
+    check_norm_grad(grad, x, got[1], got[2], weight, ops.layer_norm_backward(grad, x, got[1], got[2], weight))
+    want = ops.layer_norm_backward(grad, x, got[1], got[2], weight)[0]
+    held = x.clone()
+    assert torch.equal(ops.layer_norm_backward(grad, held, got[1], got[2], weight, out=held)[0], want)
+    held = x.clone()
+    assert torch.equal(ops.layer_norm(held, weight, bias, out=held)[0], got[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_logprobs_over_millions_of_words(ops, dtype):
+    g = gen(31)
+    vocab = 3000017
+    logits = (2 * randn(g, 2, vocab)).to(dtype)
+    row_ptr, tokens = documents(g, 2, vocab, 300)
+    weights, h = randn(g, 300), randn(g, 2)
+    got, want = check_logprobs(ops, logits, tokens, row_ptr, 20)
+    close(ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr, grad_entropy=h, entropy=got.entropy), *want.grad(weights, h))
+    logprobs, grad = ops.token_logprobs_grad(logits, tokens, weights, row_ptr)
+    close(grad, *want.grad(weights))
+    assert torch.equal(logprobs, got.logprobs)
