@@ -735,28 +735,6 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
         RowGrad g;
         g.h = kEntropy ? a.grad_entropy[row] : 0.0f;
         g.entropy = kEntropy ? a.entropy[row] : 0.0f;
-        if (kLoss && t1 > t0) {
-            const LaneSums sums = walk_row<T, false>(Span<T>{logits, begin, end}, wave, kWaves, [](float) {});
-            float m = sums.m;
-            double s = sums.s, u = 0.0;
-            join_lanes(m, s, u);
-            if (kWaves > 1) {
-                if (lane == 0) part[wave] = RowPart{s, u, m, 0};
-                __syncthreads();
-                join_parts(part, kWaves, m, s, u);
-            }
-            const RowStats st(m, s, u);
-            g.m = st.m;
-            g.log_s = st.log_s;
-            g.inv_s = (float)(1.0 / s);
-        } else if (!kLoss) {
-            g.m = a.stats[2 * row];
-            g.log_s = a.stats[2 * row + 1];
-            g.inv_s = (float)exp(-(double)g.log_s);
-        } else {
-            g.m = -INFINITY;                       // (a row without words: nothing to read it for)
-            g.log_s = g.inv_s = 0.0f;
-        }
         // the row's total and the greatest magnitude of its words' gradients; of a document that is no longer than the workgroup has
         // room for, words, gradients and logits stay in registers
         const int64_t n = t1 - t0;
@@ -768,9 +746,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
         int32_t word = -1;
         if (kSingle) {
             word = a.tokens[row];
-            if (kLoss && tid == 0) a.logprobs[row] = word_logprob(logits, word, a.vocab, g.m, g.log_s);
-            if (word >= a.vocab) word = -1;
-            if (word >= 0) {
+            if (word >= 0 && word < a.vocab) {
                 total = (double)a.grad[row];
                 most = fabsf(a.grad[row]);
             }
@@ -784,17 +760,13 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
                 WordTable(table_lds, a.slots).template clear<kThreads>(tid);
 #pragma unroll
                 for (int k = 0; k < kWordBatch; ++k) {
-                    const int64_t t = t0 + k * kThreads + tid;
                     const bool known = words[k] >= 0 && words[k] < a.vocab;
-                    owns[k] = known ? a.grad[t] : 0.0f;
+                    owns[k] = known ? a.grad[t0 + k * kThreads + tid] : 0.0f;
                     xs[k] = known ? (float)logits[words[k]] : 0.0f;
-                    if (kLoss && t < t1) a.logprobs[t] = logprob_of(xs[k], words[k], a.vocab, g.m, g.log_s);
-                    if (!known) words[k] = -1;
                     total += (double)owns[k];
                     most = fmaxf(most, fabsf(owns[k]));
                 }
             } else {
-                if (kLoss) word_logprobs<T, kThreads>(logits, a.tokens, t0, t1, tid, a.vocab, g.m, g.log_s, a.logprobs);
                 for_words<kThreads>(a.tokens, t0, t1, tid, [&](const int64_t (&t)[kWordBatch], const int32_t (&w)[kWordBatch], const bool (&)[kWordBatch]) {
                     float own[kWordBatch];
 #pragma unroll
@@ -808,22 +780,52 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
             }
             total = wave_sum(total);
             most = wave_max(most);
-            if (kWaves > 1) {
-                if (lane == 0) {
-                    totals[wave] = total;
-                    largest[wave] = most;
-                }
-                __syncthreads();
-                total = 0.0;
-                most = 0.0f;
+            if (lane == 0) {
+                totals[wave] = total;
+                largest[wave] = most;
+            }
+        }
+        const bool walked = kLoss && n > 0;        // (a row without words: nothing to read it for)
+        float m = -INFINITY;
+        double s = 0.0, u = 0.0;
+        if (walked) {
+            const LaneSums sums = walk_row<T, false>(Span<T>{logits, begin, end}, wave, kWaves, [](float) {});
+            m = sums.m;
+            s = sums.s;
+            join_lanes(m, s, u);
+            if (lane == 0) part[wave] = RowPart{s, u, m, 0};
+        }
+        if (kLoss || !kSingle) __syncthreads();
+        if (!kSingle) {
+            total = 0.0;
+            most = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) {
-                    total += totals[w];
-                    most = fmaxf(most, largest[w]);
+            for (int w = 0; w < kWaves; ++w) {
+                total += totals[w];
+                most = fmaxf(most, largest[w]);
+            }
+        }
+        if (kLoss) {
+            if (walked && kWaves > 1) join_parts(part, kWaves, m, s, u);
+            const RowStats st(m, s, u);
+            g.m = st.m;
+            g.log_s = st.log_s;
+            g.inv_s = (float)(1.0 / s);
+            if (kSingle) {
+                if (tid == 0) a.logprobs[row] = word_logprob(logits, word, a.vocab, g.m, g.log_s);
+            } else if (brief) {
+#pragma unroll
+                for (int k = 0; k < kWordBatch; ++k) {
+                    const int64_t t = t0 + k * kThreads + tid;
+                    if (t < t1) a.logprobs[t] = logprob_of(xs[k], words[k], a.vocab, g.m, g.log_s);
                 }
             } else {
-                __syncthreads();
+                word_logprobs<T, kThreads>(logits, a.tokens, t0, t1, tid, a.vocab, g.m, g.log_s, a.logprobs);
             }
+        } else {
+            g.m = a.stats[2 * row];
+            g.log_s = a.stats[2 * row + 1];
+            g.inv_s = (float)exp(-(double)g.log_s);
         }
         g.total = (float)total;
         const bool finite = most < INFINITY && total == total;
@@ -835,7 +837,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
         } else if (kSingle) {
             if (kLoss) __syncthreads();
             stream_grad<T, kThreads, kLoss, kEntropy>(logits, out, begin, end, g, a.once, [&](float (&v)[P], int32_t c) {
-                if (word >= 0 && (uint32_t)(word - c) < (uint32_t)P) {
+                if (word >= 0 && word < a.vocab && (uint32_t)(word - c) < (uint32_t)P) {
 #pragma unroll
                     for (int e = 0; e < P; ++e) v[e] += c + e == word ? (float)total : 0.0f;
                 }
