@@ -280,7 +280,7 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
  *   tokens    n_tokens (< 2^31) words.  Below zero: no word (log-probability 0, no gradient); vocab or more: NaN, no gradient.
  *   row_ptr   rows + 1 entries as in mlda_create, here on the device: row r has the words row_ptr[r] .. row_ptr[r+1]-1 (the bounds are
  *             clamped to 0 .. n_tokens).  Null: one word to a row, n_tokens = rows.
- *   logprobs  n_tokens entries
+ *   logprobs  n_tokens entries.  Tokens before row_ptr[0] and from row_ptr[rows] on are no row's: 0.  (Without rows nothing is written.)
  *   stats     rows x 2: the greatest logit m and the logarithm of the sum of exp(logit - m), for the backward
  *             pass (their sum is the logarithm of the sum of exponentials); null: not wanted
  *   entropy   rows entries; null: not wanted

@@ -308,6 +308,18 @@ __device__ __forceinline__ void row_tokens(const int64_t* row_ptr, int64_t n_tok
     }
 }
 
+// Tokens before the first row's and behind the last row's are no row's words: their log-probability is 0, as a word's below zero.  One of
+// `parts` shares of them, so that a batch out of a long list of tokens does not leave them all to one workgroup.
+template <int kThreads>
+__device__ __forceinline__ void clear_rest(const int64_t* row_ptr, int64_t rows, int64_t n_tokens, int64_t part, int64_t parts, float* logprobs) {
+    if (!row_ptr) return;
+    const int64_t head = min(max(row_ptr[0], (int64_t)0), n_tokens), tail = min(max(row_ptr[rows], head), n_tokens);
+    const int64_t n = head + (n_tokens - tail);
+    if (n == 0) return;
+    const int64_t last = n * (part + 1) / parts;
+    for (int64_t i = n * part / parts + threadIdx.x; i < last; i += kThreads) logprobs[i < head ? i : tail + (i - head)] = 0.0f;
+}
+
 constexpr int kWordBatch = 4;                     // words that a thread has on their way
 
 // f(token's number, word, is there one) for the tokens [begin, end), `threads` threads side by side; every thread calls it as often.
@@ -365,6 +377,7 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int64_t row, co
         row_tokens(a.row_ptr, a.n_tokens, row, begin, end);
         word_logprobs<T, kThreads>(static_cast<const T*>(a.logits) + row * a.stride, a.tokens, min(begin + done, end), end, (int)threadIdx.x, a.vocab, st.m, st.log_s,
                                    a.logprobs);
+        clear_rest<kThreads>(a.row_ptr, a.rows, a.n_tokens, row, a.rows, a.logprobs);
     }
     if (threadIdx.x == 0) {
         if (a.stats) {
@@ -393,6 +406,7 @@ __global__ __launch_bounds__(kLogprobWaves * kWave) void logprob_words_kernel(Lo
         begin = min(begin + item % split * each, end);
         word_logprobs<T, kThreads>(static_cast<const T*>(a.logits) + row * a.stride, a.tokens, begin, min(begin + each, end), (int)threadIdx.x,
                                    a.vocab, a.stats[2 * row], a.stats[2 * row + 1], a.logprobs);
+        clear_rest<kThreads>(a.row_ptr, a.rows, a.n_tokens, item, a.rows * split, a.logprobs);
     }
 }
 
@@ -826,6 +840,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
             } else {
                 word_logprobs<T, kThreads>(logits, a.tokens, t0, t1, tid, a.vocab, g.m, g.log_s, a.logprobs);
             }
+            clear_rest<kThreads>(a.row_ptr, a.rows, a.n_tokens, row, a.rows, a.logprobs);
         } else {
             g.m = a.stats[2 * row];
             g.log_s = a.stats[2 * row + 1];

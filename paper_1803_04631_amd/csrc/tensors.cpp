@@ -91,6 +91,11 @@ void* at_of(const Tensor& t, const char* name, at::IntArrayRef shape, at::Scalar
 
 Tensor empty(at::IntArrayRef shape, at::ScalarType type, at::Device device) { return at::empty(shape, at::TensorOptions(device).dtype(type)); }
 Tensor fp32(at::IntArrayRef shape, at::Device device) { return empty(shape, at::kFloat, device); }
+// A number for each token: the library writes all of them, but without rows it has nothing to do.
+Tensor of_tokens(int64_t n, int64_t rows, at::Device device) {
+    const Tensor t = empty({n}, at::kFloat, device);
+    return rows ? t : t.zero_();
+}
 
 Tensor out_for(const Maybe& out, const Tensor& like, const Rows& rows, Rows& r) {
     const Tensor t = out ? *out : empty(like.sizes(), like.scalar_type(), rows.device);
@@ -181,7 +186,7 @@ std::tuple<Tensor, Tensor, Maybe, Maybe, Maybe> token_logprobs(const Tensor& log
     const Rows& r = d.r;
     TORCH_CHECK_VALUE(alternatives >= 0 && alternatives <= MLDA_MAX_ALTERNATIVES && alternatives <= r.cols,
                       "alternatives must be in 0 .. ", MLDA_MAX_ALTERNATIVES, ", and no more than there are words");
-    const Tensor logprobs = fp32({d.n}, r.device), stats = fp32({r.rows, 2}, r.device);
+    const Tensor logprobs = of_tokens(d.n, r.rows, r.device), stats = fp32({r.rows, 2}, r.device);
     Maybe entropies, ids, top;
     if (entropy) entropies = fp32({r.rows}, r.device);
     if (alternatives) {
@@ -221,7 +226,7 @@ std::tuple<Tensor, Tensor> token_logprobs_grad(const Tensor& logits, const Tenso
     const Documents d(logits, tokens, row_ptr);
     const Rows& r = d.r;
     void* at_weights = at_of(weights, "weights", {d.n}, at::kFloat, r.device);
-    const Tensor logprobs = fp32({d.n}, r.device);
+    const Tensor logprobs = of_tokens(d.n, r.rows, r.device);
     Rows ro;
     const Tensor grad = out_for(out, logits, r, ro);
     const Workspace w(d.workspace(0), r.device);

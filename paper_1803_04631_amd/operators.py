@@ -48,7 +48,8 @@ def layer_norm_backward(grad_y, x, mean, rstd, weight=None, out=None):
 def token_logprobs(logits, tokens, row_ptr=None, alternatives: int = 0, entropy: bool = False) -> TokenLogprobs:
     """Log-probabilities of tokens (int32 words) under the softmax of their rows of logits [rows, vocab]:
     row r has the tokens row_ptr[r] .. row_ptr[r+1]-1 (int64, on the GPU, its last entry at most the number
-    of tokens), or without row_ptr one each.  Tokens below zero are none.  With `alternatives` also each row's
+    of tokens), or without row_ptr one each.  Tokens below zero are none; their log-probability is 0, and so
+    is that of tokens before the first row's or behind the last row's.  With `alternatives` also each row's
     likeliest words, ties to the lowest; with `entropy` the entropies."""
     return TokenLogprobs(*_tensors.token_logprobs(logits, tokens, row_ptr, alternatives, entropy))
 

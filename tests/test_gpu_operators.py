@@ -694,3 +694,40 @@ def test_logprobs_over_millions_of_words(ops, dtype):
     logprobs, grad = ops.token_logprobs_grad(logits, tokens, weights, row_ptr)
     close(grad, *want.grad(weights))
     assert torch.equal(logprobs, got.logprobs)
+
+
+@pytest.mark.parametrize("rows,vocab,inside", [(20, 300, 40), (3, 20000, 500), (600, 300, 900), (2100, 3000, 900), (520, 5001, 60), (2, 700, 9000)])
+def test_tokens_of_no_row(ops, rows, vocab, inside):
+    """Tokens before the first row's and behind the last row's: their log-probabilities are zeros, wherever the memory comes from."""
+    g = gen(rows + inside)
+    head, tail = 37, 5001
+    total = head + inside + tail
+    logits, weights = randn(g, rows, vocab), randn(g, total)
+    row_ptr, tokens = documents(g, rows, vocab, inside)
+    outside = torch.full((total,), 2 ** 31 - 1, dtype=torch.int32, device="cuda")       # (would be NaN if they were looked up)
+    outside[head:head + inside] = tokens
+    want = ops.token_logprobs(logits, tokens, row_ptr).logprobs
+    fused, grad = ops.token_logprobs_grad(logits, tokens, weights[head:head + inside], row_ptr)
+
+    def used_memory():
+        torch.full((total,), 5.0, device="cuda")
+
+    for first, last in ((head, 0), (0, tail), (head, tail)):
+        t, w = outside[head - first:head + inside + last], weights[head - first:head + inside + last]
+        used_memory()
+        got = ops.token_logprobs(logits, t, row_ptr + first).logprobs
+        used_memory()
+        got_fused, got_grad = ops.token_logprobs_grad(logits, t, w, row_ptr + first)
+        for all_of, part in ((got, want), (got_fused, fused)):
+            assert torch.equal(all_of[first:first + inside], part)
+            assert not all_of[:first].any() and not all_of[first + inside:].any()
+        assert torch.equal(got_grad, grad)
+        assert torch.equal(ops.token_logprobs_backward(w, logits, t, ops.token_logprobs(logits, t, row_ptr + first).stats, row_ptr + first),
+                           ops.token_logprobs_backward(weights[head:head + inside], logits, tokens, ops.token_logprobs(logits, tokens, row_ptr).stats, row_ptr))
+    # no rows at all
+    used_memory()
+    got = ops.token_logprobs(logits[:0], outside, row_ptr[:1], alternatives=3, entropy=True)
+    assert got.logprobs.shape == (total,) and not got.logprobs.any() and got.entropy.shape == (0,) and got.top_ids.shape == (0, 3)
+    used_memory()
+    logprobs, nothing = ops.token_logprobs_grad(logits[:0], outside, weights, row_ptr[:1])
+    assert not logprobs.any() and nothing.shape == (0, vocab)
