@@ -478,32 +478,37 @@ __global__ __launch_bounds__(256) void layer_norm_grad_columns_kernel(LayerNormG
     }
 }
 
-// The workgroups' sums added up, in their order, and rounded to the weight's type: 16 columns of [dw, db] a workgroup, by 64
+// The workgroups' sums added up, in their order, and rounded to the weight's type: 16 columns of [dw, db] a workgroup at a time, by 64
 // slices of the workgroups.
+constexpr int kFinalCols = 16;
 template <class W>
 __global__ __launch_bounds__(1024) void layer_norm_grad_final_kernel(const float* partial, int32_t partials, int32_t cols,
                                                                      W* grad_weight, W* grad_bias) {
-    constexpr int kCols = 16, kSlices = 64;
-    __shared__ float joined[kSlices][kCols + 1];
-    const int slice = (int)threadIdx.x / kCols, lane = (int)threadIdx.x % kCols;
-    const int64_t i = (int64_t)blockIdx.x * kCols + lane;
-    float sum = 0.0f;
-    if (i < 2 * (int64_t)cols)
+    constexpr int kSlices = 64;
+    __shared__ float joined[2][kSlices][kFinalCols + 1];
+    const int slice = (int)threadIdx.x / kFinalCols, lane = (int)threadIdx.x % kFinalCols;
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * kFinalCols; first < 2 * (int64_t)cols; first += (int64_t)gridDim.x * kFinalCols, turn ^= 1) {
+        const int64_t i = first + lane;
+        float sum = 0.0f;
+        if (i < 2 * (int64_t)cols)
 #pragma unroll 4
-        for (int p = slice; p < partials; p += kSlices) sum += partial[(int64_t)p * 2 * cols + i];
-    joined[slice][lane] = sum;
-    __syncthreads();
-    // a column to each group of 16 lanes: four slices a lane, then the lanes
-    const int column = (int)threadIdx.x / 16, part = (int)threadIdx.x % 16;
-    if (threadIdx.x >= kCols * 16) return;
-    sum = (joined[part][column] + joined[part + 16][column]) + (joined[part + 32][column] + joined[part + 48][column]);
-    sum = row16_sum(sum);
-    const int64_t at = (int64_t)blockIdx.x * kCols + column;
-    if (part != 0 || at >= 2 * (int64_t)cols) return;
-    if (at < cols) {
-        if (grad_weight) grad_weight[at] = (W)sum;
-    } else if (grad_bias) {
-        grad_bias[at - cols] = (W)sum;
+            for (int p = slice; p < partials; p += kSlices) sum += partial[(int64_t)p * 2 * cols + i];
+        joined[turn][slice][lane] = sum;
+        __syncthreads();
+        // a column to each group of 16 lanes: four slices a lane, then the lanes
+        const int column = (int)threadIdx.x / 16, part = (int)threadIdx.x % 16;
+        if (threadIdx.x >= kFinalCols * 16) continue;
+        const float(&from)[kSlices][kFinalCols + 1] = joined[turn];
+        sum = (from[part][column] + from[part + 16][column]) + (from[part + 32][column] + from[part + 48][column]);
+        sum = row16_sum(sum);
+        const int64_t at = first + column;
+        if (part != 0 || at >= 2 * (int64_t)cols) continue;
+        if (at < cols) {
+            if (grad_weight) grad_weight[at] = (W)sum;
+        } else if (grad_bias) {
+            grad_bias[at - cols] = (W)sum;
+        }
     }
 }
 

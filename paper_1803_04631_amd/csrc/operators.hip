@@ -28,7 +28,7 @@ int launched(const char* what) {
 constexpr int32_t kMostCols = 1 << 30;        // columns and words are 32-bit in the kernels, with room for a tile past the end
 constexpr int kCus = 256;
 constexpr int64_t kWaveRowBytes = 16384, kGroupRowBytes = 65536;
-constexpr int64_t kMostGroups = 1 << 20;      // of a launch: rows beyond are taken in turn
+constexpr int64_t kMostGroups = 1 << 20;      // of a launch, which has fewer than 2^32 threads: what is beyond is taken in turn
 
 bool known_type(int32_t t) { return t == MLDA_FP32 || t == MLDA_BF16 || t == MLDA_FP16; }
 size_t type_bytes(int32_t t) { return t == MLDA_FP32 ? 4 : 2; }
@@ -407,8 +407,9 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
         }
         RC_TRY(launched("layer_norm_grad_kernel"));
         if (!sums || (rows > 0 && !a.partial)) return MLDA_OK;
-        hipLaunchKernelGGL((mlda::layer_norm_grad_final_kernel<W>), dim3((unsigned)((2 * (int64_t)cols + 15) / 16)), dim3(1024), 0, stream,
-                           a.partial, rows > 0 ? groups : 0, cols, static_cast<W*>(grad_weight), static_cast<W*>(grad_bias));
+        const int64_t finals = std::min((2 * (int64_t)cols + mlda::kFinalCols - 1) / mlda::kFinalCols, kMostGroups);
+        hipLaunchKernelGGL((mlda::layer_norm_grad_final_kernel<W>), dim3((unsigned)finals), dim3(1024), 0, stream, a.partial,
+                           rows > 0 ? groups : 0, cols, static_cast<W*>(grad_weight), static_cast<W*>(grad_bias));
         return launched("layer_norm_grad_final_kernel");
     });
 }

@@ -731,3 +731,19 @@ def test_tokens_of_no_row(ops, rows, vocab, inside):
     used_memory()
     logprobs, nothing = ops.token_logprobs_grad(logits[:0], outside, weights, row_ptr[:1])
     assert not logprobs.any() and nothing.shape == (0, vocab)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_layer_norm_gradients_of_more_columns_than_a_launch_has_groups_for(ops, dtype):
+    """16 columns' sums to a workgroup of 1,024 threads: 2^25 columns would be 2^32 threads, more than a launch may have."""
+    g = gen(41)
+    cols = 2 ** 25 + 5
+    x, grad = randn(g, 2, cols, dtype=dtype), randn(g, 2, cols, dtype=dtype)
+    weight = (1 + 0.3 * randn(g, cols)).to(dtype)
+    mean, rstd = x.double().mean(1).float(), (1 / x.double().std(1)).float()
+    want = norm_grad64(grad, x, mean, rstd, weight)
+    got = ops.layer_norm_backward(grad, x, mean, rstd, weight)
+    check_norm_grad(grad, x, mean, rstd, weight, got)
+    # two rows: each column's sums are two products and an addition, as far from the start as from the end
+    for a, b, size in ((got[1], want[1], 6.0), (got[2], want[2], 2.0)):
+        close(a, b, size * U * (grad.double().abs() * 8).sum(0))
