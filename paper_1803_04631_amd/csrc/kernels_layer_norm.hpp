@@ -6,7 +6,8 @@
 // Bound by memory (7 and 13 operations an element).  A row is held by a team of lanes, so many 16-byte pieces each, from its one read
 // to its one write: four or sixteen lanes, a wave, or a workgroup, by the bytes of a row.  Teams take row after row, so that
 // weight and bias are read once and the weight's gradient is summed in registers; the next row's loads are on their way
-// while a row is worked on.  Sums are fp32 in a fixed order, the deviations' squares are taken after the mean is known.
+// while a row is worked on.  Sums are in a fixed order, fp32 where a lane adds up 64 columns at the most, fp64 in longer rows; the
+// deviations' squares are taken after the mean is known.
 #pragma once
 #include "vec_io.hpp"
 
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNo
     __shared__ float slots[2][kThreads / kWave];
     const int lane = (int)threadIdx.x % kTeam;
     const int32_t cols = a.cols;
-    const float n_cols = (float)cols;              // (a quotient is right where the sum is: a row of equal numbers has no variance)
+    const float n_cols = (float)cols;              // (a quotient is right where the sum is)
     Columns<W, P> w[kHeld ? kPieces : 1], b[kHeld ? kPieces : 1];
     if constexpr (kHeld) {
 #pragma unroll
@@ -168,33 +169,36 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNo
 }
 
 // Rows that no team has the registers for: a workgroup reads them three times, the second and third time from the caches (2,003 x 40,000
-// fp32 172 us, 3.7 TB/s of the row once in and once out).
+// fp32 172 us, 3.7 TB/s of the row once in and once out).  A thread adds up any number of columns, so in fp64, which the reads leave time for: the
+// sum of equal numbers is exact, whatever their number.
 template <class T, class W>
 __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a) {
     constexpr int P = kPack<T>;
-    __shared__ float slots[2][16];
+    __shared__ double slots[2][16];
     const int32_t cols = a.cols;
-    const float n_cols = (float)cols;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
         T* y = static_cast<T*>(a.y) + row * a.y_stride;
-        float sum = 0.0f;
+        double sum = 0.0;
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             float v[P];
             unpack(load_some(x + c, (int)min((int64_t)P, cols - c), 0.0f, c), v, T());
 #pragma unroll
-            for (int e = 0; e < P; ++e) sum += v[e];
+            for (int e = 0; e < P; ++e) sum += (double)v[e];
         }
-        const float mean = team_sum<1024>(sum, slots[0]) / n_cols;
-        float squares = 0.0f;
+        const float mean = (float)(group_sum<1024>(sum, slots[0]) / cols);
+        double squares = 0.0;
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             const int n = (int)min((int64_t)P, cols - c);
             float v[P];
             unpack(load_some(x + c, n, 0.0f, c), v, T());
 #pragma unroll
-            for (int e = 0; e < P; ++e) squares += e < n ? (v[e] - mean) * (v[e] - mean) : 0.0f;
+            for (int e = 0; e < P; ++e) {
+                const double d = e < n ? (double)(v[e] - mean) : 0.0;
+                squares = __builtin_fma(d, d, squares);
+            }
         }
-        const float rstd = 1.0f / sqrtf(team_sum<1024>(squares, slots[1]) / n_cols + a.eps);
+        const float rstd = 1.0f / sqrtf((float)(group_sum<1024>(squares, slots[1]) / cols) + a.eps);
         // (x and y may be the same rows: what is written below is read by the same thread only)
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             const int n = (int)min((int64_t)P, cols - c);
@@ -385,42 +389,39 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
 }
 
 // Rows without room in registers: the gradient of x by a workgroup a row, which reads the row twice (2,003 x 40,000 fp32 with the sums
-// below 368 us, 2.6 TB/s of everything once).
+// below 368 us, 2.6 TB/s of everything once).  Sums over columns in fp64, as above.
 template <class T, class W>
 __global__ __launch_bounds__(1024) void layer_norm_grad_long_kernel(LayerNormGradArgs a) {
     constexpr int P = kPack<T>;
-    __shared__ float slots[2][32];
+    __shared__ double slots[2][2][16];
     const int32_t cols = a.cols;
-    const float n_cols = (float)cols;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
         const T* grad = static_cast<const T*>(a.grad) + row * a.grad_stride;
         T* dx = static_cast<T*>(a.grad_x) + row * a.grad_x_stride;
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float sum_h = 0.0f, sum_hu = 0.0f;
+        double sum_h = 0.0, sum_hu = 0.0;
         auto piece = [&](int64_t c, float (&u)[P], float (&h)[P]) {
             const int n = (int)min((int64_t)P, cols - c);
             Columns<W, P> w;
             float unused[P];
             w.load(a.weight, (int32_t)c, cols, 1.0f);
             grad_piece<T, W>(load_some(x + c, n, 0.0f, c), load_some(grad + c, n, 0.0f, c), w, mean, rstd, u, h, unused);
-            return n;
         };
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             float u[P], h[P];
             piece(c, u, h);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                sum_h += h[e];
-                sum_hu = __builtin_fmaf(h[e], u[e], sum_hu);
+                sum_h += (double)h[e];
+                sum_hu = __builtin_fma((double)h[e], (double)u[e], sum_hu);
             }
         }
-        team_sums<1024>(sum_h, sum_hu, slots[turn]);
-        const float mean_h = sum_h / n_cols, mean_hu = sum_hu / n_cols;
+        const float mean_h = (float)(group_sum<1024>(sum_h, slots[turn][0]) / cols), mean_hu = (float)(group_sum<1024>(sum_hu, slots[turn][1]) / cols);
         for (int64_t c = (int64_t)threadIdx.x * P; c < cols; c += 1024 * P) {
             float u[P], h[P], v[P];
-            const int n = piece(c, u, h);
+            piece(c, u, h);
 #pragma unroll
             for (int e = 0; e < P; ++e) v[e] = rstd * ((h[e] - mean_h) - u[e] * mean_hu);
             store_piece(dx, c, 0, cols, pack(v, T()), a.once);

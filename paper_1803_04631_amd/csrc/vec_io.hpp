@@ -267,6 +267,18 @@ __device__ __forceinline__ float team_sum(float v, float* slots) {
     return v;
 }
 
+// The same in fp64 over a workgroup.
+template <int kThreads>
+__device__ __forceinline__ double group_sum(double v, double* slots) {
+    v = wave_sum(v);
+    if (lane_id() == 0) slots[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int w = 0; w < kThreads / kWave; ++w) v += slots[w];
+    return v;
+}
+
 // Two sums with one barrier; slots of twice the size.
 template <int kTeam>
 __device__ __forceinline__ void team_sums(float& a, float& b, float* slots) {

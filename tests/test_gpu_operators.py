@@ -747,3 +747,41 @@ def test_layer_norm_gradients_of_more_columns_than_a_launch_has_groups_for(ops, 
     # two rows: each column's sums are two products and an addition, as far from the start as from the end
     for a, b, size in ((got[1], want[1], 6.0), (got[2], want[2], 2.0)):
         close(a, b, size * U * (grad.double().abs() * 8).sum(0))
+
+
+def check_norm_grad_columns(g, x, mean, rstd, weight, got, adds):
+    """The gradient of x where the sums over columns are within `adds` units of roundoff of their magnitudes.  h is rounded once and u
+    twice (difference, product); a mean once more; then two differences and two products."""
+    dx = norm_grad64(g, x, mean, rstd, weight)[0]
+    r = rstd.double()[:, None]
+    h = g.double().abs() if weight is None else (g.double() * weight.double()).abs()
+    u = (x.double() - mean.double()[:, None]).abs() * r
+    mean_h, mean_hu = h.sum(1, keepdim=True) / x.shape[1], (h * u).sum(1, keepdim=True) / x.shape[1]
+    close(got, dx, 1.01 * r * U * (4 * h + (5 + adds) * mean_h + (9 + adds) * u * mean_hu))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [70001, 2 ** 22 + 3])
+def test_layer_norm_sums_of_long_rows_lose_nothing(ops, cols, dtype):
+    """Bounds that do not grow with the columns: sums are in fp64, the mean is rounded once."""
+    g = gen(43)
+    x = torch.empty(4, cols, device="cuda")
+    x[0] = 0.1                                       # (no variance: its sum is exact in fp64)
+    x[1] = 1000 + 0.5 * randn(g, cols)
+    x[2] = torch.rand(cols, generator=g, device="cuda")
+    x[3] = randn(g, cols)
+    x = x.to(dtype)
+    y, mean, rstd = ops.layer_norm(x)
+    want_y, want_mean, want_rstd = norm64(x, None, None, 1e-5)
+    assert not y[0].any() and torch.equal(mean[0], x[0, 0].float())
+    off = (1.01 * U * want_mean.abs())               # of the mean: one rounding
+    close(mean, want_mean, 0.0)
+    # the deviations are rounded once, their squares' mean, eps, the root and the quotient (to an ulp, 2 u) as well
+    size = 10 * U + (off * want_rstd) ** 2
+    close(rstd, want_rstd, want_rstd * size)
+    close(y, want_y, want_rstd[:, None] * off[:, None] + want_y.abs() * (size + 3 * U)[:, None])
+    # gradients of one sign, whose sums over columns are as large as they can be
+    for grad in (torch.full((4, cols), 0.1, device="cuda"), torch.rand(4, cols, generator=g, device="cuda") * 0.3 + x.float().sign()):
+        grad = grad.to(dtype)
+        got = ops.layer_norm_backward(grad, x, mean, rstd)
+        check_norm_grad_columns(grad, x, mean, rstd, None, got[0], 1)
