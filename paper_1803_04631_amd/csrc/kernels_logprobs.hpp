@@ -206,6 +206,49 @@ struct LaneSums {
     }
 };
 
+// A lane's sums over all of its tiles.
+struct RowSums {
+    float m;
+    double s, u;
+};
+
+// The fp32 sums of a lane lose more the more terms have been added one after the other, so that after so many tiles (256 terms) they
+// go into sums in fp64.  Few rows have more, and a lane's registers decide how many rows a CU has: these sums are in LDS, each read and
+// written by its own thread only.
+template <class T> constexpr int kFoldTiles = 256 / (kTilePieces * kPack<T>);
+
+template <int kThreads>
+struct FoldLds {
+    double s[kThreads], u[kThreads];
+    float m[kThreads];
+};
+
+struct Fold {
+    double *s, *u;                                   // of this thread, in LDS
+    float* m;                                        // the bound they are relative to
+    bool empty = true;
+
+    template <int kThreads>
+    __device__ __forceinline__ explicit Fold(FoldLds<kThreads>& lds) : s(&lds.s[threadIdx.x]), u(&lds.u[threadIdx.x]), m(&lds.m[threadIdx.x]) {}
+    __device__ __forceinline__ Fold(double* s_at, double* u_at, float* m_at) : s(s_at), u(u_at), m(m_at) {}
+
+    // (a lane's bound only grows)
+    __device__ __forceinline__ RowSums with(const LaneSums& l) const {
+        if (empty) return RowSums{l.m, (double)l.s, (double)l.u};
+        const float d = fmaxf(*m - l.m, kVanished);
+        const double f = exp_of(d);
+        return RowSums{l.m, f * *s + (double)l.s, f * __builtin_fma((double)d, *s, *u) + (double)l.u};
+    }
+    __device__ __forceinline__ void take(LaneSums& l) {
+        const RowSums r = with(l);
+        *s = r.s;
+        *u = r.u;
+        *m = r.m;
+        l.s = l.u = 0.0f;
+        empty = false;
+    }
+};
+
 // The sums of all lanes of a wave, each relative to its own bound, as one, relative to the greatest.
 __device__ __forceinline__ void join_lanes(float& m, double& s, double& u) {
     const float most = wave_max(m), d = fmaxf(m - most, kVanished);
@@ -267,9 +310,10 @@ __device__ __forceinline__ float tile_max(const Raw (&now)[kTilePieces]) {
 
 // `seen(greatest logit of the tile)` is called for each tile of the wave.
 template <class T, bool kEntropy, class Seen>
-__device__ __forceinline__ LaneSums walk_row(const Span<T>& span, int wave, int waves, Seen&& seen) {
+__device__ __forceinline__ RowSums walk_row(const Span<T>& span, int wave, int waves, Fold folded, Seen&& seen) {
     constexpr int P = kPack<T>;
     LaneSums sums;
+    int tiles = 0;
     for_tiles(span, wave, waves, [&](const Raw (&now)[kTilePieces], int64_t) {
         const float most = tile_max<T>(now);
         seen(most);
@@ -281,8 +325,12 @@ __device__ __forceinline__ LaneSums walk_row(const Span<T>& span, int wave, int 
 #pragma unroll
             for (int e = 0; e < P; ++e) sums.add<kEntropy>(v[e]);
         }
+        if (++tiles == kFoldTiles<T>) {
+            folded.take(sums);
+            tiles = 0;
+        }
     });
-    return sums;
+    return folded.with(sums);
 }
 
 // The log-probability of a word of that logit: NaN for one outside the vocabulary, 0 for none.
@@ -418,7 +466,10 @@ struct TopLds {
     float stretch[kStretches][kLanes];            // each lane's greatest logit of each stretch
     float most[kLanes];                           // and of all
     uint64_t best[kHeld];                         // candidates, then the answer
-    uint64_t held[kWaves][kHeld];                 // of the waves, where every logit is looked at
+    union {
+        uint64_t held[kWaves][kHeld];             // of the waves, where every logit is looked at
+        double folded[kWaves][2][kWave];          // before that, with `most`: the lanes' sums so far
+    };
     int32_t chosen[kLanes];                       // lane and stretch
     int chosen_n, n, counts[kWaves];
 };
@@ -527,7 +578,7 @@ __device__ __forceinline__ int find_top(const Span<T>& span, float most, int n, 
 // 122 (3.9: instructions, and rows at odd addresses); one row of 102,000 bf16 in 25 segments 6.9 us, and 4.9 to join them.
 template <class T, bool kEntropy, bool kTop, int kWaves>
 __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) {
-    __shared__ std::conditional_t<kTop, TopLds<kWaves>, int> lds;
+    __shared__ std::conditional_t<kTop, TopLds<kWaves>, FoldLds<kWaves * kWave>> lds;
     __shared__ RowPart part[kWaves];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), lane = lane_id();
     const int64_t items = a.rows * a.segments;
@@ -536,12 +587,12 @@ __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) 
         const int32_t begin = (int32_t)(item % a.segments) * a.segment_cols;
         const int32_t end = min(a.vocab - begin, a.segment_cols) + begin;
         const Span<T> span{static_cast<const T*>(a.logits) + row * a.stride, begin, end};
-        LaneSums sums;
+        RowSums sums;
         if constexpr (kTop) {
             StretchMost<kWaves> seen{lds, stretch_tiles<T, kWaves>(span)};
-            sums = walk_row<T, kEntropy>(span, wave, kWaves, seen);
+            sums = walk_row<T, kEntropy>(span, wave, kWaves, Fold(&lds.folded[wave][0][lane], &lds.folded[wave][1][lane], &lds.most[threadIdx.x]), seen);
         } else {
-            sums = walk_row<T, kEntropy>(span, wave, kWaves, [](float) {});
+            sums = walk_row<T, kEntropy>(span, wave, kWaves, Fold(lds), [](float) {});
         }
         float m = sums.m;
         double s = sums.s, u = sums.u;
@@ -740,6 +791,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
     __shared__ RowPart part[kWaves];
     __shared__ double totals[kWaves];
     __shared__ float largest[kWaves];
+    __shared__ std::conditional_t<kLoss, FoldLds<kThreads>, int> folded;
     const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = lane_id();
     const int64_t items = a.rows * a.segments;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -806,12 +858,14 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
         const bool walked = kLoss && n > 0;        // (a row without words: nothing to read it for)
         float m = -INFINITY;
         double s = 0.0, u = 0.0;
-        if (walked) {
-            const LaneSums sums = walk_row<T, false>(Span<T>{logits, begin, end}, wave, kWaves, [](float) {});
-            m = sums.m;
-            s = sums.s;
-            join_lanes(m, s, u);
-            if (lane == 0) part[wave] = RowPart{s, u, m, 0};
+        if constexpr (kLoss) {
+            if (walked) {
+                const RowSums sums = walk_row<T, false>(Span<T>{logits, begin, end}, wave, kWaves, Fold(folded), [](float) {});
+                m = sums.m;
+                s = sums.s;
+                join_lanes(m, s, u);
+                if (lane == 0) part[wave] = RowPart{s, u, m, 0};
+            }
         }
         if (kLoss || !kSingle) __syncthreads();
         if (!kSingle) {

@@ -785,3 +785,33 @@ def test_layer_norm_sums_of_long_rows_lose_nothing(ops, cols, dtype):
         grad = grad.to(dtype)
         got = ops.layer_norm_backward(grad, x, mean, rstd)
         check_norm_grad_columns(grad, x, mean, rstd, None, got[0], 1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sums_over_millions_of_equal_words_lose_nothing(ops, dtype):
+    """Lanes that add up thousands of equal terms each, which no exact fp32 number is: the bound is of 256 additions in fp32, however long
+    the row."""
+    rows, vocab, most = 512, 2 ** 21 + 11, 8192
+    logits = torch.full((vocab,), -2.3, device="cuda", dtype=dtype)
+    logits[:most] = 0.0                              # (every lane's maximum is the row's)
+    low = float(logits[most])
+    s = most + (vocab - most) * math.exp(low)
+    log_s = math.log(s)
+    entropy = log_s - (vocab - most) * math.exp(low) * low / s
+    off = (256 + 4 + 3 * abs(low)) * U
+    logits = logits.expand(rows, vocab).contiguous()
+    tokens = torch.full((rows,), most + 5, device="cuda", dtype=torch.int32)
+    weights = torch.full((rows,), 3.0, device="cuda")
+
+    def all_close(got, want, bound):
+        close(got, torch.full_like(got, want, dtype=torch.float64), bound)
+
+    got = ops.token_logprobs(logits, tokens, entropy=True)
+    all_close(got.stats[:, 1], log_s, off + U * log_s)
+    all_close(got.logprobs, low - log_s, off + 2 * U * log_s)
+    all_close(got.entropy, entropy, off * (1 + abs(low)) + U * log_s)
+    fused, grad = ops.token_logprobs_grad(logits, tokens, weights, out=logits)
+    all_close(fused, low - log_s, off + 2 * U * log_s)
+    p = math.exp(low) / s
+    all_close(grad[:, most + 6:most + 9], -3.0 * p, 3.0 * p * (off + U * log_s + 12 * U))
+    all_close(grad[:, most + 5], 3.0 - 3.0 * p, 8 * U)
