@@ -119,7 +119,9 @@ __global__ __launch_bounds__(kClipThreads) void clip_kernel(ClipArgs a, const do
     const double n = norm_of(partial, partials, slots);
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     const bool scaled = n > most && n < INFINITY;
-    const float scale = scaled ? (float)(most / n) : 1.0f;
+    const double factor = scaled ? most / n : 1.0;
+    const float scale = (float)factor;
+    const bool tiny = factor < 0x1p-126;     // (where fp32 has fewer bits for it, or none, though the largest gradients times it are not that small)
     for_units<true>(a, [&](auto tag, int i, uint32_t unit) {
         typedef decltype(tag) T;
         constexpr int P = kPack<T>;
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(kClipThreads) void clip_kernel(ClipArgs a, const do
             float v[P];
             unpack(r, v, T());
 #pragma unroll
-            for (int e = 0; e < P; ++e) v[e] *= scale;
+            for (int e = 0; e < P; ++e) v[e] = tiny ? (float)((double)v[e] * factor) : v[e] * scale;
             return pack(v, T());
         };
         if (n == kClipUnit) {

@@ -815,3 +815,17 @@ def test_sums_over_millions_of_equal_words_lose_nothing(ops, dtype):
     p = math.exp(low) / s
     all_close(grad[:, most + 6:most + 9], -3.0 * p, 3.0 * p * (off + U * log_s + 12 * U))
     all_close(grad[:, most + 5], 3.0 - 3.0 * p, 8 * U)
+
+
+@pytest.mark.parametrize("max_norm", [1.0, 1e-3, 1e-8, 1e-20])
+def test_clip_by_factors_below_the_range_of_fp32(ops, max_norm):
+    """The norm is beyond fp32's range or close to its end: the factor has few bits in fp32, from 2^-150 on none, and what is scaled by it
+    is still a number."""
+    g = gen(51)
+    large = torch.full((8195,), 3e38, device="cuda") * (1 - 0.3 * torch.rand(8195, generator=g, device="cuda"))
+    for tensors in ([large], [large, large[:1000].bfloat16(), 1e30 * randn(g, 9000), randn(g, 77, dtype=torch.float16)]):
+        check_clip(ops, [t.clone() for t in tensors], max_norm)
+    out = [torch.empty_like(large)]
+    ops.clip_grads([large], max_norm, out=out)
+    # of 8,195 numbers of between 2.1e38 and 3e38 none is less than 0.7 of the largest, and their norm is max_norm
+    assert float(out[0].min()) > 0.7 * max_norm / math.sqrt(8195)
