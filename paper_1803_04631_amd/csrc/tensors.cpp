@@ -103,6 +103,15 @@ Tensor out_for(const Maybe& out, const Tensor& like, const Rows& rows, Rows& r) 
     return t;
 }
 
+// Tells torch that a tensor of the caller's has been written, as its own operations in place do: a backward pass that has saved it can
+// see that.  (Tensors of inference mode have no versions.)
+void written(const Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void written(const Maybe& out) {
+    if (out) written(*out);
+}
+
 struct Workspace {
     Tensor held;
     void* at = nullptr;
@@ -140,6 +149,7 @@ std::tuple<Tensor, Tensor, Tensor> layer_norm(const Tensor& x, const Maybe& weig
     const c10::DeviceGuard guard(r.device);
     check(mlda_layer_norm(r.at, r.stride, c.weight, c.bias, ry.at, ry.stride, mean.data_ptr<float>(), rstd.data_ptr<float>(), r.rows, r.cols,
                           eps, r.kind, c.kind, stream_of(r.device)));
+    written(out);
     return {y, mean, rstd};
 }
 
@@ -159,6 +169,7 @@ std::tuple<Tensor, Tensor, Tensor> layer_norm_backward(const Tensor& grad_y, con
     const c10::DeviceGuard guard(r.device);
     check(mlda_layer_norm_backward(rg.at, rg.stride, r.at, r.stride, (const float*)at_mean, (const float*)at_rstd, c.weight, rx.at, rx.stride,
                                    grad_weight.data_ptr(), grad_bias.data_ptr(), r.rows, r.cols, r.kind, c.kind, w.at, w.bytes, stream_of(r.device)));
+    written(out);
     return {grad_x, grad_weight, grad_bias};
 }
 
@@ -219,6 +230,7 @@ Tensor token_logprobs_backward(const Tensor& grad_logprobs, const Tensor& logits
     const c10::DeviceGuard guard(r.device);
     check(mlda_token_logprobs_backward(r.at, r.stride, r.rows, r.cols, r.kind, d.tokens, d.row_ptr, d.n, (const float*)at_stats, (const float*)at_grad,
                                        (const float*)at_entropy, (const float*)at_h, ro.at, ro.stride, stream_of(r.device)));
+    written(out);
     return grad;
 }
 
@@ -233,6 +245,7 @@ std::tuple<Tensor, Tensor> token_logprobs_grad(const Tensor& logits, const Tenso
     const c10::DeviceGuard guard(r.device);
     check(mlda_token_logprobs_grad(r.at, r.stride, r.rows, r.cols, r.kind, d.tokens, d.row_ptr, d.n, (const float*)at_weights,
                                    logprobs.data_ptr<float>(), ro.at, ro.stride, w.at, w.bytes, stream_of(r.device)));
+    written(out);
     return {logprobs, grad};
 }
 
@@ -266,10 +279,12 @@ Tensor clip_grads(const std::vector<Tensor>& tensors, std::optional<double> most
     check(mlda_grad_norm_workspace_bytes((int32_t)n, &bytes));
     const Workspace w(bytes, device);
     const c10::DeviceGuard guard(device);
-    if (most)
+    if (most) {
         check(mlda_clip_grads(in.data(), to.data(), sizes.data(), types.data(), (int32_t)n, *most, norm.data_ptr<float>(), w.at, w.bytes, stream_of(device)));
-    else
+        for (const Tensor& t : out ? *out : tensors) written(t);
+    } else {
         check(mlda_grad_norm(in.data(), sizes.data(), types.data(), (int32_t)n, norm.data_ptr<float>(), w.at, w.bytes, stream_of(device)));
+    }
     return norm;
 }
 

@@ -6,8 +6,8 @@ Argument marshalling only, like the rest of the binding (here compiled, csrc/ten
 small calls): everything is computed by the library's HIP kernels (include/mlda.h says what exactly),
 on torch's current stream of the tensors' device, without synchronising it.  Outputs and workspaces come
 from torch's allocator.  Tensors are fp32, bf16 or fp16; results are sums in fp32 or fp64 that are rounded
-once.  Nothing is recorded for torch's differentiation: the backward passes are calls of their own.  An
-argument that a function does not take raises ValueError before anything is launched.
+once.  Nothing is recorded for torch's differentiation: the backward passes are calls of their own; a tensor
+that is written in place has a new version, so that torch notices where it had saved it.  An argument that a function does not take raises ValueError before anything is launched.
 
 Inputs that other streams work on are the caller's to order, as with torch's own operations.
 """

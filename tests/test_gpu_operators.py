@@ -829,3 +829,45 @@ def test_clip_by_factors_below_the_range_of_fp32(ops, max_norm):
     ops.clip_grads([large], max_norm, out=out)
     # of 8,195 numbers of between 2.1e38 and 3e38 none is less than 0.7 of the largest, and their norm is max_norm
     assert float(out[0].min()) > 0.7 * max_norm / math.sqrt(8195)
+
+
+def test_tensors_written_in_place_have_a_new_version(ops):
+    """torch's check of tensors that it has saved for another backward pass works as with its own operations in place."""
+    g = gen(61)
+    x, grad, weight = randn(g, 5, 300), randn(g, 5, 300), randn(g, 300)
+    tokens, weights = torch.zeros(5, dtype=torch.int32, device="cuda"), randn(g, 5)
+    _, mean, rstd = ops.layer_norm(x, weight)
+    stats = ops.token_logprobs(x, tokens).stats
+    inputs = [x, grad, weight, tokens, weights, mean, rstd, stats]
+
+    def writes(call, *outs):
+        before = [t._version for t in (*inputs, *outs)]
+        call()
+        after = [t._version for t in (*inputs, *outs)]
+        wanted = [b + any(t is o for o in outs) for b, t in zip(before, (*inputs, *outs))]
+        assert after == wanted
+
+    def new():
+        return torch.empty_like(x)
+
+    for out in (new(), x.clone()):
+        writes(lambda: ops.layer_norm(x, weight, out=out), out)
+        writes(lambda: ops.layer_norm_backward(grad, x, mean, rstd, weight, out=out), out)
+        writes(lambda: ops.token_logprobs_backward(weights, x, tokens, stats, out=out), out)
+        writes(lambda: ops.token_logprobs_grad(x, tokens, weights, out=out), out)
+        writes(lambda: ops.clip_grads([x], 0.1, out=[out]), out)
+        writes(lambda: ops.clip_grads([out, mean], 0.1), out, mean)
+    writes(lambda: ops.layer_norm(x, weight))
+    writes(lambda: ops.grad_norm([x, grad]))
+    writes(lambda: ops.layer_norm(x, weight, out=x), x)
+    writes(lambda: ops.token_logprobs_grad(x, tokens, weights, out=x), x)
+    for write in (lambda y: ops.layer_norm(y, out=y), lambda y: ops.clip_grads([y], 1e-3), lambda y: ops.token_logprobs_grad(y, tokens, weights, out=y)):
+        leaf = randn(g, 5, 300).requires_grad_()
+        y = leaf.exp()                               # (whose derivative is y)
+        write(y)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+    with torch.inference_mode():
+        y = randn(g, 5, 300)
+        ops.layer_norm(y, out=y)
+        ops.clip_grads([y], 0.1)
