@@ -311,7 +311,9 @@ PYBIND11_MODULE(_tensors, m) {
         return token_logprobs_grad(tensor(logits, "logits"), tensor(tokens, "tokens"), tensor(weights, "weights"), maybe(row_ptr, "row_ptr"),
                                    maybe(out, "out"));
     });
+    m.def("grad_norm", [](H tensors) { return clip_grads(tensors_of(tensors, "every one of tensors"), std::nullopt, std::nullopt); });
     m.def("clip_grads", [](H tensors, std::optional<double> most, H out) {
+        TORCH_CHECK_VALUE(most, "max_norm must be a number: grad_norm gives the norm alone");
         return clip_grads(tensors_of(tensors, "every one of tensors"), most,
                           out.is_none() ? std::nullopt : std::optional<std::vector<Tensor>>(tensors_of(out, "every one of out")));
     });

@@ -7,7 +7,10 @@ small calls): everything is computed by the library's HIP kernels (include/mlda.
 on torch's current stream of the tensors' device, without synchronising it.  Outputs and workspaces come
 from torch's allocator.  Tensors are fp32, bf16 or fp16; results are sums in fp32 or fp64 that are rounded
 once.  Nothing is recorded for torch's differentiation: the backward passes are calls of their own; a tensor
-that is written in place has a new version, so that torch notices where it had saved it.  An argument that a function does not take raises ValueError before anything is launched.
+that is written in place has a new version, so that torch notices where it had saved it.  A tensor
+that a function does not take raises ValueError, a number that the library refuses (a negative eps, say)
+MldaError, both before anything is launched.  What is written (`out`) is in an input's place where that is
+said, or overlaps no input and no other output; a tensor that is clipped is listed once.
 
 Inputs that other streams work on are the caller's to order, as with torch's own operations.
 """
@@ -71,7 +74,7 @@ def token_logprobs_grad(logits, tokens, weights, row_ptr=None, out=None):
 def grad_norm(tensors):
     """The norm over all tensors of a gradient: the square root of the sum of all squares, as a scalar
     tensor."""
-    return _tensors.clip_grads(tensors, None, None)
+    return _tensors.grad_norm(tensors)
 
 
 def clip_grads(tensors, max_norm: float, out=None):

@@ -871,3 +871,12 @@ def test_tensors_written_in_place_have_a_new_version(ops):
         y = randn(g, 5, 300)
         ops.layer_norm(y, out=y)
         ops.clip_grads([y], 0.1)
+
+
+def test_clipping_wants_a_norm(ops):
+    t = torch.full((10,), 3.0, device="cuda")
+    out = [torch.zeros(10, device="cuda")]
+    for call in (lambda: ops.clip_grads([t], None), lambda: ops.clip_grads([t], None, out=out)):
+        with pytest.raises(ValueError, match="max_norm"):
+            call()
+    assert (t == 3.0).all() and not out[0].any()
