@@ -182,8 +182,25 @@ struct Candidates {
 };
 
 // ---------------------------------------------------------------- one pass over a row, or a segment
-// exp2 of a product that is at most zero: a product of the type's lowest values may overflow to minus infinity, which is meant.
-__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2E); }
+// x - m for a bound m of x, and its exponential.  The product t = d log2(e) alone, rounded, would leave an exponential with |d| units of
+// roundoff: w = d - t ln(2) is what it leaves out, and 2^t + 2^t w is within three units at any distance (2,400 x 102,000 fp32 186 us, so
+// 181 without).  Logits of 16 bits have 2^-9 or 2^-12 of themselves for an error, and their kernels are held up by instructions: there the
+// product is taken as it is (1,024 x 102,000 bf16 40 us, with w 50; 6,007 x 40,009 with the 20 likeliest words 131, with w 142).
+constexpr float kLn2 = 0.693147182464599609375f, kLn2Low = -1.904654299957768e-9f;      // ln(2) as fp32 has it, and the rest
+template <class T>
+constexpr bool kExact = sizeof(T) == 4;
+
+template <class T>
+__device__ __forceinline__ float below(float x, float m) {
+    if constexpr (kExact<T>) return __builtin_elementwise_maximum(x - m, kVanished);     // (NaN stays NaN; t - t is none at infinity)
+    return x - m;
+}
+template <class T>
+__device__ __forceinline__ float exp_of(float d) {
+    const float t = d * kLog2E, e = __builtin_amdgcn_exp2f(t);       // (a product may overflow to minus infinity, which is meant)
+    if constexpr (!kExact<T>) return e;
+    return __builtin_fmaf(e, __builtin_fmaf(-t, kLn2Low, __builtin_fmaf(-t, kLn2, d)), e);
+}
 
 struct LaneSums {
     float m = kLowest;        // (a finite bound: minus infinity minus it is minus infinity, whose exponential is 0)
@@ -191,16 +208,16 @@ struct LaneSums {
 
     __device__ __forceinline__ void raise(float to) {
         if (to > m) {
-            const float d = fmaxf(m - to, kVanished);
-            const float f = exp_of(d);
+            const float d = below<float>(m, to);
+            const float f = exp_of<float>(d);
             u = f * __builtin_fmaf(d, s, u);
             s *= f;
             m = to;
         }
     }
-    template <bool kEntropy>
+    template <class T, bool kEntropy>
     __device__ __forceinline__ void add(float x) {
-        const float d = x - m, e = exp_of(d);
+        const float d = below<T>(x, m), e = exp_of<T>(d);
         s += e;
         if constexpr (kEntropy) u = __builtin_fmaf(e, fmaxf(d, kVanished), u);
     }
@@ -235,8 +252,8 @@ struct Fold {
     // (a lane's bound only grows)
     __device__ __forceinline__ RowSums with(const LaneSums& l) const {
         if (empty) return RowSums{l.m, (double)l.s, (double)l.u};
-        const float d = fmaxf(*m - l.m, kVanished);
-        const double f = exp_of(d);
+        const float d = below<float>(*m, l.m);
+        const double f = exp_of<float>(d);
         return RowSums{l.m, f * *s + (double)l.s, f * __builtin_fma((double)d, *s, *u) + (double)l.u};
     }
     __device__ __forceinline__ void take(LaneSums& l) {
@@ -251,8 +268,8 @@ struct Fold {
 
 // The sums of all lanes of a wave, each relative to its own bound, as one, relative to the greatest.
 __device__ __forceinline__ void join_lanes(float& m, double& s, double& u) {
-    const float most = wave_max(m), d = fmaxf(m - most, kVanished);
-    const double f = s != 0.0 ? (double)exp_of(d) : 0.0;
+    const float most = wave_max(m), d = below<float>(m, most);
+    const double f = s != 0.0 ? (double)exp_of<float>(d) : 0.0;
     u = wave_sum(f != 0.0 ? f * (u + (double)d * s) : 0.0);
     s = wave_sum(f * s);
     m = most;
@@ -323,7 +340,7 @@ __device__ __forceinline__ RowSums walk_row(const Span<T>& span, int wave, int w
             float v[P];
             unpack(now[j], v, T());
 #pragma unroll
-            for (int e = 0; e < P; ++e) sums.add<kEntropy>(v[e]);
+            for (int e = 0; e < P; ++e) sums.add<T, kEntropy>(v[e]);
         }
         if (++tiles == kFoldTiles<T>) {
             folded.take(sums);
@@ -755,9 +772,9 @@ struct RowGrad {
     float m, log_s, inv_s;       // of the row
     float total, h, entropy;     // G, gradient of the entropy, entropy
     // of one logit, without its own words' gradients
-    template <bool kEntropy>
+    template <class T, bool kEntropy>
     __device__ __forceinline__ float of(float x) const {
-        const float d = x - m, p = exp_of(d) * inv_s;
+        const float d = below<T>(x, m), p = exp_of<T>(d) * inv_s;
         if constexpr (kEntropy) return -p * (total + h * (fmaxf(d, kVanished) - log_s + entropy));
         return -p * total;
     }
@@ -776,7 +793,7 @@ __device__ __forceinline__ void stream_grad(const T* row, T* out, int32_t begin,
         float v[P];
         unpack(load_piece(row - shift, c, lo, hi, -INFINITY, kLoss && once), v, T());
 #pragma unroll
-        for (int e = 0; e < P; ++e) v[e] = g.template of<kEntropy>(v[e]);
+        for (int e = 0; e < P; ++e) v[e] = g.template of<T, kEntropy>(v[e]);
         own(v, (int32_t)(c - shift));
         store_piece(out - shift, c, lo, hi, pack(v, T()), once);
     }
@@ -943,7 +960,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
                 __syncthreads();
 #pragma unroll
                 for (int k = 0; k < kWordBatch; ++k)
-                    if (slot[k] >= 0) xs[k] = value(table.sums[slot[k]]) + g.template of<kEntropy>(xs[k]);
+                    if (slot[k] >= 0) xs[k] = value(table.sums[slot[k]]) + g.template of<T, kEntropy>(xs[k]);
                 stream_grad<T, kThreads, kLoss, kEntropy>(logits, out, begin, end, g, a.once, [](float (&)[P], int32_t) {});
                 __syncthreads();
 #pragma unroll
@@ -957,7 +974,7 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
                 // the words' columns are worked out before the row is written over, and written last
                 for (int i = tid; i < table.slots; i += kThreads) {
                     const int32_t w = table.words[i];
-                    if (w >= 0) table.sums[i] = (unsigned long long)__float_as_uint(value(table.sums[i]) + g.template of<kEntropy>((float)logits[w]));
+                    if (w >= 0) table.sums[i] = (unsigned long long)__float_as_uint(value(table.sums[i]) + g.template of<T, kEntropy>((float)logits[w]));
                 }
                 __syncthreads();
                 stream_grad<T, kThreads, kLoss, kEntropy>(logits, out, begin, end, g, a.once, [](float (&)[P], int32_t) {});

@@ -880,3 +880,18 @@ def test_clipping_wants_a_norm(ops):
         with pytest.raises(ValueError, match="max_norm"):
             call()
     assert (t == 3.0).all() and not out[0].any()
+
+
+@pytest.mark.parametrize("rows", [2, 600])
+def test_probabilities_far_below_the_greatest_are_exact(ops, rows):
+    """Where the difference to the greatest logit is a number of fp32, so is its exponential: three units of roundoff and those of
+    the products, whatever the distance.  (A row's common factor is that of a word with the greatest logit.)"""
+    vocab = 6001
+    x = -80 * torch.rand(rows, vocab, generator=gen(71), device="cuda")
+    x[:, :2] = 0.0
+    tokens, weights = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.ones(rows, device="cuda")
+    got = ops.token_logprobs(x, tokens, entropy=True)
+    for grad in (ops.token_logprobs_grad(x, tokens, weights)[1], ops.token_logprobs_backward(weights, x, tokens, got.stats)):
+        ratio = grad[:, 2:].double() / grad[:, 1:2].double()
+        want = torch.exp(x[:, 2:].double())
+        assert ((ratio / want - 1).abs().max() <= 6 * U).item(), ((ratio / want - 1).abs().max() / U).item()
