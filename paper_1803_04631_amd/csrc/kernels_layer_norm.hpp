@@ -234,10 +234,11 @@ __device__ __forceinline__ void grad_piece(Raw x, Raw g, const Columns<W, kPack<
     }
 }
 
-// kSums: the weight's and bias' gradients are summed here.  kHeld: the weight is kept, and the next row's pieces are loaded ahead.
+// kSums: the weight's and bias' gradients are summed here, and the weight is kept.  kAhead: the next row's pieces are loaded ahead.
 // 300,000 x 1,000 bf16 374 us (4.8 TB/s), fp32 712 (5.1); 30,011 x 1,537 bf16, rows at odd addresses, 59 us (4.7); 8,009 x 10,000 fp32, whose
-// sums take a third of the registers, 255 (3.8).
-template <class T, class W, int kTeam, int kPieces, bool kSums, bool kHeld = kSums>
+// sums and weights take three eighths of the registers, 210 (4.6).  Four waves a SIMD are worth more than the few registers of a lane that 16-bit
+// rows with fp32 weights keep in memory for it (5 to 11 of 128): 30,011 x 1,537 66 us, with three waves and none 77; 300,000 x 1,000 339 and 389.
+template <class T, class W, int kTeam, int kPieces, bool kSums, bool kAhead = kSums>
 __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ? 4 : 1) void layer_norm_grad_kernel(LayerNormGradArgs a) {
     constexpr int P = kPack<T>, kThreads = team_threads(kTeam), kTeams = kThreads / kTeam;
     __shared__ float slots[2][2 * (kThreads / kWave)];
@@ -246,13 +247,11 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
     const int lane = (int)threadIdx.x % kTeam;
     const int32_t cols = a.cols;
     const float n_cols = (float)cols;
-    Columns<W, P> w[kHeld ? kPieces : 1];
+    Columns<W, P> w[kSums ? kPieces : 1];
     float dw[kSums ? kPieces * P : 1], db[kSums ? kPieces * P : 1];
-    if constexpr (kHeld) {
+    if constexpr (kSums) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) w[j].load(a.weight, (j * kTeam + lane) * P, cols, 1.0f);
-    }
-    if constexpr (kSums) {
 #pragma unroll
         for (int k = 0; k < kPieces * P; ++k) dw[k] = db[k] = 0.0f;
     }
@@ -276,9 +275,9 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
         to_mean = there ? a.mean[r] : 0.0f;
         to_rstd = there ? a.rstd[r] : 0.0f;
     };
-    if (kHeld) load_row(row, next_x, next_g, next_mean, next_rstd);
+    if (kAhead) load_row(row, next_x, next_g, next_mean, next_rstd);
     for (int64_t i = 0; i < rounds; ++i, row += step) {
-        if constexpr (kHeld) {
+        if constexpr (kAhead) {
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
                 x[j] = next_x[j];
@@ -291,14 +290,14 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
             load_row(row, x, g, mean, rstd);
         }
         const void* weight = a.weight;             // (as in layer_norm_kernel)
-        if constexpr (!kHeld && !kSums) asm volatile("" : "+s"(weight));
+        if constexpr (!kSums) asm volatile("" : "+s"(weight));
         float sum_h = 0.0f, sum_hu = 0.0f;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             float u[P], h[P], grad[P];
-            if constexpr (!kHeld) w[0].load(weight, (j * kTeam + lane) * P, cols, 1.0f);
-            forget(w[kHeld ? j : 0].raw);
-            grad_piece<T, W>(x[j], g[j], w[kHeld ? j : 0], mean, rstd, u, h, grad);
+            if constexpr (!kSums) w[0].load(weight, (j * kTeam + lane) * P, cols, 1.0f);
+            forget(w[kSums ? j : 0].raw);
+            grad_piece<T, W>(x[j], g[j], w[kSums ? j : 0], mean, rstd, u, h, grad);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
                 sum_h += h[e];
@@ -314,9 +313,9 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
         for (int j = 0; j < kPieces; ++j) {
             const int32_t c = (j * kTeam + lane) * P;
             float u[P], h[P], v[P];
-            if constexpr (!kHeld) w[0].load(weight, c, cols, 1.0f);
-            forget(w[kHeld ? j : 0].raw);
-            grad_piece<T, W>(x[j], g[j], w[kHeld ? j : 0], mean, rstd, u, h, v);
+            if constexpr (!kSums) w[0].load(weight, c, cols, 1.0f);
+            forget(w[kSums ? j : 0].raw);
+            grad_piece<T, W>(x[j], g[j], w[kSums ? j : 0], mean, rstd, u, h, v);
             if constexpr (kSums) {                 // (not beside the sums above: what that needs would be kept until here)
 #pragma unroll
                 for (int e = 0; e < P; ++e) {
@@ -326,7 +325,12 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
             }
 #pragma unroll
             for (int e = 0; e < P; ++e) v[e] = rstd * ((h[e] - mean_h) - u[e] * mean_hu);
-            if (dx) store_piece(dx, c, 0, cols, pack(v, T()), a.once);
+            // (a team that its sums fill has no registers for two kinds of stores: 8,009 x 10,000 fp32 210 us, with both 223)
+            if constexpr (kSums && !kAhead) {
+                if (dx) store_some(dx + c, pack(v, T()), min(max(cols - c, 0), P));
+            } else {
+                if (dx) store_piece(dx, c, 0, cols, pack(v, T()), a.once);
+            }
         }
     }
     if constexpr (kSums) {

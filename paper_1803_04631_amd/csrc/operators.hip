@@ -96,7 +96,7 @@ void with_team(int64_t row_bytes, F&& f) {
     else f(Team<1024, 8>());
 }
 constexpr int64_t kHeldBytes = 131072;            // of a row that a team holds
-// of one beside whose gradient there is room for the weight's (two sums a column; 8,009 x 10,000 fp32 with the sums on their own 333 us, so 255)
+// of one beside whose gradient there is room for the weight's (two sums a column; 8,009 x 10,000 fp32 with the sums on their own 333 us, so 210)
 constexpr int64_t summed_bytes(int64_t type_bytes) { return type_bytes == 4 ? 65536 : 32768; }
 
 // The same for the gradient, where a column takes four times the registers; f(team, workgroups that fit a CU).
@@ -332,7 +332,8 @@ int mlda_layer_norm(const void* x, int64_t x_stride, const void* weight, const v
         } else {
             with_team(bytes, [&](auto t) {
                 constexpr int kThreads = mlda::team_threads(t.team), kTeams = kThreads / t.team;
-                constexpr bool kHeld = t.pieces * t.team < 8192;
+                // (3,001 x 30,000 bf16 with fp32 weights, which fill the registers, 74 us, held 77)
+                constexpr bool kHeld = t.pieces * t.team < (sizeof(W) > sizeof(T) ? 4096 : 8192);
                 const int64_t groups = std::min<int64_t>((rows + kTeams - 1) / kTeams, kThreads == 256 ? 8 * kCus : 2 * kCus);
                 hipLaunchKernelGGL((mlda::layer_norm_kernel<T, W, t.team, t.pieces, kHeld>), dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
             });
