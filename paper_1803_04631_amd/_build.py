@@ -2,8 +2,11 @@
 on torch tensors, with the host compiler."""
 from __future__ import annotations
 
+import importlib.util
 import os
+import shutil
 import subprocess
+import sys
 import sysconfig
 import tempfile
 
@@ -23,11 +26,25 @@ HIPCC_FLAGS = [
 ]
 
 
+def _tensors_lack() -> str | None:
+    """What _tensors.so cannot be built without and is not there: the host compiler, or torch's or Python's headers."""
+    compiler = os.environ.get("CXX", "g++")
+    if shutil.which(compiler) is None:
+        return f"no host compiler ({compiler})"
+    if importlib.util.find_spec("torch") is None:
+        return "no torch"
+    import torch
+    for header in (os.path.join(os.path.dirname(torch.__file__), "include", "ATen", "ATen.h"), os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        if not os.path.exists(header):
+            return f"no {header}"
+    return None
+
+
 def _tensors_command(rocm: str) -> list[str]:
     """_tensors.so against torch's headers and libraries, and libmlda.so beside it."""
     import torch
     at = os.path.dirname(torch.__file__)
-    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
             "-DTORCH_API_INCLUDE_EXTENSION_H", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
             "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
             "-isystem", os.path.join(rocm, "include"), "-isystem", sysconfig.get_paths()["include"],
@@ -36,7 +53,8 @@ def _tensors_command(rocm: str) -> list[str]:
 
 
 def build(verbose: bool = False) -> str:
-    """Always compiles, the sources side by side; returns the library path."""
+    """Always compiles, the sources side by side; returns the library path.  The sampler needs libmlda.so alone: where there is nothing to
+    build _tensors.so with, that is said, and the operators raise ImportError."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
     def run(cmds):
@@ -56,5 +74,11 @@ def build(verbose: bool = False) -> str:
         compiled = [flag for flag in HIPCC_FLAGS if flag != "-shared"]
         run([hipcc, *compiled, "-c", "-o", o, os.path.join(CSRC, source)] for o, source in zip(linked, SOURCES))
         run([[hipcc, "--offload-arch=gfx950", "-shared", "-Wl,-soname,libmlda.so", "-o", LIB_PATH, *linked, "-lpthread"]])
-    run([_tensors_command(os.environ.get("ROCM_PATH", "/opt/rocm"))])
+    if os.path.exists(TENSORS_PATH):
+        os.remove(TENSORS_PATH)                      # (calls into the library as it was before)
+    lack = _tensors_lack()
+    if lack:
+        print(f"{TENSORS_PATH} is not built, and the operators on tensors are not there: {lack}", file=sys.stderr, flush=True)
+    else:
+        run([_tensors_command(os.environ.get("ROCM_PATH", "/opt/rocm"))])
     return LIB_PATH

@@ -16,13 +16,17 @@ Inputs that other streams work on are the caller's to order, as with torch's own
 """
 from __future__ import annotations
 
+import os
 from typing import NamedTuple, Optional
 
 import torch
 
 from . import load_library
+from ._build import TENSORS_PATH
 
 load_library()                      # (raises where the library has not been built)
+if not os.path.exists(TENSORS_PATH):
+    raise ImportError(f"{TENSORS_PATH} is missing: build with a host compiler and torch's headers at hand (paper_1803_04631_amd.build())")
 from . import _tensors              # noqa: E402
 
 MAX_ALTERNATIVES = 32               # MLDA_MAX_ALTERNATIVES

@@ -143,3 +143,21 @@ def test_the_binding_wants_tensors_on_a_gpu():
                  lambda: operators.grad_norm([x]), lambda: operators.clip_grads([x], 1.0), lambda: operators.layer_norm(None), lambda: operators.clip_grads([], 1.0)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_the_library_is_built_where_the_calls_on_tensors_cannot_be(tmp_path, monkeypatch, capsys):
+    """The sampler's build needs hipcc alone, as before there were operators on tensors."""
+    from paper_1803_04631_amd import _build
+    stub = tmp_path / "hipcc"                        # writes its output and nothing else
+    stub.write_text('#!/bin/sh\nwhile [ $# -gt 0 ]; do if [ "$1" = -o ]; then echo built > "$2"; fi; shift; done\n')
+    stub.chmod(0o755)
+    stale = tmp_path / "_tensors.so"
+    stale.write_text("of another library")
+    monkeypatch.setattr(_build, "LIB_PATH", str(tmp_path / "libmlda.so"))
+    monkeypatch.setattr(_build, "TENSORS_PATH", str(stale))
+    monkeypatch.setenv("HIPCC", str(stub))
+    monkeypatch.setenv("CXX", str(tmp_path / "no-such-compiler"))
+    monkeypatch.setattr(_build, "_HERE", str(tmp_path))
+    assert _build.build() == str(tmp_path / "libmlda.so")
+    assert (tmp_path / "libmlda.so").read_text() == "built\n" and not stale.exists()
+    assert "no-such-compiler" in capsys.readouterr().err
