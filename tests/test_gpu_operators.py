@@ -895,3 +895,131 @@ def test_probabilities_far_below_the_greatest_are_exact(ops, rows):
         ratio = grad[:, 2:].double() / grad[:, 1:2].double()
         want = torch.exp(x[:, 2:].double())
         assert ((ratio / want - 1).abs().max() <= 6 * U).item(), ((ratio / want - 1).abs().max() / U).item()
+
+
+# ------------------------------------------------------------------------------------------ more than the caches hold, and other forms of full size
+@pytest.mark.parametrize("rows,cols,dtype", [(33001, 1537, torch.bfloat16), (33001, 1537, torch.float16), (25001, 1003, torch.float32), (6007, 9001, torch.float32),
+                                             (3001, 20001, torch.bfloat16), (700, 45001, torch.float32), (1100, 50001, torch.bfloat16), (500, 70001, torch.float16)])
+def test_layer_norm_of_more_than_the_caches_hold(ops, rows, cols, dtype):
+    """What a call that moves more than 192 MB writes goes past the caches, by other instructions: odd rows, all forms, in place too."""
+    g = gen(rows + cols)
+    x = (randn(g, rows, cols) * 1.5 + randn(g, rows, 1)).to(dtype)
+    grad = randn(g, rows, cols, dtype=dtype)
+    assert 2 * x.numel() * x.element_size() > 192e6 or 3 * x.numel() * x.element_size() > 192e6
+    for kind in {dtype, torch.float32}:
+        weight, bias = (1 + 0.3 * randn(g, cols)).to(kind), randn(g, cols, dtype=kind)
+        got = ops.layer_norm(x, weight, bias)
+        check_norm(x, weight, bias, 1e-5, got)
+        held = x.clone()
+        assert torch.equal(ops.layer_norm(held, weight, bias, out=held)[0], got[0])
+        grads = ops.layer_norm_backward(grad, x, got[1], got[2], weight)
+        check_norm_grad(grad, x, got[1], got[2], weight, grads)
+        # a lane adds up 64 columns at the most, the lanes and waves join in ten steps and 16 additions; sums in fp64 are within that, too
+        check_norm_grad_columns(grad, x, got[1], got[2], weight, grads[0], 64 + 10 + 16)
+        for held, args in ((x.clone(), lambda t: (grad, t)), (grad.clone(), lambda t: (t, x))):
+            again = ops.layer_norm_backward(*args(held), got[1], got[2], weight, out=held)
+            assert all(torch.equal(a, b) for a, b in zip(again, grads))
+
+
+@pytest.mark.parametrize("rows,vocab,total,dtype", [(701, 70001, 9000, torch.bfloat16), (701, 70001, None, torch.float16), (523, 50021, 20000, torch.float32),
+                                                    (523, 50021, None, torch.float32), (60, 420001, 3000, torch.float32), (9001, 5501, 90000, torch.bfloat16),
+                                                    (2003, 25003, None, torch.bfloat16)])
+def test_logprobs_gradients_of_more_than_the_caches_hold(ops, rows, vocab, total, dtype):
+    g = gen(rows + vocab)
+    logits = (2 * randn(g, rows, vocab)).to(dtype)
+    assert 2 * logits.numel() * logits.element_size() > 192e6
+    if total is None:
+        row_ptr, tokens = None, torch.randint(vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    else:
+        row_ptr, tokens = documents(g, rows, vocab, total)
+    weights, h = randn(g, len(tokens)), randn(g, rows)
+    got, want = check_logprobs(ops, logits, tokens, row_ptr, 0)
+    plain = ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr)
+    close(plain, *want.grad(weights))
+    both = ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr, grad_entropy=h, entropy=got.entropy)
+    close(both, *want.grad(weights, h))
+    logprobs, fused = ops.token_logprobs_grad(logits, tokens, weights, row_ptr)
+    close(logprobs, want.logprobs, want.off_logp[want.row, want.tokens])
+    close(fused, *want.grad(weights))
+    del want
+    for expected, call in ((plain, lambda t: ops.token_logprobs_backward(weights, t, tokens, got.stats, row_ptr, out=t)),
+                           (both, lambda t: ops.token_logprobs_backward(weights, t, tokens, got.stats, row_ptr, grad_entropy=h, entropy=got.entropy, out=t)),
+                           (fused, lambda t: ops.token_logprobs_grad(t, tokens, weights, row_ptr, out=t)[1])):
+        held = logits.clone()
+        assert call(held) is held and torch.equal(held, expected)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_logprobs_gradients_of_the_largest_table(ops, dtype):
+    """Documents of about a thousand words over more columns than sums by column have room for: 8,192 slots, 96 KB of LDS.  Some fill it to
+    the last word that it takes, some have one more, and are done by ranges of columns."""
+    g = gen(81)
+    rows, vocab = 520, 15001
+    lengths = torch.randint(700, 1300, (rows,), generator=g, device="cuda")
+    lengths[:8] = torch.tensor([7168, 7169, 8000, 2048, 2049, 0, 1, 20000], device="cuda")
+    row_ptr = torch.cat([lengths.new_zeros(1), lengths.cumsum(0)])
+    total = int(row_ptr[-1])
+    assert total / rows > 512
+    tokens = torch.randint(vocab, (total,), generator=g, device="cuda", dtype=torch.int32)
+    tokens[:7168] = torch.randperm(vocab, generator=g, device="cuda")[:7168].int()       # (all different: as many slots)
+    logits, weights, h = (2 * randn(g, rows, vocab)).to(dtype), randn(g, total), randn(g, rows)
+    got, want = check_logprobs(ops, logits, tokens, row_ptr, 0)
+    close(ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr, grad_entropy=h, entropy=got.entropy), *want.grad(weights, h))
+    plain = ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr)
+    close(plain, *want.grad(weights))
+    assert torch.equal(plain, ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr))
+    logprobs, grad = ops.token_logprobs_grad(logits, tokens, weights, row_ptr)
+    close(logprobs, want.logprobs, want.off_logp[want.row, want.tokens])
+    close(grad, *want.grad(weights))
+    held = logits.clone()
+    assert torch.equal(ops.token_logprobs_grad(held, tokens, weights, row_ptr, out=held)[1], grad)
+
+
+@pytest.mark.parametrize("vocab,dtype", [(1025, torch.float32), (3001, torch.bfloat16), (9001, torch.float32), (12287, torch.float32), (24571, torch.bfloat16),
+                                         (20011, torch.float16)])
+def test_logprobs_of_a_wave_to_a_row(ops, vocab, dtype):
+    """Many rows of 4 to 48 KB: a wave walks a row of up to 24 tiles, and looks for its likeliest words by itself."""
+    g = gen(vocab)
+    rows = 2061
+    rank = torch.arange(vocab, device="cuda", dtype=torch.float32)
+    base = randn(g, rows, vocab)
+    few = torch.full((vocab,), True, device="cuda")
+    few[torch.randperm(vocab, generator=g, device="cuda")[:9]] = False
+    row_ptr, tokens = documents(g, rows, vocab, 3 * rows)
+    for name, x, top in (("random", 3 * base, 32), ("random", 3 * base, 1), ("constant", torch.zeros_like(base), 20), ("rising", (rank / 1000).expand(rows, vocab), 20),
+                         ("falling", (-rank / 1000).expand(rows, vocab), 20), ("few values", torch.round(base), 5), ("nine allowed", base.masked_fill(few, -INF), 20),
+                         ("nine allowed, lowest", base.masked_fill(few, torch.finfo(dtype).min), 20), ("none allowed", torch.full_like(base, -INF), 3)):
+        print(name, top, flush=True)
+        check_logprobs(ops, x.to(dtype).contiguous(), tokens, row_ptr, top)
+    check_logprobs(ops, (3 * base).to(dtype), tokens, row_ptr, 0)
+    check_logprobs(ops, (3 * base).to(dtype), tokens, row_ptr, 0, entropy=False)
+
+
+def test_logprobs_of_more_rows_than_a_launch_has_groups(ops):
+    g = gen(91)
+    rows, vocab = 2 ** 20 + 70003, 5
+    logits = randn(g, rows, vocab)
+    single = torch.randint(vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    for row_ptr, tokens in ((None, single), documents(g, rows, vocab, 2 * rows)):
+        weights, h = randn(g, len(tokens)), randn(g, rows)
+        got, want = check_logprobs(ops, logits, tokens, row_ptr, 3)
+        close(ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr, grad_entropy=h, entropy=got.entropy), *want.grad(weights, h))
+        logprobs, grad = ops.token_logprobs_grad(logits, tokens, weights, row_ptr)
+        close(logprobs, want.logprobs, want.off_logp[want.row, want.tokens])
+        close(grad, *want.grad(weights))
+
+
+@pytest.mark.parametrize("rows", [4, 600])
+def test_words_within_clamped_bounds(ops, rows):
+    """Bounds outside the tokens: the rows have the words within them, log-probabilities and gradients."""
+    g = gen(rows)
+    logits, tokens, weights = randn(g, rows, 700), torch.randint(700, (50,), generator=g, device="cuda", dtype=torch.int32), randn(g, 50)
+    row_ptr = torch.full((rows + 1,), 10 ** 12, device="cuda")
+    row_ptr[:4] = torch.tensor([-3, 20, 20, 45], device="cuda")
+    good = row_ptr.clamp(0, 50)
+    got, want = ops.token_logprobs(logits, tokens, row_ptr), Exact(logits, tokens, good)
+    close(got.logprobs, want.logprobs, want.off_logp[want.row, want.tokens])
+    logprobs, grad = ops.token_logprobs_grad(logits, tokens, weights, row_ptr)
+    close(logprobs, want.logprobs, want.off_logp[want.row, want.tokens])
+    close(grad, *want.grad(weights))
+    close(ops.token_logprobs_backward(weights, logits, tokens, got.stats, row_ptr), *want.grad(weights))
