@@ -289,7 +289,7 @@ int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const vo
  * Words that are not allowed have a logit of minus infinity (or the type's lowest value).  A row that allows no word at all (all minus
  * infinity) has log-probabilities of minus infinity and entropy 0; one with NaN or plus infinity has NaN.
  * Exponentials, here and in the gradients, are within 3 units of fp32's roundoff (2^-24) for fp32 logits, and for 16-bit logits
- * within 3 + d units, at a distance d to the row's greatest logit.
+ * within 3 + 1.3 d units, at a distance d to the row's greatest logit.
  * The workspace is 8-byte aligned.
  */
 int mlda_token_logprobs_workspace_bytes(int64_t rows, int32_t vocab, int32_t alternatives, int32_t type, size_t* bytes);

@@ -29,7 +29,7 @@ struct ClipArgs {
     uint32_t first_unit[kClipTensors + 1];   // of each tensor; the last entry is the number of units
     uint8_t type[kClipTensors];
     int32_t tensors;
-    double* partial;                         // [launches][kClipGroups]: the sum of squares of each workgroup
+    double* partial;                         // where the sums of squares go, one of each workgroup (launch after launch, without gaps)
 };
 
 // f(type tag, tensor's number, unit) for the units of this workgroup's run, first to last or last to first.

@@ -721,7 +721,7 @@ struct LogprobGradArgs {
     const int64_t* row_ptr;
     int64_t n_tokens;
     const float* grad;           // of each word's log-probability
-    float* stats;                // read, or, with kLoss, written (null: not wanted)
+    const float* stats;          // (with kLoss they are found)
     const float* entropy;        // both null: no gradient of the entropy
     const float* grad_entropy;
     float* logprobs;             // kLoss

@@ -143,7 +143,7 @@ int check_logits(const void* logits, int64_t stride, int64_t rows, int32_t vocab
 }
 
 // Few rows are cut into segments, so that there is work for the whole chip; a workgroup has at least a tile for each wave, and
-// segments are no more than the lanes that join them.  From as many rows as CUs on, rows are worked on whole.
+// segments are no more than the lanes that join them.  From twice as many rows as CUs on, rows are worked on whole.
 void segments_of(int64_t rows, int32_t vocab, int32_t unit, int32_t* segments, int32_t* cols) {
     int64_t n = 1;
     if (rows < 2 * kCus) {
@@ -284,9 +284,10 @@ int32_t clip_launches(int32_t n) { return std::max(1, (n + mlda::kClipTensors - 
 
 // Calls f(args, grid, launch) for each launch's share of the tensors.
 template <class F>
-int for_launches(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int32_t n, double* partial, F&& f) {
+int for_launches(const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, int32_t n, F&& f) {
     for (int32_t l = 0; l < clip_launches(n); ++l) {
         mlda::ClipArgs a;
+        a.partial = nullptr;
         const int32_t first = l * mlda::kClipTensors;
         a.tensors = std::min(n - first, mlda::kClipTensors);
         uint64_t units = 0;
@@ -298,8 +299,6 @@ int for_launches(const void* const* in, void* const* out, const int64_t* sizes, 
         }
         if (units > 0xffffffffull) return refuse("gradients: more than 2^32 units of elements in one launch's tensors");
         a.first_unit[a.tensors] = (uint32_t)units;
-        a.partial = partial + (int64_t)l * mlda::kClipGroups;
-        // every launch leaves as many sums as it has workgroups, the rest of its share is not read
         RC_TRY(f(a, units));
     }
     return MLDA_OK;
@@ -454,7 +453,7 @@ int mlda_token_logprobs_backward(const void* logits, int64_t stride, int64_t row
     RC_TRY(check_grad_out(grad_logits, grad_stride, logits, stride, rows, vocab, type));
     if (!stats || (n_tokens > 0 && !grad_logprobs)) return refuse("log-probabilities: stats or grad_logprobs are null");
     if (grad_entropy && !entropy) return refuse("log-probabilities: a gradient of the entropy needs the entropy");
-    mlda::LogprobGradArgs a{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, grad_logprobs, const_cast<float*>(stats), entropy,
+    mlda::LogprobGradArgs a{logits, stride, rows, vocab, tokens, row_ptr, n_tokens, grad_logprobs, stats, entropy,
                             grad_entropy, nullptr, grad_logits, grad_stride, 1, vocab, 0, 0, false};
     segments_of(rows, vocab, 1024 * (int32_t)(16 / type_bytes(type)), &a.segments, &a.segment_cols);
     return run_grad<false>(a, type, (hipStream_t)hip_stream);
@@ -502,7 +501,7 @@ unsigned clip_groups(uint64_t units) { return (unsigned)std::max<uint64_t>(1, st
 // The workgroups' sums of squares, packed: the number of them is returned in *partials.
 int sum_squares(const void* const* tensors, const int64_t* sizes, const int32_t* types, int32_t n, double* partial, int32_t* partials, hipStream_t stream) {
     *partials = 0;
-    return for_launches(tensors, nullptr, sizes, types, n, partial, [&](mlda::ClipArgs& a, uint64_t units) {
+    return for_launches(tensors, nullptr, sizes, types, n, [&](mlda::ClipArgs& a, uint64_t units) {
         const unsigned groups = clip_groups(units);
         a.partial = partial + *partials;
         *partials += (int32_t)groups;
@@ -545,7 +544,7 @@ int mlda_clip_grads(const void* const* tensors, void* const* out, const int64_t*
     int32_t partials = 0;
     const hipStream_t stream = (hipStream_t)hip_stream;
     RC_TRY(sum_squares(tensors, sizes, types, n_tensors, partial, &partials, stream));
-    return for_launches(tensors, out, sizes, types, n_tensors, partial, [&](mlda::ClipArgs& a, uint64_t units) {
+    return for_launches(tensors, out, sizes, types, n_tensors, [&](mlda::ClipArgs& a, uint64_t units) {
         hipLaunchKernelGGL(mlda::clip_kernel, dim3(clip_groups(units)), dim3(mlda::kClipThreads), 0, stream, a, partial, partials, max_norm, norm);
         return launched("clip_kernel");
     });
