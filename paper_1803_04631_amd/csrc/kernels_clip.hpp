@@ -7,7 +7,7 @@
 // each workgroup, whatever tensors it crosses.  Squares are summed in fp64: no gradient that fp32 holds overflows it,
 // and the order is fixed: by thread, by workgroup, then over the workgroups.  The scaling goes over each run
 // from its end to its start, where what was read last is still in the caches, and keeps what it reads and writes out of them:
-// 142e6 fp32 elements 281 us, without the latter 332 (100 us of it the first read, 5.7 TB/s).
+// 142e6 fp32 elements 281 us, without the latter 318 (98 us of it the first read, 5.8 TB/s).
 #pragma once
 #include "vec_io.hpp"
 

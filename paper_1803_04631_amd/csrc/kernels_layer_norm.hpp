@@ -169,7 +169,7 @@ __global__ __launch_bounds__(team_threads(kTeam)) void layer_norm_kernel(LayerNo
 }
 
 // Rows that no team has the registers for: a workgroup reads them three times, the second and third time from the caches (2,003 x 40,000
-// fp32 172 us, 3.7 TB/s of the row once in and once out).  A thread adds up any number of columns, so in fp64, which the reads leave time for: the
+// fp32 174 us, 3.7 TB/s of the row once in and once out).  A thread adds up any number of columns, so in fp64, which the reads leave time for: the
 // sum of equal numbers is exact, whatever their number.
 template <class T, class W>
 __global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs a) {
@@ -235,9 +235,10 @@ __device__ __forceinline__ void grad_piece(Raw x, Raw g, const Columns<W, kPack<
 }
 
 // kSums: the weight's and bias' gradients are summed here, and the weight is kept.  kAhead: the next row's pieces are loaded ahead.
-// 300,000 x 1,000 bf16 374 us (4.8 TB/s), fp32 712 (5.1); 30,011 x 1,537 bf16, rows at odd addresses, 59 us (4.7); 8,009 x 10,000 fp32, whose
-// sums and weights take three eighths of the registers, 210 (4.6).  Four waves a SIMD are worth more than the few registers of a lane that 16-bit
-// rows with fp32 weights keep in memory for it (5 to 11 of 128): 30,011 x 1,537 66 us, with three waves and none 77; 300,000 x 1,000 339 and 389.
+// 300,000 x 1,000 bf16 374 us (4.8 TB/s), fp32 712 (5.1); 30,011 x 1,537 bf16, rows at odd addresses, 59 us (4.7; the vector units work in 93%
+// of the cycles); 8,009 x 10,000 fp32, whose sums and weights take three eighths of the registers, 209 (4.6).  Four waves a SIMD are worth
+// more than the few registers of a lane that 16-bit rows with fp32 weights keep in memory for it (5 to 11 of 128): 30,011 x 1,537 66 us,
+// with three waves and none 77; 300,000 x 1,000 339 and 389.
 template <class T, class W, int kTeam, int kPieces, bool kSums, bool kAhead = kSums>
 __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ? 4 : 1) void layer_norm_grad_kernel(LayerNormGradArgs a) {
     constexpr int P = kPack<T>, kThreads = team_threads(kTeam), kTeams = kThreads / kTeam;
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
             }
 #pragma unroll
             for (int e = 0; e < P; ++e) v[e] = rstd * ((h[e] - mean_h) - u[e] * mean_hu);
-            // (a team that its sums fill has no registers for two kinds of stores: 8,009 x 10,000 fp32 210 us, with both 223)
+            // (a team that its sums fill has no registers for two kinds of stores: 8,009 x 10,000 fp32 209 us, with both 223)
             if constexpr (kSums && !kAhead) {
                 if (dx) store_some(dx + c, pack(v, T()), min(max(cols - c, 0), P));
             } else {
@@ -393,7 +394,7 @@ __global__ __launch_bounds__(team_threads(kTeam), kTeam <= 512 && kPieces == 2 ?
 }
 
 // Rows without room in registers: the gradient of x by a workgroup a row, which reads the row twice (2,003 x 40,000 fp32 with the sums
-// below 368 us, 2.6 TB/s of everything once).  Sums over columns in fp64, as above.
+// below 366 us, 2.6 TB/s of everything once).  Sums over columns in fp64, as above.
 template <class T, class W>
 __global__ __launch_bounds__(1024) void layer_norm_grad_long_kernel(LayerNormGradArgs a) {
     constexpr int P = kPack<T>;

@@ -8,7 +8,7 @@
 //
 // One pass over a row has the maximum, both sums and the likeliest words: each lane keeps a running maximum and rescales
 // its sums when it grows; lanes, waves and segments of a row are joined at the end.  Bound by memory where the logits have 4 bytes;
-// with 2 the instructions issued (about ten an element) are not far behind.
+// with 2 by the vector instructions issued (with entropies and likeliest words 11 to 15 an element).
 //
 // The statistics of a row are kept as the pair (m, ln s): their sum is the logarithm of the sum of exponentials, and
 // differences to m lose nothing where m is large.  A row whose logits are all minus infinity has (-inf, 0).
@@ -183,8 +183,8 @@ struct Candidates {
 
 // ---------------------------------------------------------------- one pass over a row, or a segment
 // x - m for a bound m of x, and its exponential.  The product t = d log2(e) alone, rounded, would leave an exponential with |d| units of
-// roundoff: w = d - t ln(2) is what it leaves out, and 2^t + 2^t w is within three units at any distance (2,400 x 102,000 fp32 186 us, so
-// 181 without).  Logits of 16 bits have 2^-9 or 2^-12 of themselves for an error, and their kernels are held up by instructions: there the
+// roundoff: w = d - t ln(2) is what it leaves out, and 2^t + 2^t w is within three units at any distance (2,400 x 102,000 fp32 176 us,
+// 174 without).  Logits of 16 bits have 2^-9 or 2^-12 of themselves for an error, and their kernels are held up by instructions: there the
 // product is taken as it is (1,024 x 102,000 bf16 40 us, with w 50; 6,007 x 40,009 with the 20 likeliest words 131, with w 142).
 constexpr float kLn2 = 0.693147182464599609375f, kLn2Low = -1.904654299957768e-9f;      // ln(2) as fp32 has it, and the rest
 template <class T>
@@ -593,8 +593,8 @@ __device__ __forceinline__ int find_top(const Span<T>& span, float most, int n, 
 }
 
 // Workgroup by workgroup a row, or a segment of one: with one segment all is done, else logprob_join_kernel goes on.  2,400 x 102,000 fp32
-// 180 us (5.4 TB/s), bf16 91; 2,048 x 141,000 fp16 with entropy and the 5 likeliest words 118 us (4.9), 6,007 x 40,009 bf16 with 20
-// 122 (3.9: instructions, and rows at odd addresses); one row of 102,000 bf16 in 25 segments 6.9 us, and 4.9 to join them.
+// 176 us (5.6 TB/s), bf16 91; 2,048 x 141,000 fp16 with entropy and the 5 likeliest words 115 us (5.0), 6,007 x 40,009 bf16 with 20
+// 122 (3.9): the vector units work in 91 and 92% of the cycles of both; one row of 102,000 bf16 in 25 segments 6.9 us, and 5.5 to join them.
 template <class T, bool kEntropy, bool kTop, int kWaves>
 __global__ __launch_bounds__(kWaves * kWave) void logprob_kernel(LogprobArgs a) {
     __shared__ std::conditional_t<kTop, TopLds<kWaves>, FoldLds<kWaves * kWave>> lds;
@@ -785,7 +785,7 @@ struct RowGrad {
 template <class T, int kThreads, bool kLoss, bool kEntropy, class Own>
 __device__ __forceinline__ void stream_grad(const T* row, T* out, int32_t begin, int32_t end, const RowGrad& g, bool once, Own&& own) {
     // a column's place is its number plus `shift`: all pieces but the first and the last lie at 16-byte boundaries, wherever rows begin
-    // (6,007 x 40,009 bf16 words 198 us, now 186)
+    // (6,007 x 40,009 bf16, one word a row: at the row's own 202 us, so 190)
     constexpr int P = kPack<T>;
     const int shift = (int)(reinterpret_cast<uintptr_t>(row) / sizeof(T) % P);
     const int64_t lo = (int64_t)begin + shift, hi = (int64_t)end + shift;
@@ -801,7 +801,7 @@ __device__ __forceinline__ void stream_grad(const T* row, T* out, int32_t begin,
 
 // Rows, or segments of rows.  kLoss: the statistics and the words' log-probabilities are found first, by the same workgroup
 // (one segment); the row is read twice then, and the last cache gives it no faster than memory does.  1,024 x 102,000 bf16, 330 words a
-// row: 75 us for the gradient alone (5.6 TB/s), 114 with the loss; 8,000 x 12,000 fp32, one word a row, 145 and 150.  Table: a word's
+// row: 72 us for the gradient alone (5.8 TB/s), 109 with the loss; 8,000 x 12,000 fp32, one word a row, 143 and 151.  Table: a word's
 // slot costs 12 bytes of LDS, against 8 bytes a column.  kSingle: one word to a row.  The logits' rows may be the gradient's.
 template <class T, int kThreads, bool kLoss, bool kEntropy, bool kSingle>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs a) {

@@ -35,8 +35,9 @@ size_t type_bytes(int32_t t) { return t == MLDA_FP32 ? 4 : 2; }
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 // Whether a call that reads and writes so many bytes leaves them out of the caches (256 MB on the way to memory): what is written then
-// does not push out what is still to be read.  Below, the next call finds the results there.  The gradient of 1,024 x 102,000 bf16 logits 109 us,
-// written past the caches 80; of 1,000 x 5,000 fp32, 40 MB in all, 12 either way.
+// does not push out what is still to be read.  Below, the next call finds the results there.  The gradient of 1,024 x 102,000 bf16 logits 97 us,
+// written past the caches 72, with the loss 122 and 109; layer norm's gradients of 30,011 x 1,537 bf16 75 and 62; but layer norm of 300,000 x 1,000
+// 247 and 253; the gradient of 1,000 x 5,000 fp32, 40 MB in all, 15 either way.
 bool passes_caches(double bytes) { return bytes > 192e6; }
 
 // f(tag) for the type; the type is known.
@@ -81,7 +82,7 @@ struct Team {
 };
 
 // f(team) for the lanes that share a row and the 16-byte pieces that each holds: as few lanes as have the registers.  300,000 x 1,000 bf16
-// by a wave a row 250 us, by four 424; 30,011 x 1,537 37 and 49.
+// by a wave a row 253 us, by four 585; 30,011 x 1,537 38 and 66.
 template <class F>
 void with_team(int64_t row_bytes, F&& f) {
     if (row_bytes <= 64) f(Team<4, 1>());
@@ -96,7 +97,7 @@ void with_team(int64_t row_bytes, F&& f) {
     else f(Team<1024, 8>());
 }
 constexpr int64_t kHeldBytes = 131072;            // of a row that a team holds
-// of one beside whose gradient there is room for the weight's (two sums a column; 8,009 x 10,000 fp32 with the sums on their own 333 us, so 210)
+// of one beside whose gradient there is room for the weight's (two sums a column; 8,009 x 10,000 fp32 with the sums on their own 315 us, so 209)
 constexpr int64_t summed_bytes(int64_t type_bytes) { return type_bytes == 4 ? 65536 : 32768; }
 
 // The same for the gradient, where a column takes four times the registers; f(team, workgroups that fit a CU).
@@ -123,7 +124,7 @@ int32_t norm_grad_groups(int64_t rows, int32_t cols, int32_t type) {
         groups = std::min<int64_t>((rows + kTeams - 1) / kTeams, per_cu * kCus);
     });
     // their sums, written and read, are to be no more than what the rows are, unless they are less than 1 MB: 247 x 14,375 bf16 with a
-    // workgroup a row 31 us, so 27
+    // workgroup a row 31 us, so 28
     groups = std::min(groups, std::max<int64_t>(rows * (int64_t)type_bytes(type) * 3 / 16, (1 << 20) / (8 * (int64_t)cols)));
     return (int32_t)std::max<int64_t>(1, groups);
 }
@@ -158,8 +159,8 @@ void segments_of(int64_t rows, int32_t vocab, int32_t unit, int32_t* segments, i
 // Where documents are this long on average, their words are looked up by more workgroups than there are rows.
 constexpr int64_t kLongDocument = 2048;
 
-// Many short rows have a wave each instead of a workgroup of four: 4,096 rows of 12,000 bf16 with the 20 likeliest words 27 us against
-// 38, 20,000 of 3,001 49 against 110; but of 100,000 fp32 317 against 284, and 1,024 of 48,001 bf16 33 against 25.
+// Many short rows have a wave each instead of a workgroup of four: 4,096 rows of 12,000 bf16 with the 20 likeliest words 29 us against
+// 40, 20,000 of 3,001 54 against 126; but 4,096 of 100,000 fp32 318 against 301, and 1,024 of 48,001 bf16 35 against 27.
 bool wave_rows(int64_t rows, int32_t vocab, int32_t type) {
     const int64_t bytes = (int64_t)vocab * (int64_t)type_bytes(type);
     return bytes <= 4096 || (bytes <= 49152 && rows >= 8 * kCus);
@@ -206,9 +207,10 @@ int run_logprobs(mlda::LogprobArgs a, int32_t type, void* workspace, hipStream_t
 }
 
 // The words' table has eight slots for each word of a document of mean length (longer ones fit up to seven times that), and so many that
-// a document of more words, done by ranges of columns, has at most some sixty ranges.  Where sums for all columns take no
-// more room there is no table (0 slots); *columns: of a range.  (With four slots a word 1,024 documents of 330 words over 102,000 columns
-// took 182 us, as the few that were too long held up the end; so 133.)
+// a document of more words, done by ranges of columns, has at most 64 ranges, up to 786,432 columns; beyond, the table has its most slots, and there
+// is a range for every 12,288 columns.  Where sums for all columns take no more room there is no table (0 slots); *columns: of a
+// range.  (With four slots a word 1,000 documents of 100 words over 5,000 columns, with the loss, took 21 us, as the few that were
+// too long held up the end; so 15.  14,235 of 22 over 400 28 and 27.)
 int32_t table_slots(int64_t rows, int64_t n_tokens, int32_t cols, int32_t* columns) {
     constexpr int32_t kMostSlots = 8192;
     int32_t slots = 64;
@@ -219,8 +221,8 @@ int32_t table_slots(int64_t rows, int64_t n_tokens, int32_t cols, int32_t* colum
     return 0;
 }
 
-// Threads that share a row, by its bytes.  Loss and gradient with 64, 256 and 512 threads: 20,000 x 3,001 bf16 59, 92 and 168 us,
-// 1,000 x 5,000 fp32 33, 19 and 27, 1,024 x 102,000 bf16 (256 and 512) 230 and 157.
+// Threads that share a row, by its bytes.  Loss and gradient with 64, 256 and 512 threads: 20,000 x 3,001 bf16 62, 109 and 190 us,
+// 1,000 x 5,000 fp32 30, 15 and 19, 8,000 x 12,000 fp32 193, 151 and 176, 1,024 x 102,000 bf16 346, 142 and 109.
 int grad_threads(int64_t cols, int32_t type) {
     const int64_t bytes = cols * (int64_t)type_bytes(type);
     return bytes <= kWaveRowBytes ? 64 : bytes <= kGroupRowBytes ? 256 : 512;

@@ -1,7 +1,7 @@
 // The operators' calls on torch tensors: argument checks, outputs, workspaces, and one call of the C ABI each (include/mlda.h), on
 // torch's current stream of the tensors' device.  operators.py is what a user imports, and says what each call does.
 //
-// This is compiled code because small calls are spent here: layer norm of one document takes the GPU 4 us, and
+// This is compiled code because small calls are spent here: layer norm of one document takes the GPU 2.8 us, and
 // took 12 us to call through ctypes.
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
