@@ -265,7 +265,8 @@ int mlda_layer_norm(const void* x, int64_t x_stride, const void* weight, const v
  *   grad_x = rstd (h - mean over columns of h - u (mean over columns of h u)),
  *   grad_weight = sum over rows of grad_y u, grad_bias = sum over rows of grad_y.
  * Each of grad_x (of the type of x; may be x or grad_y), grad_weight and grad_bias (of weight_type) may be null: not wanted.  Without
- * rows grad_weight and grad_bias are zeros.  The workspace (4-byte aligned) is for grad_weight and grad_bias.
+ * rows grad_weight and grad_bias are zeros.  They are sums in fp32, each within (rows / 256 + 64) 2^-24 of the sum of its terms'
+ * magnitudes before it is rounded.  The workspace (4-byte aligned) is for grad_weight and grad_bias.
  */
 int mlda_layer_norm_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes);
 int mlda_layer_norm_backward(const void* grad_y, int64_t grad_y_stride, const void* x, int64_t x_stride, const float* mean,
