@@ -335,6 +335,74 @@ int mlda_grad_norm(const void* const* tensors, const int64_t* sizes, const int32
 int mlda_clip_grads(const void* const* tensors, void* const* out, const int64_t* sizes, const int32_t* types, int32_t n_tensors,
                     double max_norm, float* norm, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Matrices in microscaled 4-bit floating point: rows of cols columns (1 .. 2^30) in blocks of 32, whose last may be short.  With a the greatest
+ * magnitude of a block its scale is the least 2^s, s >= -127, with a < 7 2^s, and x is held as x / 2^s rounded to nearest, ties to even, among
+ * 0, 1/2, 1, 3/2, 2, 3, 4, 6 (the codes 0 .. 7; 8 more: negative).  What is held is within 1/6 of x, or within 2^s / 4.
+ *   codes    rows x blocks x 16 bytes, 16-byte aligned: column 2j of a row is the lower half of its byte j, 2j + 1 the upper; columns behind
+ *            the last have the code 0 (mlda_mx_linear relies on that)
+ *   scales   rows x blocks bytes: s + 127; 255: the block holds NaN or infinity, and stands for NaN as a whole
+ * mlda_mx_dequantize writes x, what codes and scales stand for, rounded to its type (fp32 and bf16 hold all of it).
+ */
+int mlda_mx_quantize(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, int64_t rows, int32_t cols, int32_t type,
+                      void* hip_stream);
+int mlda_mx_dequantize(const uint8_t* codes, const uint8_t* scales, void* x, int64_t x_stride, int64_t rows, int32_t cols, int32_t type,
+                        void* hip_stream);
+
+/*
+ * The product of rows with a matrix that is held in 4 bits: y[r][n] = sum over columns of Q(x)[r][k] W[n][k] + bias[n], Q(x) what
+ * mlda_mx_quantize makes of x.
+ *   codes, scales   the matrix W of words rows (1 .. 2^30) and cols columns
+ *   bias            words entries of bias_type (out_type, or MLDA_FP32); null: zeros
+ *   y               rows x words of out_type; not in the place of x
+ * Sums are fp32: within (cols / 128 + 8) 2^-24 of the sum of its terms' magnitudes before y is rounded.  A row or word with a block of NaN has
+ * NaN.  The workspace (16-byte aligned) is for Q(x).
+ */
+int mlda_mx_linear_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes);
+int mlda_mx_linear(const void* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales, const void* bias, void* y, int64_t y_stride,
+                    int64_t rows, int32_t cols, int32_t words, int32_t type, int32_t out_type, int32_t bias_type, void* dev_workspace,
+                    size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Dropout: y = x / (1 - p) where an element is kept, else 0 (whatever x is), plus residual.  It is kept where a 32-bit number u is at least p 2^32,
+ * rounded.  The upper half of u is 16 bits of Philox4x32-10 with the key seed and the counter (column / 8, first_row + row, step, 1): the lower
+ * half of its word column % 8 / 2 for an even column, the upper for an odd; the lower half of u is the same of the counter (.., .., .., 2).  So a
+ * mask depends on nothing but seed, step and the element's place, and is drawn again by the backward pass: the gradient with respect to x is
+ * the same call on the gradient of y, without residual; that of residual is the gradient of y itself.
+ *   p           0 .. 1 (1: everything is dropped)
+ *   step        of the training, or another number: each has masks of its own
+ *   dev_step    device, 1 entry, added to step (modulo 2^32) when the kernel runs, so that a captured graph can draw another mask at each
+ *               replay; null: 0
+ *   first_row   the number of x's first row, so that parts of a batch have the whole's masks; first_row + rows at most 2^32
+ *   residual    null: none
+ *   y           may be x or residual
+ */
+int mlda_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y, int64_t y_stride, int64_t rows,
+                 int32_t cols, double p, uint64_t seed, uint32_t step, const int64_t* dev_step, int64_t first_row, int32_t type,
+                 void* hip_stream);
+
+/*
+ * The clipped policy loss with a KL term, and its gradient with respect to the log-probabilities of n_tokens (< 2^31) words (as
+ * mlda_token_logprobs gives them; mlda_token_logprobs_backward takes the gradient).  With l a word's log-probability, o that with which it was drawn, f
+ * that of a reference model, A its advantage, w its weight and d = l - o, a word is clipped where A > 0 and d > ln(1 + high), or A < 0 and
+ * d < ln(1 - low), and
+ *   loss = sum of w (kl (exp(f - l) - (f - l) - 1) - A b),  b = 1 + high or 1 - low where clipped, else exp(d)
+ *   grad_logprobs = w (kl (1 - exp(f - l)) - A (0 where clipped, else exp(d))).
+ *   reference       null: no KL term (kl must be 0)
+ *   row_ptr         rows + 1 entries as in mlda_token_logprobs; advantages has an entry for each row.  Null: one for each word, rows = n_tokens.
+ *   weights         n_tokens entries; null: 1 / n_tokens each.  A word of weight 0 is none: its numbers are of no matter, its gradient is 0.  So are
+ *                   words before row_ptr[0] and from row_ptr[rows] on.
+ *   low, high       0 <= low <= 1, high >= 0 (1 and infinity: never clipped)
+ *   kl              finite
+ *   sums            3 entries: the loss, the sum of w (exp(f - l) - (f - l) - 1), and the sum of w of the words that are clipped
+ *   grad_logprobs   n_tokens entries; may be logprobs
+ * Everything is computed in fp64 and rounded once.  The workspace is 8-byte aligned.
+ */
+int mlda_policy_loss_workspace_bytes(int64_t n_tokens, size_t* bytes);
+int mlda_policy_loss(const float* logprobs, const float* old_logprobs, const float* reference, const float* advantages, const float* weights,
+                     const int64_t* row_ptr, int64_t rows, int64_t n_tokens, double low, double high, double kl, float* sums,
+                     float* grad_logprobs, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* mlda_strerror(int code);
 const char* mlda_last_error(void);
 

@@ -67,6 +67,13 @@ def load_library() -> ctypes.CDLL:
         "mlda_grad_norm_workspace_bytes": [i32, p],
         "mlda_grad_norm": [p, p, p, i32, p, p, sz, p],
         "mlda_clip_grads": [p, p, p, p, i32, dbl, p, p, sz, p],
+        "mlda_mx_quantize": [p, i64, p, p, i64, i32, i32, p],
+        "mlda_mx_dequantize": [p, p, p, i64, i64, i32, i32, p],
+        "mlda_mx_linear_workspace_bytes": [i64, i32, p],
+        "mlda_mx_linear": [p, i64, p, p, p, p, i64, i64, i32, i32, i32, i32, i32, p, sz, p],
+        "mlda_dropout": [p, i64, p, i64, p, i64, i64, i32, dbl, u64, u32, p, i64, i32, p],
+        "mlda_policy_loss_workspace_bytes": [i64, p],
+        "mlda_policy_loss": [p, p, p, p, p, p, i64, i64, dbl, dbl, dbl, p, p, p, sz, p],
     }
     for name, argtypes in sig.items():
         fn = getattr(lib, name)
@@ -90,7 +97,9 @@ EXPORTED = ["mlda_workspace_bytes", "mlda_create", "mlda_workspace_bytes_streame
             "mlda_philox_uniform", "mlda_layer_norm", "mlda_layer_norm_workspace_bytes",
             "mlda_layer_norm_backward", "mlda_token_logprobs_workspace_bytes", "mlda_token_logprobs",
             "mlda_token_logprobs_backward", "mlda_token_logprobs_grad", "mlda_grad_norm_workspace_bytes",
-            "mlda_grad_norm", "mlda_clip_grads", "mlda_strerror", "mlda_last_error"]
+            "mlda_grad_norm", "mlda_clip_grads", "mlda_mx_quantize", "mlda_mx_dequantize",
+            "mlda_mx_linear_workspace_bytes", "mlda_mx_linear", "mlda_dropout",
+            "mlda_policy_loss_workspace_bytes", "mlda_policy_loss", "mlda_strerror", "mlda_last_error"]
 
 
 def _check(rc: int):

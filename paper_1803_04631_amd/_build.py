@@ -13,7 +13,7 @@ import tempfile
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libmlda.so")
-SOURCES = ["mlda.hip", "operators.hip"]
+SOURCES = ["mlda.hip", "operators.hip", "mx4.hip", "training.hip"]
 TENSORS_PATH = os.path.join(_HERE, "_tensors.so")
 
 HIPCC_FLAGS = [

@@ -6,6 +6,7 @@
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
@@ -288,6 +289,145 @@ Tensor clip_grads(const std::vector<Tensor>& tensors, std::optional<double> most
     return norm;
 }
 
+// A matrix held in 4 bits: the tuple (codes, scales, cols) that operators.py calls Mx4.
+struct Mx4 {
+    Tensor codes, scales;
+    int64_t rows, cols, blocks;
+    at::Device device = at::kCPU;
+    Mx4(py::handle h, const char* name) {
+        TORCH_CHECK_VALUE(PyTuple_Check(h.ptr()) && PyTuple_GET_SIZE(h.ptr()) == 3, name, " must be an Mx4: codes, scales and the number of columns");
+        codes = tensor(PyTuple_GET_ITEM(h.ptr(), 0), "codes");
+        scales = tensor(PyTuple_GET_ITEM(h.ptr(), 1), "scales");
+        cols = PyLong_Check(PyTuple_GET_ITEM(h.ptr(), 2)) ? PyLong_AsLongLong(PyTuple_GET_ITEM(h.ptr(), 2)) : -1;
+        if (PyErr_Occurred()) throw py::error_already_set();
+        TORCH_CHECK_VALUE(codes.defined() && codes.is_cuda(), "codes must be a tensor on a GPU: there is no CPU path");
+        TORCH_CHECK_VALUE(cols >= 1 && cols <= INT32_MAX && codes.dim() == 2, name, " must be a matrix with at least one column");
+        rows = codes.size(0);
+        blocks = (cols + 31) / 32;
+        device = codes.device();
+        at_of(codes, "codes", {rows, blocks * 16}, at::kByte, device);
+        at_of(scales, "scales", {rows, blocks}, at::kByte, device);
+    }
+    const uint8_t* at_codes() const { return codes.data_ptr<uint8_t>(); }
+    const uint8_t* at_scales() const { return scales.data_ptr<uint8_t>(); }
+};
+
+std::tuple<Tensor, Tensor, int64_t> mx4_quantize(const Tensor& x, const std::optional<Mx4>& out) {
+    const Rows r = rows_of(x, "x");
+    Tensor codes, scales;
+    if (out) {
+        TORCH_CHECK_VALUE(out->rows == r.rows && out->cols == r.cols && out->device == r.device, "out must have the shape and device of x");
+        codes = out->codes;
+        scales = out->scales;
+    } else {
+        const int64_t blocks = ((int64_t)r.cols + 31) / 32;
+        codes = empty({r.rows, blocks * 16}, at::kByte, r.device);
+        scales = empty({r.rows, blocks}, at::kByte, r.device);
+    }
+    const c10::DeviceGuard guard(r.device);
+    check(mlda_mx_quantize(r.at, r.stride, codes.data_ptr<uint8_t>(), scales.data_ptr<uint8_t>(), r.rows, r.cols, r.kind, stream_of(r.device)));
+    if (out) {
+        written(codes);
+        written(scales);
+    }
+    return {codes, scales, r.cols};
+}
+
+Tensor mx4_dequantize(const Mx4& q, const std::optional<at::ScalarType>& dtype, const Maybe& out) {
+    const Tensor x = out ? *out : empty({q.rows, q.cols}, dtype.value_or(at::kFloat), q.device);
+    const Rows r = rows_of(x, out ? "out" : "dtype");
+    TORCH_CHECK_VALUE(r.rows == q.rows && r.cols == q.cols && r.device == q.device && (!dtype || x.scalar_type() == *dtype),
+                      "out must have the shape and device of the matrix, and the type that is asked for");
+    const c10::DeviceGuard guard(r.device);
+    check(mlda_mx_dequantize(q.at_codes(), q.at_scales(), r.at, r.stride, r.rows, r.cols, r.kind, stream_of(r.device)));
+    written(out);
+    return x;
+}
+
+Tensor mx4_linear(const Tensor& x, const Mx4& weight, const Maybe& bias, const std::optional<at::ScalarType>& dtype, const Maybe& out) {
+    const Rows r = rows_of(x, "x");
+    TORCH_CHECK_VALUE(weight.cols == r.cols && weight.device == r.device && weight.rows >= 1 && weight.rows <= INT32_MAX,
+                      "weight must have as many columns as x, at least one row, and be on its device");
+    const Tensor y = out ? *out : empty({r.rows, weight.rows}, dtype.value_or(x.scalar_type()), r.device);
+    const Rows ry = rows_of(y, out ? "out" : "dtype");
+    TORCH_CHECK_VALUE(ry.rows == r.rows && ry.cols == weight.rows && ry.device == r.device && (!dtype || y.scalar_type() == *dtype),
+                      "out must have the rows of x, the weight's rows as columns, and the type that is asked for, on the device of x");
+    void* at_bias = nullptr;
+    int bias_kind = MLDA_FP32;
+    if (bias) {
+        bias_kind = bias->defined() ? type_code(*bias) : -1;
+        TORCH_CHECK_VALUE(bias_kind == ry.kind || bias_kind == MLDA_FP32, "bias must have the type of the result, or be fp32");
+        at_bias = at_of(*bias, "bias", {weight.rows}, bias->scalar_type(), r.device);
+    }
+    size_t bytes = 0;
+    check(mlda_mx_linear_workspace_bytes(r.rows, r.cols, &bytes));
+    const Workspace w(bytes, r.device);
+    const c10::DeviceGuard guard(r.device);
+    check(mlda_mx_linear(r.at, r.stride, weight.at_codes(), weight.at_scales(), at_bias, ry.at, ry.stride, r.rows, r.cols, ry.cols, r.kind, ry.kind,
+                          bias_kind, w.at, w.bytes, stream_of(r.device)));
+    written(out);
+    return y;
+}
+
+// `step`: a number, or a tensor of one on the GPU that the kernel reads.
+Tensor dropout(const Tensor& x, double p, uint64_t seed, py::handle step, int64_t first_row, const Maybe& residual, const Maybe& out) {
+    const Rows r = rows_of(x, "x");
+    uint32_t number = 0;
+    const int64_t* at_step = nullptr;
+    if (THPVariable_Check(step.ptr())) {
+        const Tensor& t = THPVariable_Unpack(step.ptr());
+        TORCH_CHECK_VALUE(t.defined() && t.numel() == 1 && t.scalar_type() == at::kLong && t.device() == r.device,
+                          "step must be a number, or an int64 tensor of one entry on the device of x");
+        at_step = t.data_ptr<int64_t>();
+    } else {
+        const long long n = PyLong_Check(step.ptr()) ? PyLong_AsLongLong(step.ptr()) : -1;
+        if (PyErr_Occurred()) PyErr_Clear();
+        TORCH_CHECK_VALUE(n >= 0 && n <= UINT32_MAX, "step must be a number in 0 .. 2^32 - 1, or an int64 tensor of one entry on the device of x");
+        number = (uint32_t)n;
+    }
+    Rows rr{};
+    if (residual) rr = rows_like(*residual, "residual", r);
+    Rows ry;
+    const Tensor y = out_for(out, x, r, ry);
+    const c10::DeviceGuard guard(r.device);
+    check(mlda_dropout(r.at, r.stride, rr.at, rr.stride, ry.at, ry.stride, r.rows, r.cols, p, seed, number, at_step, first_row, r.kind, stream_of(r.device)));
+    written(out);
+    return y;
+}
+
+// (loss, KL term, clipped weight as views of one tensor, gradient)
+std::tuple<Tensor, Tensor, Tensor, Tensor> policy_loss(const Tensor& logprobs, const Tensor& old, const Tensor& advantages, const Maybe& weights,
+                                                       const Maybe& reference, const Maybe& row_ptr, double low, double high, double kl, const Maybe& out) {
+    TORCH_CHECK_VALUE(logprobs.defined() && logprobs.is_cuda(), "logprobs must be a tensor on a GPU: there is no CPU path");
+    const at::Device device = logprobs.device();
+    const int64_t n = logprobs.numel();
+    TORCH_CHECK_VALUE(!row_ptr || (row_ptr->defined() && row_ptr->numel() >= 1), "row_ptr must have one entry more than there are rows");
+    const int64_t rows = row_ptr ? row_ptr->numel() - 1 : n;
+    auto floats = [&](const Tensor& t, const char* name, int64_t size) { return static_cast<float*>(at_of(t, name, {size}, at::kFloat, device)); };
+    const float* at_l = floats(logprobs, "logprobs", n);
+    const float* at_old = floats(old, "old_logprobs", n);
+    const float* at_reference = reference ? floats(*reference, "reference", n) : nullptr;
+    const float* at_advantages = floats(advantages, "advantages", rows);
+    const float* at_weights = weights ? floats(*weights, "weights", n) : nullptr;
+    const int64_t* at_ptr = row_ptr ? static_cast<int64_t*>(at_of(*row_ptr, "row_ptr", {rows + 1}, at::kLong, device)) : nullptr;
+    const Tensor grad = out ? *out : fp32({n}, device), sums = fp32({3}, device);
+    float* at_grad = floats(grad, "out", n);
+    size_t bytes = 0;
+    check(mlda_policy_loss_workspace_bytes(n, &bytes));
+    const Workspace w(bytes, device);
+    const c10::DeviceGuard guard(device);
+    check(mlda_policy_loss(at_l, at_old, at_reference, at_advantages, at_weights, at_ptr, rows, n, low, high, kl, sums.data_ptr<float>(), at_grad, w.at,
+                           w.bytes, stream_of(device)));
+    written(out);
+    return {sums.select(0, 0), sums.select(0, 1), sums.select(0, 2), grad};
+}
+
+std::optional<at::ScalarType> type_of(py::handle h) {
+    if (h.is_none()) return std::nullopt;
+    TORCH_CHECK_VALUE(THPDtype_Check(h.ptr()), "dtype must be a torch type");
+    return reinterpret_cast<THPDtype*>(h.ptr())->scalar_type;
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_tensors, m) {
@@ -316,5 +456,19 @@ PYBIND11_MODULE(_tensors, m) {
         TORCH_CHECK_VALUE(most, "max_norm must be a number: grad_norm gives the norm alone");
         return clip_grads(tensors_of(tensors, "every one of tensors"), most,
                           out.is_none() ? std::nullopt : std::optional<std::vector<Tensor>>(tensors_of(out, "every one of out")));
+    });
+    m.def("mx4_quantize", [](H x, H out) {
+        return mx4_quantize(tensor(x, "x"), out.is_none() ? std::nullopt : std::optional<Mx4>(Mx4(out, "out")));
+    });
+    m.def("mx4_dequantize", [](H q, H dtype, H out) { return mx4_dequantize(Mx4(q, "q"), type_of(dtype), maybe(out, "out")); });
+    m.def("mx4_linear", [](H x, H weight, H bias, H dtype, H out) {
+        return mx4_linear(tensor(x, "x"), Mx4(weight, "weight"), maybe(bias, "bias"), type_of(dtype), maybe(out, "out"));
+    });
+    m.def("dropout", [](H x, double p, uint64_t seed, H step, int64_t first_row, H residual, H out) {
+        return dropout(tensor(x, "x"), p, seed, step, first_row, maybe(residual, "residual"), maybe(out, "out"));
+    });
+    m.def("policy_loss", [](H logprobs, H old, H advantages, H weights, H reference, H row_ptr, double low, double high, double kl, H out) {
+        return policy_loss(tensor(logprobs, "logprobs"), tensor(old, "old_logprobs"), tensor(advantages, "advantages"), maybe(weights, "weights"),
+                           maybe(reference, "reference"), maybe(row_ptr, "row_ptr"), low, high, kl, maybe(out, "out"));
     });
 }

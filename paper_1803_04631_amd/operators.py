@@ -1,6 +1,7 @@
 """Operators on CUDA tensors for models that are trained and scored next to the sampled topics: layer
-norm, log-probabilities of documents' words with entropy and likeliest words, their gradients, and
-the global gradient norm with clipping.
+norm, log-probabilities of documents' words with entropy and likeliest words, their gradients, the
+global gradient norm with clipping, dropout, the clipped policy loss, and matrices in microscaled
+4-bit floating point with the product that scores documents against them.
 
 Argument marshalling only, like the rest of the binding (here compiled, csrc/tensors.cpp, for the sake of
 small calls): everything is computed by the library's HIP kernels (include/mlda.h says what exactly),
@@ -30,6 +31,21 @@ if not os.path.exists(TENSORS_PATH):
 from . import _tensors              # noqa: E402
 
 MAX_ALTERNATIVES = 32               # MLDA_MAX_ALTERNATIVES
+
+
+class Mx4(NamedTuple):
+    """A matrix [rows, cols] held in 4 bits (include/mlda.h has the format).  Rows [a, b) of it are
+    Mx4(codes[a:b], scales[a:b], cols)."""
+    codes: torch.Tensor                        # [rows, 16 ceil(cols / 32)] uint8
+    scales: torch.Tensor                       # [rows, ceil(cols / 32)] uint8
+    cols: int
+
+
+class PolicyLoss(NamedTuple):
+    loss: torch.Tensor                         # scalars, fp32
+    kl: torch.Tensor                           # sum of the weighted KL terms
+    clipped: torch.Tensor                      # sum of the weights of the words that are clipped
+    grad_logprobs: torch.Tensor                # [n_tokens] fp32: the loss' gradient
 
 
 class TokenLogprobs(NamedTuple):
@@ -85,3 +101,46 @@ def clip_grads(tensors, max_norm: float, out=None):
     """Scales the tensors of a gradient, in place or into those of `out`, by max_norm / norm where their norm
     exceeds max_norm; a norm that is not finite scales nothing.  Returns the norm before."""
     return _tensors.clip_grads(tensors, max_norm, out)
+
+
+def mx4_quantize(x, out=None) -> Mx4:
+    """x [rows, cols] in blocks of 32 columns, each with a power of two as its scale and 4 bits an element:
+    the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale, with a sign.  A block with NaN or infinity is NaN.
+    `out` (an Mx4 of that shape) takes it."""
+    return Mx4(*_tensors.mx4_quantize(x, out))
+
+
+def mx4_dequantize(q: Mx4, dtype=None, out=None):
+    """What q stands for, [rows, cols] of the type dtype (fp32, if neither it nor `out` says another)."""
+    return _tensors.mx4_dequantize(q, dtype, out)
+
+
+def mx4_linear(x, weight: Mx4, bias=None, dtype=None, out=None):
+    """The product of x [rows, cols], put into 4 bits as mx4_quantize does, with the transpose of weight [words, cols], plus
+    bias [words] (of the result's type, or fp32): [rows, words] of the type dtype (x's, if neither it nor `out` says
+    another).  For scoring: there is no backward pass; mx4_dequantize gives the weights that one would need."""
+    return _tensors.mx4_linear(x, weight, bias, dtype, out)
+
+
+def dropout(x, p: float, seed: int, step=0, first_row: int = 0, residual=None, out=None):
+    """x [rows, cols] with elements dropped with probability p, the others times 1 / (1 - p), plus residual.  Which ones depends on
+    seed (64 bits), step and an element's row (first_row is the number of x's first) and column alone, so nothing is kept for
+    the backward pass.  step: a number below 2^32, or an int64 tensor of one entry on the GPU, read when the kernel runs (a
+    captured graph that counts it up draws another mask at each replay).  `out` (x or residual, for instance) takes the result."""
+    return _tensors.dropout(x, p, seed, step, first_row, residual, out)
+
+
+def dropout_backward(grad_y, p: float, seed: int, step=0, first_row: int = 0, out=None):
+    """The gradient of dropout's x, for the gradient grad_y of its result and the same p, seed, step and first_row; that of its
+    residual is grad_y itself.  `out` (grad_y, for instance) takes it."""
+    return _tensors.dropout(grad_y, p, seed, step, first_row, None, out)
+
+
+def policy_loss(logprobs, old_logprobs, advantages, weights=None, reference=None, row_ptr=None, low: float = 0.2, high: float = 0.2, kl: float = 0.0,
+                out=None) -> PolicyLoss:
+    """The clipped policy loss of words with log-probabilities logprobs [n_tokens] that were drawn with old_logprobs: the sum over
+    the words of weights (1 / n_tokens each without) times -min(ratio A, clip(ratio, 1 - low, 1 + high) A), ratio = exp(logprobs -
+    old_logprobs), plus kl times exp(d) - d - 1 with d = reference - logprobs; and its gradient for token_logprobs_backward.  The
+    advantages A are the words' own, or with row_ptr (as token_logprobs takes it) those of their rows.  A word of weight 0 and one of no row
+    count for nothing, whatever their numbers are.  `out` (logprobs, for instance) takes the gradient."""
+    return PolicyLoss(*_tensors.policy_loss(logprobs, old_logprobs, advantages, weights, reference, row_ptr, low, high, kl, out))
