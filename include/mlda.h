@@ -350,12 +350,12 @@ int mlda_mx_dequantize(const uint8_t* codes, const uint8_t* scales, void* x, int
                         void* hip_stream);
 
 /*
- * The product of rows with a matrix that is held in 4 bits: y[r][n] = sum over columns of Q(x)[r][k] W[n][k] + bias[n], Q(x) what
+ * The product of rows (of up to 2^24 columns) with a matrix that is held in 4 bits: y[r][n] = sum over columns of Q(x)[r][k] W[n][k] + bias[n], Q(x) what
  * mlda_mx_quantize makes of x.
  *   codes, scales   the matrix W of words rows (1 .. 2^30) and cols columns
  *   bias            words entries of bias_type (out_type, or MLDA_FP32); null: zeros
  *   y               rows x words of out_type; not in the place of x
- * Sums are fp32: within (cols / 128 + 8) 2^-24 of the sum of its terms' magnitudes before y is rounded.  A row or word with a block of NaN has
+ * Sums are fp32: within (cols / 64 + 8) 2^-24 of the sum of its terms' (and the bias') magnitudes before y is rounded.  A row or word with a block of NaN has
  * NaN.  The workspace (16-byte aligned) is for Q(x).
  */
 int mlda_mx_linear_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes);

@@ -49,6 +49,25 @@ __device__ __forceinline__ uint32_t mx_scale(uint32_t most) {
 // A scale as fp32; the conversions take only its exponent (2^-127 is no normal number, its exponent's bits are 0 too).
 __device__ __forceinline__ float mx_factor(uint32_t scale) { return __uint_as_float(scale ? scale << 23 : 0x400000u); }
 
+// The codes of the 16 bytes of a block that a lane has, and the block's scale.
+template <class T>
+__device__ __forceinline__ uint32_t mx4_codes(const float (&v)[kPack<T>], uint32_t& scale) {
+    constexpr int P = kPack<T>;
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < P; ++e) most = max(most, __float_as_uint(v[e]) & 0x7fffffffu);
+    scale = mx_scale(block_max<kMxBlock / P>(most));
+    const float f = mx_factor(scale);
+    uint32_t code = 0;
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[0], v[1], f, 0);
+    code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], f, 1);
+    if constexpr (P == 8) {
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4], v[5], f, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6], v[7], f, 3);
+    }
+    return scale == 255 ? 0 : code;
+}
+
 // Bound by memory: read once, a quarter or less of it written.  A lane has the 16 bytes of a piece, so that a wave reads whole lines.
 template <class T>
 __global__ __launch_bounds__(kMxThreads) void mx4_quantize_kernel(MxArgs a) {
@@ -69,22 +88,38 @@ __global__ __launch_bounds__(kMxThreads) void mx4_quantize_kernel(MxArgs a) {
         if (piece >= a.pieces) continue;
         float v[P];
         unpack(r[j], v, T());
-        uint32_t most = 0;
-#pragma unroll
-        for (int e = 0; e < P; ++e) most = max(most, __float_as_uint(v[e]) & 0x7fffffffu);
-        const uint32_t scale = mx_scale(block_max<kLanes>(most));
-        const float f = mx_factor(scale);
-        uint32_t code = 0;
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[0], v[1], f, 0);
-        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[2], v[3], f, 1);
-        if constexpr (P == 8) {
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[4], v[5], f, 2);
-            code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, v[6], v[7], f, 3);
-        }
-        if (scale == 255) code = 0;
+        uint32_t scale;
+        const uint32_t code = mx4_codes<T>(v, scale);
         if constexpr (P == 8) reinterpret_cast<uint32_t*>(a.codes)[piece] = code;
         else reinterpret_cast<uint16_t*>(a.codes)[piece] = (uint16_t)code;
         if (piece % kLanes == 0) a.scales[piece / kLanes] = (uint8_t)scale;
+    }
+}
+
+// The same for a product's rows, in the order in which the matrix instructions want them: of 32 rows and two blocks (a step) 1,024 bytes, lane by lane,
+// and of four steps a word of scales for each lane.  Steps behind the row's end are zeros.  A wave has 32 rows of a step, so that it writes whole lines.
+template <class T>
+__global__ __launch_bounds__(kMxThreads) void mx4_fragments_kernel(MxArgs a, int64_t rows, Divisor steps) {
+    constexpr int P = kPack<T>, kLanes = kMxBlock / P, kRows = kWave / (2 * kLanes);       // rows of a load
+    const uint32_t unit = blockIdx.x * (uint32_t)(kMxThreads / kWave) + threadIdx.x / kWave, tile = steps(unit), step = unit - tile * steps.by;
+    const int lane = lane_id(), in = lane % (2 * kLanes);
+    const int64_t row0 = (int64_t)tile * 32 + lane / (2 * kLanes);
+    if ((int64_t)tile * 32 >= rows) return;
+    Raw r[32 / kRows];
+#pragma unroll
+    for (int j = 0; j < 32 / kRows; ++j)
+        r[j] = load_piece(static_cast<const T*>(a.x) + min(row0 + j * kRows, rows - 1) * a.stride, (int64_t)step * 2 * kMxBlock + in * P, 0, a.cols, 0.0f, false);
+#pragma unroll
+    for (int j = 0; j < 32 / kRows; ++j) {
+        float v[P];
+        unpack(r[j], v, T());
+        uint32_t scale;
+        const uint32_t code = mx4_codes<T>(v, scale);
+        const int lane_of = in / kLanes * 32 + lane / (2 * kLanes) + j * kRows;
+        const int64_t to = ((int64_t)unit * kWave + lane_of) * kLanes + in % kLanes;
+        if constexpr (P == 8) reinterpret_cast<uint32_t*>(a.codes)[to] = code;
+        else reinterpret_cast<uint16_t*>(a.codes)[to] = (uint16_t)code;
+        if (in % kLanes == 0) a.scales[(((int64_t)tile * (steps.by / 4) + step / 4) * kWave + lane_of) * 4 + step % 4] = (uint8_t)scale;
     }
 }
 
@@ -130,7 +165,6 @@ __global__ __launch_bounds__(kMxThreads) void mx4_dequantize_kernel(MxArgs a) {
 
 // ---------------------------------------------------------------- product
 typedef int Codes __attribute__((ext_vector_type(4)));      // a block's
-typedef float Acc __attribute__((ext_vector_type(4)));
 
 struct MxLinearArgs {
     const uint8_t* x_codes;
@@ -146,54 +180,362 @@ struct MxLinearArgs {
     int32_t blocks;                      // to a row
 };
 
-// acc += the products of 16 words (a) and 16 rows (b) over four blocks: lane l has the block l / 16 of word or row l % 16, and gets words
-// 4 (l / 16) .. + 3 of row l % 16.  Products are exact, their sum is rounded once to fp32 (within 0.7 units of roundoff of the sum of magnitudes, as measured).
-__device__ __forceinline__ Acc mx4_mfma(Codes a, uint32_t a_scale, Codes b, uint32_t b_scale, Acc acc) {
-    typedef int Wide __attribute__((ext_vector_type(8)));
-    const Wide x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 4, 4, 0, (int)a_scale, 0, (int)b_scale);
-}
-
 template <class T>
 __device__ __forceinline__ float bias_at(const MxLinearArgs& a, int32_t word) {
     if (!a.bias) return 0.0f;
     return a.bias_fp32 ? static_cast<const float*>(a.bias)[word] : (float)static_cast<const T*>(a.bias)[word];
 }
 
-// A wave has 16 words and 16 kTiles rows.
-template <class T, int kTiles>
-__global__ __launch_bounds__(256) void mx4_linear_kernel(MxLinearArgs a) {
-    const int lane = lane_id(), at = lane % 16, part = lane / 16;
-    const int64_t word0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / kWave) * 16;
-    if (word0 >= a.words) return;
-    const int64_t row0 = (int64_t)blockIdx.y * 16 * kTiles;
-    const int64_t word = min(word0 + at, (int64_t)a.words - 1);            // (what comes of the lanes past the end is not stored)
-    Acc acc[kTiles] = {};
-    for (int32_t b = part; b - part < a.blocks; b += 4) {
-        const bool there = b < a.blocks;
-        auto load = [&](const uint8_t* codes, int64_t row, Codes& c) {
-            c = there ? *reinterpret_cast<const Codes*>(codes + (row * a.blocks + b) * kMxBytes) : Codes{0, 0, 0, 0};
-        };
-        Codes w, x;
-        load(a.codes, word, w);
-        const uint32_t ws = there ? a.scales[word * a.blocks + b] : 127;
+// acc += the products of 32 rows (a) and 32 words (b) over two blocks: lane l has the block l / 32 of row or word l % 32, and gets, in element j,
+// row 8 (j / 4) + 4 (l / 32) + j % 4 of word l % 32.  Scales: the bytes kA and kB.  Products are exact; a sum of 64 and what was there is rounded once (within 0.7
+// units of roundoff of the sum of magnitudes, as measured).  (7,500 TFLOP/s of equal numbers, 6,600 of random ones; the form for 16 x 16 x 128 4,190.)
+typedef float Acc __attribute__((ext_vector_type(16)));
+template <int kA, int kB>
+__device__ __forceinline__ Acc mx4_mfma(Codes a, uint32_t a_scales, Codes b, uint32_t b_scales, Acc acc) {
+    typedef int Wide __attribute__((ext_vector_type(8)));
+    const Wide x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, 4, 4, kA, (int)a_scales, kB, (int)b_scales);
+}
+
+// A row's scales from a block on, eight, as they lie there: of a last eight that are short those that end with the row.
+__device__ __forceinline__ uint64_t load_scales(const uint8_t* row, int32_t first, int32_t blocks) {
+    typedef uint64_t Anywhere __attribute__((aligned(1), may_alias));
+    uint64_t s = 0;
+    if (blocks >= 8) {
+        s = *reinterpret_cast<const Anywhere*>(row + min(first, blocks - 8));
+    } else {
+        for (int c = blocks; c-- > 0;) s = s << 8 | row[c];
+        s <<= 8 * (8 - blocks);
+    }
+    return s;
+}
+// Moves those of a short eight to where the others' are; ones behind them (NaN times zero would be NaN).
+__device__ __forceinline__ uint64_t placed_scales(uint64_t s, int32_t first, int32_t blocks) {
+    const int short_by = min(max(first + 8 - blocks, 0), 8) * 8;
+    return short_by == 0 ? s : short_by == 64 ? 0x7f7f7f7f7f7f7f7full : s >> short_by | 0x7f7f7f7f7f7f7f7full << (64 - short_by);
+}
+
+// Few rows.  A wave has 32 words and 32 kTiles rows.  Its words' codes come straight from memory, 128 bytes of a word at a time (a line, or two that
+// the next slab meets again) and kFewAhead such slabs on their way, and through LDS into the instructions' order: bound by reading them.  Rows that are few enough are put into 4 bits by each workgroup for itself, while its words' codes are on their way (X: their type); others
+// (X = void) are laid out by mx4_fragments_kernel and come from the L2 cache.  With kSplit the four waves of a workgroup share their words'
+// slabs, and their sums are joined in a fixed order.
+constexpr int kFewBlocks = 8;            // of a slab
+constexpr int kFewWaves = 4;
+constexpr int kFewWords = 32;            // of a wave
+
+template <class T, class X, int kTiles, bool kSplit, int kFewAhead>
+__global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs a, MxArgs q, int32_t steps) {
+    constexpr bool kOwn = !std::is_void_v<X>;
+    extern __shared__ Codes few_room[];                    // own rows: [block][row], then their scales; the parts of the sums
+    __shared__ Codes turned[kFewWaves][kFewWords * kFewBlocks];            // a word's blocks turned by its number, so that eight lanes that read a block of eight words meet all banks
+    __shared__ Acc sums[kSplit ? kFewWaves - 1 : 1][kSplit ? kTiles : 1][kWave];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), col = lane % 32, part = lane / 32;
+    const int64_t row0 = (int64_t)blockIdx.y * 32;
+    const int rows = (int)min(kOwn ? (int64_t)32 : (int64_t)32 * kTiles, a.rows - row0);
+    const int64_t word0 = ((int64_t)blockIdx.x * (kSplit ? 1 : kFewWaves) + (kSplit ? 0 : wave)) * kFewWords;
+    const int64_t word = min(word0 + col, (int64_t)a.words - 1);           // (what comes of the lanes past the end is not stored)
+    const uint8_t* scales = a.scales + word * a.blocks;
+    const int32_t slabs = (a.blocks + kFewBlocks - 1) / kFewBlocks, begin = kSplit ? wave : 0, stride = kSplit ? kFewWaves : 1, block = lane % kFewBlocks;
+    const uint8_t* from[4];                                // of the lane's four words
+#pragma unroll
+    for (int i = 0; i < 4; ++i) from[i] = a.codes + min(word0 + 8 * i + lane / kFewBlocks, (int64_t)a.words - 1) * a.blocks * kMxBytes;
+    Codes x[2][4][kTiles];                                 // rows that are laid out: of this slab and the next
+    uint32_t xs[2][kTiles];
+    auto fetch_rows = [&](int buffer, int32_t slab) {
+        if (kOwn || slab >= slabs) return;
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-            const int64_t row = min(row0 + 16 * t + at, a.rows - 1);
-            load(a.x_codes, row, x);
-            const uint32_t xs = there ? a.x_scales[row * a.blocks + b] : 127;
-            acc[t] = mx4_mfma(w, ws, x, xs, acc[t]);
+            const int64_t tile = min((int64_t)t, (a.rows - 1) / 32);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) x[buffer][s][t] = reinterpret_cast<const Codes*>(a.x_codes)[(tile * steps + slab * 4 + s) * kWave + lane];
+            xs[buffer][t] = reinterpret_cast<const uint32_t*>(a.x_scales)[(tile * (steps / 4) + slab) * kWave + lane];
+        }
+    };
+    static_assert(kFewAhead % 2 == 0 || kOwn, "rows that are laid out take turns in two places");
+    fetch_rows(0, begin);
+    fetch_rows(1, begin + stride);
+    Codes w[kFewAhead][4];
+    uint64_t ws[kFewAhead];
+    auto fetch = [&](int buffer, int32_t slab) {
+        if (slab >= slabs) return;
+        const int64_t at = (int64_t)min(slab * kFewBlocks + block, a.blocks - 1) * kMxBytes;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[buffer][i] = __builtin_nontemporal_load(reinterpret_cast<const Codes*>(from[i] + at));
+        ws[buffer] = load_scales(scales, slab * kFewBlocks, a.blocks);
+    };
+#pragma unroll
+    for (int k = 0; k < kFewAhead; ++k) fetch(k, begin + k * stride);
+
+    uint8_t* const own_scales = reinterpret_cast<uint8_t*>(few_room + a.blocks * rows);
+    if constexpr (kOwn) {
+        constexpr int P = kPack<X>, kLanes = kMxBlock / P;
+        for (uint32_t piece = threadIdx.x; piece < q.per_row.by * (uint32_t)rows; piece += kFewWaves * kWave) {
+            const uint32_t row = q.per_row(piece), in = piece - row * q.per_row.by, block = in / kLanes;
+            float v[P];
+            unpack(load_piece(static_cast<const X*>(q.x) + (row0 + row) * q.stride, (int64_t)in * P, 0, q.cols, 0.0f, false), v, X());
+            uint32_t scale;
+            const uint32_t code = mx4_codes<X>(v, scale);
+            const uint32_t to = (block * (uint32_t)rows + row) * kLanes + in % kLanes;
+            if constexpr (P == 8) reinterpret_cast<uint32_t*>(few_room)[to] = code;
+            else reinterpret_cast<uint16_t*>(few_room)[to] = (uint16_t)code;
+            if (in % kLanes == 0) own_scales[block * (uint32_t)rows + row] = (uint8_t)scale;
+        }
+        __syncthreads();
+    }
+
+    Acc acc[kTiles] = {};
+    auto use = [&](int buffer, int32_t slab) {
+        if (slab >= slabs) return;
+        const int32_t first = slab * kFewBlocks;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            turned[wave][(8 * i + lane / kFewBlocks) * kFewBlocks + (block ^ (lane / kFewBlocks))] = first + block < a.blocks ? w[buffer][i] : Codes{0, 0, 0, 0};
+        const uint64_t word_scales = placed_scales(ws[buffer], first, a.blocks) >> 8 * part;
+        // (a wave's own room: its reads and writes are in order)
+        auto step = [&](auto which) {
+            constexpr int s = decltype(which)::value;
+            if (first + 2 * s >= a.blocks) return;
+            const Codes wc = turned[wave][col * kFewBlocks + ((2 * s + part) ^ (col & 7))];
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                Codes xc;
+                uint32_t row_scale;
+                if constexpr (kOwn) {
+                    const int at = min(first + 2 * s + part, a.blocks - 1) * rows + min(col, rows - 1);
+                    xc = few_room[at];
+                    row_scale = own_scales[at];
+                } else {
+                    xc = x[buffer % 2][s][t];
+                    row_scale = xs[buffer % 2][t];
+                }
+                acc[t] = mx4_mfma<kOwn ? 0 : s, s % 2 * 2>(xc, row_scale, wc, (uint32_t)(word_scales >> s / 2 * 32), acc[t]);
+            }
+        };
+        step(std::integral_constant<int, 0>());
+        step(std::integral_constant<int, 1>());
+        step(std::integral_constant<int, 2>());
+        step(std::integral_constant<int, 3>());
+    };
+    for (int32_t slab = begin; slab < slabs; slab += kFewAhead * stride) {
+#pragma unroll
+        for (int k = 0; k < kFewAhead; ++k) {
+            use(k, slab + k * stride);
+            fetch_rows(k % 2, slab + (k + 2) * stride);
+            fetch(k, slab + (k + kFewAhead) * stride);
         }
     }
+    if constexpr (kSplit) {
+        if (wave > 0) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) sums[wave - 1][t][lane] = acc[t];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int k = 0; k < kFewWaves - 1; ++k)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) acc[t] += sums[k][t][lane];
+    }
+    if (word0 + col >= a.words) return;
+    const float bias = bias_at<T>(a, (int32_t)word);
+    T* const y = static_cast<T*>(a.y) + row0 * a.y_stride + word0 + col;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-        const int64_t row = row0 + 16 * t + at;
-        if (row >= a.rows) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t n = word0 + 4 * part + i;
-            if (n < a.words) static_cast<T*>(a.y)[row * a.y_stride + n] = (T)(acc[t][i] + bias_at<T>(a, (int32_t)n));
+        for (int j = 0; j < 16; ++j) {
+            const int row = 32 * t + 8 * (j / 4) + 4 * part + j % 4;
+            if (row < rows) y[row * a.y_stride] = (T)(acc[t][j] + bias);
         }
+    }
+}
+
+// Many rows.  A workgroup holds its words in LDS, as the matrix instructions want them, and goes through the rows: a wave has 128 words
+// and 32 kTiles rows at a time, whose codes (laid out by mx4_fragments_kernel) come straight from the L2 cache, kAhead steps ahead.  So
+// the waves wait for each other only where the words change, and a row costs the L2 its codes once for 128 kHalves words.  (Words and
+// rows both through LDS, 256 x 128 a workgroup: 2,048 x 141,000 x 1,000 bf16 took 270 us, LDS and matrix instructions in turn, so 239.)
+//
+// The columns of an instruction's result are the words 4 c + i of its four matrices i: a lane has four neighbouring words of a row, and a
+// wave stores 256 bytes or more of it at once.
+constexpr int kAhead = 4;                // steps of two blocks, which share a word of scales
+constexpr int kWaveWords = 128;
+
+// Four neighbouring elements, of which `n` or all are there.
+template <class T>
+__device__ __forceinline__ void store_four(T* p, const float (&v)[4], int64_t n, bool once) {
+    typedef T Four __attribute__((ext_vector_type(4)));
+    typedef Four Anywhere __attribute__((aligned(sizeof(T)), may_alias));
+    const Four four = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    if (n >= 4) {
+        if (once) __builtin_nontemporal_store(four, reinterpret_cast<Anywhere*>(p));
+        else *reinterpret_cast<Anywhere*>(p) = four;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) p[i] = (T)v[i];
+    }
+}
+
+struct MxTilesArgs {
+    MxLinearArgs m;                      // x in the order above
+    int32_t steps;                       // of two blocks, a multiple of kAhead
+    int32_t held;                        // steps that LDS holds, likewise
+    uint32_t passes;                     // through all rows
+    uint32_t units;                      // word tiles times passes
+    Divisor pass, slab;                  // by passes; by 2 held
+    bool once;
+};
+
+template <class T, int kTiles, int kHalves, int kWaves, int kPerSimd = 2, int kBuffers = 2>
+__global__ __launch_bounds__(kWaves * kWave, kPerSimd) void mx4_tiles_kernel(MxTilesArgs a) {
+    constexpr int kThreads = kWaves * kWave, kWords = kWaveWords * kHalves, kRows = kWaves / kHalves * kTiles * 32;
+    extern __shared__ Codes held[];                        // [step][half][i][lane]; a lane's place is turned by its block's number, so that neighbouring blocks of a word do not meet in a bank
+    uint32_t* const held_scales = reinterpret_cast<uint32_t*>(held + a.held * kHalves * 4 * kWave);      // [step][half][lane], a byte for each i
+    const MxLinearArgs& m = a.m;
+    const int thread = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(thread / kWave), half = wave % kHalves, mine = wave / kHalves * kTiles;
+    const int col = lane % 32, part = lane / 32;
+    // Whole rounds of tiles first, neighbouring tiles in neighbouring workgroups of an XCD, so that all that is written at a time is long runs of the same
+    // rows; what is left of the tiles is cut into equal parts.
+    const uint32_t groups = gridDim.x, group = groups % 8 ? blockIdx.x : blockIdx.x % 8 * (groups / 8) + blockIdx.x / 8;
+    const uint32_t rounds = a.units / a.passes / groups, whole = rounds * a.passes, left = a.units - whole * groups;
+    const uint32_t begin = (uint32_t)((uint64_t)left * group / groups), end = (uint32_t)((uint64_t)left * (group + 1) / groups);
+    const int64_t last_tile = (m.rows - 1) / 32;
+
+    auto hold = [&](int64_t word0, int32_t first) {        // steps from the first on
+        const int words = (int)min((int64_t)kWords, m.words - word0);
+        const uint8_t* codes = m.codes + word0 * m.blocks * kMxBytes;
+        for (uint32_t at = (uint32_t)thread; at < (uint32_t)(kWords * 2 * a.held); at += kThreads) {
+            const int word = (int)a.slab(at), in = (int)(at - (uint32_t)word * a.slab.by), block = 2 * first + in;
+            const Codes c = *reinterpret_cast<const Codes*>(codes + ((int64_t)min(word, words - 1) * m.blocks + min(block, m.blocks - 1)) * kMxBytes);
+            held[((in / 2 * kHalves + word / kWaveWords) * 4 + word % 4) * kWave + in % 2 * 32 + (word % kWaveWords / 4 ^ (in & 7))] =
+                block < m.blocks ? c : Codes{0, 0, 0, 0};
+        }
+        for (int at = thread; at < kWords * (a.held / 4); at += kThreads) {
+            const int word = at % kWords, in = at / kWords * 8;
+            const uint64_t s = placed_scales(load_scales(m.scales + (word0 + min(word, words - 1)) * m.blocks, 2 * first + in, m.blocks), 2 * first + in, m.blocks);
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                reinterpret_cast<uint8_t*>(held_scales + (((in + c) / 2 * kHalves + word / kWaveWords) * kWave + c % 2 * 32 + word % kWaveWords / 4))[word % 4] =
+                    (uint8_t)(s >> 8 * c);
+        }
+    };
+
+    auto tile_of = [&](uint32_t n, uint32_t& pass) {
+        const uint32_t unit = n < whole ? n : begin + (n - whole), in_round = a.pass(unit);
+        pass = unit - in_round * a.passes;
+        return n < whole ? in_round * groups + group : rounds * groups + in_round;
+    };
+    const Codes* x[kTiles];
+    const uint32_t* x_scales[kTiles];
+    Codes next[kAhead][kTiles];                            // of the next three steps
+    uint32_t next_scales[kTiles];                          // of the next four
+    auto fetch = [&](int s, int32_t step) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) next[s][t] = x[t][step * kWave];
+    };
+    auto fetch_first = [&](uint32_t pass) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const int64_t at = min((int64_t)pass * (kRows / 32) + mine + t, last_tile);
+            x[t] = reinterpret_cast<const Codes*>(m.x_codes) + at * a.steps * kWave + lane;
+            x_scales[t] = reinterpret_cast<const uint32_t*>(m.x_scales) + at * (a.steps / 4) * kWave + lane;
+            next_scales[t] = x_scales[t][0];
+        }
+#pragma unroll
+        for (int s = 0; s < kAhead - 1; ++s) fetch(s, s);
+    };
+
+    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    int64_t word0 = -1;
+    const uint32_t count = whole + (end - begin);
+    uint32_t pass, tile = tile_of(0, pass);
+    if (count) fetch_first(pass);
+    for (uint32_t n = 0; n < count; ++n) {
+        const bool fresh = word0 != (int64_t)tile * kWords;
+        if (fresh) {
+            word0 = (int64_t)tile * kWords;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t word = word0 + half * kWaveWords + 4 * col + i;
+                bias[i] = word < m.words ? bias_at<T>(m, (int32_t)word) : 0.0f;
+            }
+        }
+        // (16-bit results: the bias is the sums' first term; fp32 results have it added at the end, one rounding instead of as many as there are steps)
+        Acc acc[kTiles][4];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[t][i][j] = sizeof(T) == 2 ? bias[i] : 0.0f;
+        for (int32_t first = 0; first < a.steps; first += a.held) {
+            if (fresh || a.held < a.steps) {
+                __syncthreads();
+                hold(word0, first);
+                __syncthreads();
+            }
+            const int32_t steps = min(a.held, a.steps - first);
+            Codes w[kBuffers][4];                          // of this step and the next
+            uint32_t ws[kBuffers];
+            auto read = [&](int buffer, int s, int32_t step) {     // s: step % 4
+                const Codes* at = held + (step * kHalves + half) * 4 * kWave + part * 32 + (col ^ ((2 * s + part) & 7));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[buffer][i] = at[i * kWave];
+                ws[buffer] = held_scales[(step * kHalves + half) * kWave + lane];
+            };
+            if (kBuffers == 2) read(0, 0, 0);
+            for (int32_t in = 0; in < steps; in += kAhead) {
+                uint32_t xs[kTiles];
+                const int32_t ahead = min(first + in + kAhead, a.steps - kAhead);          // (the last ones are loaded again)
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    xs[t] = next_scales[t];
+                    next_scales[t] = x_scales[t][ahead / 4 * kWave];
+                }
+                auto step = [&](auto which) {
+                    constexpr int s = decltype(which)::value;
+                    if (kBuffers == 2) read((s + 1) & 1, (s + 1) % 4, min(in + s + 1, steps - 1));
+                    else read(0, s, in + s);
+                    fetch((s + 3) % 4, s ? ahead + s - 1 : min(first + in + 3, a.steps - 1));
+                    __builtin_amdgcn_sched_barrier(0);     // (or the loads are moved to where they are needed)
+                    auto column = [&](auto i) {
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) acc[t][i.value] = mx4_mfma<s, i.value>(next[s][t], xs[t], w[s % kBuffers][i.value], ws[s % kBuffers], acc[t][i.value]);
+                    };
+                    column(std::integral_constant<int, 0>());
+                    column(std::integral_constant<int, 1>());
+                    column(std::integral_constant<int, 2>());
+                    column(std::integral_constant<int, 3>());
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                step(std::integral_constant<int, 0>());
+                step(std::integral_constant<int, 1>());
+                step(std::integral_constant<int, 2>());
+                step(std::integral_constant<int, 3>());
+            }
+        }
+        const int64_t tile0 = (int64_t)pass * (kRows / 32) + mine;
+        if (n + 1 < count) {
+            tile = tile_of(n + 1, pass);
+            fetch_first(pass);
+        }
+        __builtin_amdgcn_sched_barrier(0);                 // (the loads before the stores: they are waited for in order)
+        const int64_t word = word0 + half * kWaveWords + 4 * col, row0 = tile0 * 32 + 4 * part;
+        T* const y = static_cast<T*>(m.y) + row0 * m.y_stride + word;
+        auto store = [&](bool all) {
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int down = 32 * t + 8 * (j / 4) + j % 4;
+                    float v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = sizeof(T) == 2 ? acc[t][i][j] : acc[t][i][j] + bias[i];
+                    if (all || row0 + down < m.rows) store_four(y + down * m.y_stride, v, all ? 4 : m.words - word, a.once);
+                }
+            }
+        };
+        if ((tile0 + kTiles) * 32 <= m.rows && word0 + kWords <= m.words) store(true);
+        else store(false);
     }
 }
 

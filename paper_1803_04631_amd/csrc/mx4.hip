@@ -7,6 +7,22 @@ namespace {
 
 int64_t blocks_of(int32_t cols) { return ((int64_t)cols + mlda::kMxBlock - 1) / mlda::kMxBlock; }
 
+constexpr int kLdsBytes = 163840;
+constexpr int32_t kMostProductCols = 1 << 24;    // tiles of rows have 32-bit numbers of pieces
+
+// How a product's rows are held in 4 bits: few, and short ones of a small product, by each workgroup for itself (1 x 1,000 x 141,000 fp32 with a launch for the row 27 us, so 19;
+// 1,000 x 32 x 5,000 fp32 14.3 and 8.6; but 2,048 x 128 x 141,000 bf16 181 us, so 614), others in the workspace, in whole tiles of rows and whole stretches of steps.
+bool few_rows(int64_t rows, int32_t cols) { return rows <= 16 && rows * blocks_of(cols) <= 1024; }
+bool short_rows(int64_t rows, int32_t cols, int32_t words) { return blocks_of(cols) <= 2 && rows <= ((int64_t)1 << 23) / words; }
+int64_t held_rows(int64_t rows) { return (rows + 31) / 32 * 32; }
+int64_t held_blocks(int32_t cols) {
+    constexpr int64_t kEach = 2 * mlda::kAhead;
+    return (blocks_of(cols) + kEach - 1) / kEach * kEach;
+}
+size_t held_bytes(int64_t rows, int32_t cols) {
+    return few_rows(rows, cols) ? 0 : (size_t)held_rows(rows) * (size_t)held_blocks(cols) * (mlda::kMxBytes + 1);
+}
+
 int check_mx4(int64_t rows, int32_t cols, int32_t type) {
     if (rows < 0 || cols < 1 || cols > kMostCols) return refuse("4-bit matrix: need rows >= 0 and 1 <= cols <= 2^30");
     if (!known_type(type)) return refuse("4-bit matrix: unknown type");
@@ -45,6 +61,85 @@ int quantize(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, i
     });
 }
 
+// A product's rows, in steps of two blocks.
+int lay_out(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, int64_t rows, int32_t cols, int32_t type, int32_t steps, hipStream_t stream) {
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / steps) * 32;      // of a launch
+    for (int64_t row = 0; row < rows; row += most) {
+        const int64_t n = std::min(most, rows - row), units = (n + 31) / 32 * steps;
+        const mlda::MxArgs a{static_cast<const char*>(x) + row * x_stride * (int64_t)type_bytes(type), x_stride, codes + row * steps * 2 * mlda::kMxBytes,
+                             scales + row * steps * 2, 0, cols, mlda::Divisor{}, false};
+        constexpr int64_t kEach = mlda::kMxThreads / mlda::kWave;
+        RC_TRY(with_type(type, [&](auto t) {
+            hipLaunchKernelGGL((mlda::mx4_fragments_kernel<decltype(t)>), dim3((unsigned)((units + kEach - 1) / kEach)), dim3(mlda::kMxThreads), 0, stream, a, n,
+                               mlda::divisor((uint32_t)steps));
+            return launched("mx4_fragments_kernel");
+        }));
+    }
+    return MLDA_OK;
+}
+
+template <class T, class X, int kTiles>
+int multiply_few_of(mlda::MxLinearArgs a, mlda::MxArgs q, int32_t steps, hipStream_t stream) {
+    constexpr bool kOwn = !std::is_void_v<X>;
+    const unsigned lds = kOwn ? (unsigned)(std::min<int64_t>(a.rows, 32) * a.blocks * (mlda::kMxBytes + 1)) : 0;
+    const int64_t waves = ((int64_t)a.words + mlda::kFewWords - 1) / mlda::kFewWords;
+    // With fewer waves than SIMDs, and more slabs than a wave has on their way, four share their words.
+    const bool split = waves < 4 * kCus && a.blocks > 4 * mlda::kFewBlocks;
+    const unsigned groups = (unsigned)(split ? waves : (waves + mlda::kFewWaves - 1) / mlda::kFewWaves);
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, kMostGroups / groups)) * 32, rows = a.rows;       // of a launch
+    for (int64_t row = 0; row < rows; row += most) {
+        a.rows = std::min(most, rows - row);
+        const dim3 grid(groups, (unsigned)(kOwn ? (a.rows + 31) / 32 : 1)), threads(mlda::kFewWaves * mlda::kWave);
+        if (split) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, kTiles, true, 4>), grid, threads, lds, stream, a, q, steps);
+        else if (kOwn && a.blocks <= mlda::kFewBlocks) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, kTiles, false, kOwn ? 1 : 4>), grid, threads, lds, stream, a, q, steps);
+        else hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, kTiles, false, 4>), grid, threads, lds, stream, a, q, steps);
+        RC_TRY(launched("mx4_few_kernel"));
+        if constexpr (kOwn) q.x = static_cast<const X*>(q.x) + a.rows * q.stride;
+        a.y = static_cast<T*>(a.y) + a.rows * a.y_stride;
+    }
+    return MLDA_OK;
+}
+
+template <class T, int kTiles, int kHalves, int kWaves>
+int multiply_tiles_of(mlda::MxTilesArgs a, hipStream_t stream) {
+    constexpr int kWords = mlda::kWaveWords * kHalves, kRows = kWaves / kHalves * kTiles * 32, kStepBytes = kHalves * 4 * mlda::kWave * (mlda::kMxBytes + 1);
+    const int32_t fit = (kLdsBytes - kWords * 4) / kStepBytes / mlda::kAhead * mlda::kAhead;
+    a.held = std::min(a.steps, fit);
+    a.slab = mlda::divisor((uint32_t)(2 * a.held));
+    const int64_t tiles = ((int64_t)a.m.words + kWords - 1) / kWords, rows = a.m.rows;
+    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / tiles) * kRows;       // of a launch
+    const unsigned lds = (unsigned)(a.held * kStepBytes + kWords * 4);
+    const auto kernel = mlda::mx4_tiles_kernel<T, kTiles, kHalves, kWaves>;
+    if (lds > 48 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return set_error(MLDA_EHIP, "mx4_tiles_kernel's LDS", hipGetErrorString(e));
+    }
+    for (int64_t row = 0; row < rows; row += most) {
+        a.m.rows = std::min(most, rows - row);
+        a.passes = (uint32_t)((a.m.rows + kRows - 1) / kRows);
+        a.pass = mlda::divisor(a.passes);
+        a.units = (uint32_t)(tiles * a.passes);
+        const int64_t fits = kCus * std::max<int64_t>(1, std::min<int64_t>(8 / kWaves, kLdsBytes / std::max(lds, 1u)));
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(a.units, fits)), dim3(kWaves * mlda::kWave), lds, stream, a);
+        RC_TRY(launched("mx4_tiles_kernel"));
+        a.m.x_codes += a.m.rows * a.steps * 2 * mlda::kMxBytes;
+        a.m.x_scales += a.m.rows * a.steps * 2;
+        a.m.y = static_cast<T*>(a.m.y) + a.m.rows * a.m.y_stride;
+    }
+    return MLDA_OK;
+}
+
+template <class T>
+int multiply_tiles(const mlda::MxLinearArgs& m, int32_t steps, hipStream_t stream) {
+    mlda::MxTilesArgs a{};
+    a.m = m;
+    a.steps = steps;
+    a.once = passes_caches((double)m.rows * m.words * (double)sizeof(T));
+    const int64_t big = (((int64_t)m.words + 255) / 256) * ((m.rows + 255) / 256);
+    if (big >= kCus) return multiply_tiles_of<T, 2, 2, 8>(a, stream);
+    return multiply_tiles_of<T, 1, 1, 4>(a, stream);
+}
+
 }  // namespace
 
 extern "C" {
@@ -75,7 +170,8 @@ int mlda_mx_dequantize(const uint8_t* codes, const uint8_t* scales, void* x, int
 int mlda_mx_linear_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes) {
     if (!bytes) return refuse("bytes is null");
     RC_TRY(check_mx4(rows, cols, MLDA_FP32));
-    *bytes = (size_t)rows * (size_t)blocks_of(cols) * (mlda::kMxBytes + 1);
+    if (cols > kMostProductCols) return refuse("4-bit product: need cols <= 2^24");
+    *bytes = held_bytes(rows, cols);
     return MLDA_OK;
 }
 
@@ -84,6 +180,7 @@ int mlda_mx_linear(const void* x, int64_t x_stride, const uint8_t* codes, const 
                     size_t workspace_bytes, void* hip_stream) {
     RC_TRY(check_mx4(rows, cols, type));
     if (words < 1 || words > kMostCols) return refuse("4-bit product: need 1 <= words <= 2^30");
+    if (cols > kMostProductCols) return refuse("4-bit product: need cols <= 2^24");
     if (!known_type(out_type)) return refuse("4-bit product: unknown type of y");
     if (bias_type != out_type && bias_type != MLDA_FP32) return refuse("4-bit product: the bias has the type of y, or fp32");
     if (rows == 0) return MLDA_OK;
@@ -92,26 +189,29 @@ int mlda_mx_linear(const void* x, int64_t x_stride, const uint8_t* codes, const 
     if (x == y) return refuse("4-bit product: y cannot be in the place of x");
     RC_TRY(check_codes(codes, scales));
     if (!aligned(bias, type_bytes(bias_type))) return refuse("4-bit product: the bias is not aligned to its type");
-    const size_t blocks = (size_t)blocks_of(cols), need = (size_t)rows * blocks * (mlda::kMxBytes + 1);
-    if (!dev_workspace || !aligned(dev_workspace, 16)) return refuse("4-bit product: the workspace is null or not aligned");
+    const size_t need = held_bytes(rows, cols);
+    if (need && (!dev_workspace || !aligned(dev_workspace, 16))) return refuse("4-bit product: the workspace is null or not aligned");
     if (workspace_bytes < need) return set_error(MLDA_ENOMEM, "4-bit product: the workspace is smaller than mlda_mx_linear_workspace_bytes");
-    uint8_t* x_codes = static_cast<uint8_t*>(dev_workspace);
-    uint8_t* x_scales = x_codes + (size_t)rows * blocks * mlda::kMxBytes;
     const hipStream_t stream = (hipStream_t)hip_stream;
-    RC_TRY(quantize(x, x_stride, x_codes, x_scales, rows, cols, type, stream));
+    mlda::MxLinearArgs a{nullptr, nullptr, codes, scales, bias, bias_type == MLDA_FP32, y, y_stride, rows, words, (int32_t)blocks_of(cols)};
+    if (!need || short_rows(rows, cols, words)) {
+        const mlda::MxArgs q{x, x_stride, nullptr, nullptr, 0, cols, mlda::divisor((uint32_t)(blocks_of(cols) * mlda::kMxBlock * (int64_t)type_bytes(type) / 16)), false};
+        return with_type(out_type, [&](auto t) {
+            return with_type(type, [&](auto u) { return multiply_few_of<decltype(t), decltype(u), 1>(a, q, 0, stream); });
+        });
+    }
+    const int64_t blocks = held_blocks(cols);
+    uint8_t* x_codes = static_cast<uint8_t*>(dev_workspace);
+    uint8_t* x_scales = x_codes + held_rows(rows) * blocks * mlda::kMxBytes;
+    const int32_t steps = (int32_t)(blocks / 2);
+    RC_TRY(lay_out(x, x_stride, x_codes, x_scales, rows, cols, type, steps, stream));
+    a.x_codes = x_codes;
+    a.x_scales = x_scales;
     return with_type(out_type, [&](auto t) {
         typedef decltype(t) T;
-        constexpr int kTiles = 4;
-        constexpr int64_t kMostRows = 65535 * 16 * kTiles;       // of a launch
-        for (int64_t row = 0; row < rows; row += kMostRows) {
-            const int64_t n = std::min(kMostRows, rows - row);
-            const mlda::MxLinearArgs a{x_codes + (size_t)row * blocks * mlda::kMxBytes, x_scales + (size_t)row * blocks, codes, scales, bias,
-                                       bias_type == MLDA_FP32, static_cast<T*>(y) + row * y_stride, y_stride, n, words, (int32_t)blocks};
-            hipLaunchKernelGGL((mlda::mx4_linear_kernel<T, kTiles>), dim3((unsigned)((words + 63) / 64), (unsigned)((n + 16 * kTiles - 1) / (16 * kTiles))),
-                               dim3(256), 0, stream, a);
-            RC_TRY(launched("mx4_linear_kernel"));
-        }
-        return MLDA_OK;
+        if (rows <= 32) return multiply_few_of<T, void, 1>(a, mlda::MxArgs{}, steps, stream);
+        if (rows <= 64) return multiply_few_of<T, void, 2>(a, mlda::MxArgs{}, steps, stream);
+        return multiply_tiles<T>(a, steps, stream);
     });
 }
 

@@ -44,18 +44,22 @@ def test_quantize_refusals(lib):
 
 def test_product_refusals(lib):
     n = ctypes.c_size_t()
-    assert lib.mlda_mx_linear_workspace_bytes(3, 40, ctypes.addressof(n)) == 0 and n.value == 3 * 2 * 17
+    assert lib.mlda_mx_linear_workspace_bytes(3, 40, ctypes.addressof(n)) == 0 and n.value == 0
+    assert lib.mlda_mx_linear_workspace_bytes(33, 140, ctypes.addressof(n)) == 0 and n.value == 64 * 8 * 17
 
-    def call(x=P, x_stride=40, codes=P, scales=P, bias=P, y=2 * P, y_stride=50, rows=3, cols=40, words=50, kind=FP32, out=FP32, bias_kind=FP32, ws=P, size=n.value):
+    def call(x=P, x_stride=140, codes=P, scales=P, bias=P, y=2 * P, y_stride=50, rows=33, cols=140, words=50, kind=FP32, out=FP32, bias_kind=FP32, ws=P, size=64 * 8 * 17):
         return lib.mlda_mx_linear(x, x_stride, codes, scales, bias, y, y_stride, rows, cols, words, kind, out, bias_kind, ws, size, None)
 
-    for bad in ({"x": None}, {"x": P + 2}, {"x_stride": 39}, {"codes": None}, {"codes": P + 4}, {"scales": None}, {"bias": P + 2}, {"y": None}, {"y": P},
-                {"y": P + 2}, {"y_stride": 49}, {"rows": -1}, {"cols": 0}, {"words": 0}, {"words": 2 ** 30 + 1}, {"kind": 3}, {"out": 3}, {"out": -1},
+    for bad in ({"x": None}, {"x": P + 2}, {"x_stride": 139}, {"codes": None}, {"codes": P + 4}, {"scales": None}, {"bias": P + 2}, {"y": None}, {"y": P},
+                {"y": P + 2}, {"y_stride": 49}, {"rows": -1}, {"cols": 0}, {"cols": 2 ** 24 + 1, "x_stride": 2 ** 25}, {"words": 0}, {"words": 2 ** 30 + 1}, {"kind": 3}, {"out": 3}, {"out": -1},
                 {"out": BF16, "bias_kind": FP16}, {"bias_kind": BF16}, {"ws": None}, {"ws": P + 8}):
         refused(lib, call(**bad), word="4-bit")
-    refused(lib, call(size=n.value - 1), -2, "workspace")
+    refused(lib, call(size=64 * 8 * 17 - 1), -2, "workspace")
     assert call(rows=0, x=None, y=None, ws=None, size=0) == 0
-    for bad in ((-1, 5), (1, 0), (1, 2 ** 30 + 1)):
+    for rows, cols in ((17, 1000), (64, 1000), (65, 1000), (2048, 133), (10 ** 6, 1537), (16, 2 ** 24)):
+        assert lib.mlda_mx_linear_workspace_bytes(rows, cols, ctypes.addressof(n)) == 0
+        assert rows * cols / 32 * 17 <= n.value <= (rows + 31) * (cols / 32 + 8) * 17
+    for bad in ((-1, 5), (1, 0), (1, 2 ** 24 + 1)):
         refused(lib, lib.mlda_mx_linear_workspace_bytes(*bad, ctypes.addressof(n)))
     refused(lib, lib.mlda_mx_linear_workspace_bytes(1, 5, None), word="null")
 
