@@ -7,13 +7,13 @@
 // A word of weight 0 is none: nothing of it counts, whatever its numbers are.
 //
 // Everything is in fp64: the border is then the same for every way of computing it, the KL term, a difference of nearly equal numbers, keeps
-// its bits, and sums of millions of words theirs.
+// its bits, and sums of millions of words theirs.  Bound by memory all the same: 50e6 words, 20 bytes each, 197 us (one word to a thread at a time 277).  Few words are one workgroup's and one
+// launch; more leave partial sums, which a second launch joins in a fixed order.
 #pragma once
 #include "vec_io.hpp"
 
 namespace mlda {
 
-constexpr int kPolicyThreads = 256;
 constexpr int kPolicyGroups = 1024;      // of a launch at most, each of which leaves three sums
 
 struct PolicyArgs {
@@ -30,67 +30,154 @@ struct PolicyArgs {
     float* grad;
     float* sums;                         // loss, KL term, clipped weight; null: partial sums
     double* partial;
+    bool once;
 };
 
-// The row of a word: the last that begins at or before it.  -1: none.
-__device__ __forceinline__ int64_t row_of(const PolicyArgs& a, int64_t word) {
-    if (a.rows == 0 || word < a.row_ptr[0] || word >= a.row_ptr[a.rows]) return -1;
-    int64_t lo = 0, hi = a.rows - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (a.row_ptr[mid] <= word) lo = mid;
-        else hi = mid - 1;
+// The rows of two words, by a wave: the last that begins at or before each.  64 bounds are looked at at a time.
+__device__ __forceinline__ void rows_of_wave(const int64_t* row_ptr, int64_t rows, int64_t first, int64_t last, int64_t& lo, int64_t& hi) {
+    int64_t a0 = 0, a1 = rows, b0 = 0, b1 = rows;
+    while (a1 - a0 > 1 || b1 - b0 > 1) {
+        const int64_t a_step = (a1 - a0 + kWave - 1) / kWave, b_step = (b1 - b0 + kWave - 1) / kWave;
+        const int64_t a = a0 + lane_id() * a_step, b = b0 + lane_id() * b_step;
+        const int64_t at_a = row_ptr[min(a, rows)], at_b = row_ptr[min(b, rows)];
+        const int a_n = max(__popcll(__ballot(a < a1 && at_a <= first)), 1), b_n = max(__popcll(__ballot(b < b1 && at_b <= last)), 1);
+        a0 += (a_n - 1) * a_step;
+        a1 = min(a1, a0 + a_step);
+        b0 += (b_n - 1) * b_step;
+        b1 = min(b1, b0 + b_step);
     }
-    return lo;
+    lo = a0;
+    hi = max(a0, b0);
 }
 
-template <bool kReference>
-__global__ __launch_bounds__(kPolicyThreads) void policy_kernel(PolicyArgs a) {
-    __shared__ double slots[3][kPolicyThreads / kWave];
+// exp(x) - x - 1 near 0, where the difference would lose bits: the first five terms of x^2 / 2 + x^3 / 6 + ..; what is left out is below 4e-13 of it, as what
+// the difference loses is below 2^-39 of it beyond. 
+constexpr double kKlNear = 0x1p-6;
+__device__ __forceinline__ double kl_near(double x) {
+    double s = __builtin_fma(x, 1.0 / 720.0, 1.0 / 120.0);
+    s = __builtin_fma(x, s, 1.0 / 24.0);
+    s = __builtin_fma(x, s, 1.0 / 6.0);
+    s = __builtin_fma(x, s, 0.5);
+    return x * x * s;
+}
+
+// kPolicyEach: neighbouring words of a thread.  A word is some 300 instructions one after the other: those of a single workgroup have a thread each if they can (330 of
+// them with a KL term 4.9 us by four, 2.8 apart).
+template <int kThreads, int kPolicyEach, bool kReference>
+__global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
+    constexpr int kChunk = kThreads * kPolicyEach;
+    __shared__ double slots[3][kThreads / kWave];
     double loss = 0.0, kl = 0.0, clipped = 0.0;
-    for (int64_t i = (int64_t)blockIdx.x * kPolicyThreads + threadIdx.x; i < a.n; i += (int64_t)gridDim.x * kPolicyThreads) {
-        int64_t at = i;
-        if (a.row_ptr) at = row_of(a, i);
-        const double w = a.weights ? (double)a.weights[i] : a.weight;
-        double grad = 0.0;
-        if (at >= 0 && w != 0.0) {
-            const double l = a.logprobs[i], d = l - (double)a.old[i], advantage = a.advantages[at];
+    const int64_t chunks = (a.n + kChunk - 1) / kChunk;
+    const int64_t begin = chunks * blockIdx.x / gridDim.x, end = chunks * (blockIdx.x + 1) / gridDim.x;
+    for (int64_t chunk = begin; chunk < end; ++chunk) {
+        const int64_t i = chunk * kChunk + threadIdx.x * kPolicyEach;
+        const int64_t wave_first = chunk * kChunk + (int)threadIdx.x / kWave * kWave * kPolicyEach;
+        if (wave_first >= a.n) break;
+        auto load = [&](const float* p, float (&v)[kPolicyEach]) {
+            if constexpr (kPolicyEach == 4) unpack(load_piece(p, i, 0, a.n, 0.0f, a.once), v, float());
+            else v[0] = i < a.n ? p[i] : 0.0f;
+        };
+        float l[kPolicyEach], old[kPolicyEach], ref[kPolicyEach], w32[kPolicyEach], adv[kPolicyEach];
+        bool used[kPolicyEach];
+        load(a.logprobs, l);
+        load(a.old, old);
+        if (kReference) load(a.reference, ref);
+        if (a.weights) load(a.weights, w32);
+        if (a.row_ptr) {
+            const int64_t first = a.rows ? a.row_ptr[0] : 0, last = a.rows ? a.row_ptr[a.rows] : 0;
+            int64_t lo = 0, hi = 0;
+            if (a.rows) rows_of_wave(a.row_ptr, a.rows, wave_first, min(wave_first + kWave * kPolicyEach, a.n) - 1, lo, hi);
+#pragma unroll
+            for (int e = 0; e < kPolicyEach; ++e) used[e] = i + e >= first && i + e < last;
+            if (hi - lo < kWave) {
+                // a lane has the end and the advantage of a row, and every word meets all of them
+                const int64_t mine = lo + min((int64_t)lane_id(), hi - lo);
+                const int64_t ends = a.rows ? a.row_ptr[mine + 1] : 0;
+                const float advantages = a.rows ? a.advantages[mine] : 0.0f;
+                const float at_first = read_lane(advantages, 0);
+#pragma unroll
+                for (int e = 0; e < kPolicyEach; ++e) adv[e] = at_first;
+                const int more = __builtin_amdgcn_readfirstlane((int)(hi - lo));
+                for (int k = 0; k < more; ++k) {
+                    const int64_t bound = (int64_t)(uint32_t)read_lane((int)ends, k) | (int64_t)read_lane((int)(ends >> 32), k) << 32;
+                    const float next = read_lane(advantages, k + 1);
+#pragma unroll
+                    for (int e = 0; e < kPolicyEach; ++e) adv[e] = i + e >= bound ? next : adv[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPolicyEach; ++e) {
+                    int64_t most = hi;
+                    while (lo < most) {
+                        const int64_t mid = (lo + most + 1) >> 1;
+                        if (a.row_ptr[mid] <= i + e) lo = mid;
+                        else most = mid - 1;
+                    }
+                    adv[e] = a.advantages[lo];
+                }
+            }
+        } else {
+            load(a.advantages, adv);
+#pragma unroll
+            for (int e = 0; e < kPolicyEach; ++e) used[e] = i + e < a.n;
+        }
+        float grads[kPolicyEach];
+#pragma unroll
+        for (int e = 0; e < kPolicyEach; ++e) {
+            // (without branches, so that the words' chains of instructions go side by side)
+            const double w = a.weights ? (double)w32[e] : a.weight;
+            const bool counts = used[e] && w != 0.0;
+            const double d = (double)l[e] - (double)old[e], advantage = adv[e];
             const bool over = advantage > 0.0 && d > a.high, under = advantage < 0.0 && d < a.low;
             const double ratio = exp(d);
             double term = -(over ? a.at_high : under ? a.at_low : ratio) * advantage;
-            grad = over || under ? 0.0 : -ratio * advantage;
-            if (over || under) clipped += w;
+            double grad = over || under ? 0.0 : -ratio * advantage;
+            clipped += counts && (over || under) ? w : 0.0;
             if (kReference) {
-                const double e = (double)a.reference[i] - l, more = expm1(e);
-                kl += w * (more - e);
-                term += a.kl * (more - e);
-                grad -= a.kl * more;
+                const double x = (double)ref[e] - (double)l[e], near = kl_near(x), much = exp(x) - 1.0;
+                const bool is_near = fabs(x) < kKlNear;
+                const double part = is_near ? near : much - x;
+                kl += counts ? w * part : 0.0;
+                term += a.kl * part;
+                grad -= a.kl * (is_near ? x + near : much);
             }
-            loss += w * term;
-            grad *= w;
+            loss += counts ? w * term : 0.0;
+            grad = counts ? w * grad : 0.0;
+            grads[e] = (float)grad;
         }
-        a.grad[i] = (float)grad;
+        if constexpr (kPolicyEach == 4) store_piece(a.grad, i, 0, a.n, pack(grads, float()), a.once);
+        else if (i < a.n) a.grad[i] = grads[0];
     }
-    loss = group_sum<kPolicyThreads>(loss, slots[0]);
-    kl = group_sum<kPolicyThreads>(kl, slots[1]);
-    clipped = group_sum<kPolicyThreads>(clipped, slots[2]);
-    if (threadIdx.x == 0) {
-        const double all[3] = {loss, kl, clipped};
-        for (int k = 0; k < 3; ++k) {
-            if (a.sums) a.sums[k] = (float)all[k];
-            else a.partial[3 * blockIdx.x + k] = all[k];
-        }
+    loss = wave_sum(loss);
+    kl = wave_sum(kl);
+    clipped = wave_sum(clipped);
+    if (lane_id() == 0) {
+        slots[0][threadIdx.x / kWave] = loss;
+        slots[1][threadIdx.x / kWave] = kl;
+        slots[2][threadIdx.x / kWave] = clipped;
+    }
+    __syncthreads();
+    const int k = threadIdx.x / kWave;
+    if (k < 3) {
+        const double sum = wave_sum(lane_id() < kThreads / kWave ? slots[k][lane_id()] : 0.0);
+        if (lane_id() > 0) return;
+        if (a.sums) a.sums[k] = (float)sum;
+        else a.partial[k * kPolicyGroups + blockIdx.x] = sum;
     }
 }
 
-__global__ __launch_bounds__(kPolicyThreads) void policy_sums_kernel(const double* partial, int32_t groups, float* sums) {
-    __shared__ double slots[3][kPolicyThreads / kWave];
-    for (int k = 0; k < 3; ++k) {
-        double sum = 0.0;
-        for (int i = (int)threadIdx.x; i < groups; i += kPolicyThreads) sum += partial[3 * i + k];
-        sum = group_sum<kPolicyThreads>(sum, slots[k]);
-        if (threadIdx.x == 0) sums[k] = (float)sum;
-    }
+constexpr int kPolicySumThreads = 3 * kWave;               // a wave for each sum
+
+__global__ __launch_bounds__(kPolicySumThreads) void policy_sums_kernel(const double* partial, int32_t groups, float* sums) {
+    const int k = threadIdx.x / kWave;
+    double part[kPolicyGroups / kWave], v = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPolicyGroups / kWave; ++i) part[i] = partial[k * kPolicyGroups + min(i * kWave + lane_id(), groups - 1)];
+#pragma unroll
+    for (int i = 0; i < kPolicyGroups / kWave; ++i) v += i * kWave + lane_id() < groups ? part[i] : 0.0;
+    v = wave_sum(v);
+    if (lane_id() == 0) sums[k] = (float)v;
 }
 
 }  // namespace mlda

@@ -9,9 +9,16 @@
 
 namespace {
 
-unsigned policy_groups(int64_t n) {
-    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((n + mlda::kPolicyThreads - 1) / mlda::kPolicyThreads, mlda::kPolicyGroups));
+// How the words of a policy loss are dealt out: one workgroup and one launch for few, neighbouring four to a thread beyond.
+struct PolicyForm {
+    int threads, each;
+    unsigned groups;
+};
+PolicyForm policy_form(int64_t n) {
+    if (n <= 4096) return {1024, n <= 1024 ? 1 : 4, 1};
+    return {256, 4, (unsigned)std::min<int64_t>((n + 1023) / 1024, mlda::kPolicyGroups)};
 }
+constexpr size_t kPolicyBytes = (size_t)mlda::kPolicyGroups * 3 * 8;
 
 int check_tokens(int64_t n) {
     return n < 0 || n >= ((int64_t)1 << 31) ? refuse("policy loss: need 0 <= n_tokens < 2^31") : MLDA_OK;
@@ -61,8 +68,7 @@ int mlda_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
 int mlda_policy_loss_workspace_bytes(int64_t n_tokens, size_t* bytes) {
     if (!bytes) return refuse("bytes is null");
     RC_TRY(check_tokens(n_tokens));
-    const unsigned groups = policy_groups(n_tokens);
-    *bytes = groups > 1 ? (size_t)groups * 3 * 8 : 0;
+    *bytes = policy_form(n_tokens).groups > 1 ? kPolicyBytes : 0;
     return MLDA_OK;
 }
 
@@ -80,21 +86,29 @@ int mlda_policy_loss(const float* logprobs, const float* old_logprobs, const flo
     if (!aligned(logprobs, 4) || !aligned(old_logprobs, 4) || !aligned(reference, 4) || !aligned(advantages, 4) || !aligned(weights, 4) ||
         !aligned(row_ptr, 8) || !aligned(sums, 4) || !aligned(grad_logprobs, 4))
         return refuse("policy loss: an argument is not aligned to its type");
-    const unsigned groups = policy_groups(n_tokens);
+    const PolicyForm form = policy_form(n_tokens);
+    const unsigned groups = form.groups;
     if (groups > 1) {
         if (!dev_workspace || !aligned(dev_workspace, 8)) return refuse("policy loss: the workspace is null or not aligned");
-        if (workspace_bytes < (size_t)groups * 3 * 8)
+        if (workspace_bytes < kPolicyBytes)
             return set_error(MLDA_ENOMEM, "policy loss: the workspace is smaller than mlda_policy_loss_workspace_bytes");
     }
     const mlda::PolicyArgs a{logprobs, old_logprobs, reference, advantages, weights, row_ptr, rows, n_tokens, log1p(-low), log1p(high),
                              1.0 - low, 1.0 + high, kl, n_tokens ? 1.0 / (double)n_tokens : 0.0, grad_logprobs,
-                             groups > 1 ? nullptr : sums, static_cast<double*>(dev_workspace)};
+                             groups > 1 ? nullptr : sums, static_cast<double*>(dev_workspace),
+                             passes_caches((double)n_tokens * (12 + (reference ? 4 : 0) + (row_ptr ? 0 : 4) + (weights ? 4 : 0)))};
     const hipStream_t stream = (hipStream_t)hip_stream;
-    if (reference) hipLaunchKernelGGL(mlda::policy_kernel<true>, dim3(groups), dim3(mlda::kPolicyThreads), 0, stream, a);
-    else hipLaunchKernelGGL(mlda::policy_kernel<false>, dim3(groups), dim3(mlda::kPolicyThreads), 0, stream, a);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(form.threads), 0, stream, a); };
+    auto of = [&](auto with_reference) {
+        constexpr bool kReference = decltype(with_reference)::value;
+        if (form.threads == 1024) launch(form.each == 1 ? mlda::policy_kernel<1024, 1, kReference> : mlda::policy_kernel<1024, 4, kReference>);
+        else launch(mlda::policy_kernel<256, 4, kReference>);
+    };
+    if (reference) of(std::true_type());
+    else of(std::false_type());
     RC_TRY(launched("policy_kernel"));
     if (groups == 1) return MLDA_OK;
-    hipLaunchKernelGGL(mlda::policy_sums_kernel, dim3(1), dim3(mlda::kPolicyThreads), 0, stream, a.partial, (int32_t)groups, sums);
+    hipLaunchKernelGGL(mlda::policy_sums_kernel, dim3(1), dim3(mlda::kPolicySumThreads), 0, stream, a.partial, (int32_t)groups, sums);
     return launched("policy_sums_kernel");
 }
 

@@ -1,8 +1,7 @@
 """Dropout and the policy loss on the GPU, through the public entry points, against the same in 64 bits by elementary operations.
 
 Masks have no tolerance.  A kept element is a product with a scale that is rounded to fp32, and a sum with its residual: 3 u, u = 2^-24, of the magnitudes, and one
-rounding to the type.  The policy loss is computed in fp64 and rounded once to fp32; a KL term, the difference of numbers e apart, is off by 2^-50 e
-before that, and exponentials by 2^-50 of themselves.
+rounding to the type.  The policy loss is computed in fp64 and rounded once to fp32; exponentials are off by 2^-50 of themselves before that, a KL term by 2^-39 of itself.
 """
 import math
 
@@ -211,7 +210,8 @@ def policy64(l, old, advantages, weights, reference, low, high, kl):
         grad = grad - kl * torch.expm1(e)
         size = size + abs(kl) * torch.expm1(e).abs()
     each = [torch.where(used, w * v, zero) for v in (loss, term, clipped.double(), grad, size)]
-    return each[0].sum(), each[1].sum(), each[2].sum(), each[3], each[4].abs(), [v.abs().sum() for v in each[:3]]
+    terms = each[1].abs().sum()
+    return each[0].sum(), each[1].sum(), each[2].sum(), each[3], each[4].abs(), [2.0 ** -45 * each[0].abs().sum() + 2.0 ** -39 * abs(kl) * terms, 2.0 ** -39 * terms, 2.0 ** -45 * each[2].abs().sum()]
 
 
 def check_policy(ops, n, seed, row_ptr=None, weights=None, reference=True, low=0.2, high=0.25, kl=0.05, given=True):
@@ -232,17 +232,33 @@ def check_policy(ops, n, seed, row_ptr=None, weights=None, reference=True, low=0
         a = a[at.clamp(0, max(rows - 1, 0))] if rows else torch.zeros(n, device="cuda")
     loss, term, clipped, grad, size, sums = policy64(l, old, a, w, f, low, high, kl if reference else 0.0)
     for x, y, s in ((got.loss, loss, sums[0]), (got.kl, term, sums[1]), (got.clipped, clipped, sums[2])):
-        assert x.shape == () and abs(float(x) - float(y)) <= U * abs(float(y)) + 2.0 ** -45 * float(s) + 2.0 ** -149
+        assert x.shape == () and abs(float(x) - float(y)) <= U * abs(float(y)) + float(s) + 2.0 ** -149
     assert ((got.grad_logprobs.double() - grad).abs() <= U * grad.abs() + 2.0 ** -48 * size + 2.0 ** -149).all()
     return got
 
 
-@pytest.mark.parametrize("n", [0, 1, 2, 3, 63, 64, 65, 255, 256, 257, 1000, 1023, 1025, 4099, 300007])
+@pytest.mark.parametrize("n", [0, 1, 2, 3, 63, 64, 65, 255, 256, 257, 1000, 1023, 1024, 1025, 4096, 4099, 300007, 524288, 524291, 2500003])
 def test_policy_loss(ops, n):
     check_policy(ops, n, n)
     check_policy(ops, n, n + 1, reference=False)
     check_policy(ops, n, n + 2, given=False, low=0.0, high=0.0)
     check_policy(ops, n, n + 3, low=1.0, high=INF, kl=-1.0)
+
+
+@pytest.mark.parametrize("apart", [0.0, 1e-6, 1e-4, 0.0156, 0.0157, 0.1, 3.0, 60.0])
+def test_kl_term_of_like_and_unlike_models(ops, apart):
+    l = -torch.rand(1000, generator=gen(1), device="cuda")
+    f = l + apart * torch.where(torch.arange(1000, device="cuda") % 2 == 0, 1.0, -1.0)
+    w = torch.rand(1000, generator=gen(2), device="cuda")
+    got = ops.policy_loss(l, l, torch.zeros_like(l), w, f, kl=0.5)
+    x = f.double() - l.double()
+    # in 64 bits by the series up to x^12, whose next term is below 2^-40 of the whole up to 0.16; beyond by the difference, which loses 2^-53 of exp(x) + |x|
+    series = sum(x ** k / math.factorial(k) for k in range(2, 13))
+    term = torch.where(x.abs() < 0.16, series, torch.exp(x) - x - 1)
+    want, grad = (w.double() * term).sum(), 0.5 * w.double() * -torch.where(x.abs() < 0.16, x + series, torch.exp(x) - 1)
+    assert abs(float(got.kl) - float(want)) <= (U + 2.0 ** -38) * float(want) + 2.0 ** -149
+    assert abs(float(got.loss) - 0.5 * float(want)) <= (U + 2.0 ** -38) * float(want) + 2.0 ** -149
+    assert ((got.grad_logprobs.double() - grad).abs() <= (U + 2.0 ** -38) * grad.abs() + 2.0 ** -149).all()
 
 
 @pytest.mark.parametrize("lengths", [[5], [0, 0, 3, 0], [1] * 100, [300, 0, 7, 1, 0, 0, 2000, 5], [0], [], [40000] + [1, 0] * 3000])
