@@ -1,0 +1,139 @@
+"""The document model with dropout, the policy loss and 4-bit weights: runs of these operators together."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def made(rows=40, K=33, V=701, seed=3, **how):
+    from paper_1803_04631_amd.doc_model import DocModel, Documents
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    model = DocModel(K, np.arange(V), **how)
+    model.weight += 0.1 * torch.randn(V, K, generator=g, device="cuda")
+    model.scale += 0.1 * torch.randn(K, generator=g, device="cuda")
+    lengths = torch.randint(0, 30, (rows,), generator=g, device="cuda")
+    ptr = torch.cat([lengths.new_zeros(1), lengths.cumsum(0)])
+    words = Documents(ptr, torch.randint(V, (int(ptr[-1]),), generator=g, device="cuda", dtype=torch.int32))
+    row = torch.repeat_interleave(torch.arange(rows, device="cuda"), lengths)
+    return model, torch.randn(rows, K, generator=g, device="cuda"), words, row, g
+
+
+def logp64(model, x, mask=None):
+    params = [p.double().requires_grad_() for p in (model.weight, model.bias, model.scale, model.shift)]
+    y = torch.nn.functional.layer_norm(x.double(), x.shape[1:], params[2], params[3], 1e-5)
+    if mask is not None:
+        y = y * mask
+    return params, torch.log_softmax(y @ params[0].t() + params[1], 1)
+
+
+def same_gradients(grads, loss, params):
+    # fp32 products over up to 701 terms: about 1e-4 of the largest entry at the most
+    for got, exact in zip(grads, torch.autograd.grad(loss, params)):
+        assert (got.double() - exact).abs().max() <= 1e-4 * exact.abs().max()
+
+
+def test_gradients_with_dropout():
+    from paper_1803_04631_amd import operators
+    model, x, words, row, _ = made(dropout=0.3, seed=3)
+    for steps in (0, 5):
+        model.steps = steps
+        logprob, grads = model.gradients(x, words)
+        kept = operators.dropout(torch.ones_like(x), 0.3, model.seed, steps)
+        assert 0.5 < float((kept != 0).double().mean()) < 0.9
+        params, logp = logp64(model, x, (kept != 0).double() / 0.7)
+        want = logp[row, words.tokens.long()].mean()
+        assert abs(float(logprob) - want.item()) <= 1e-4 * abs(want.item())
+        same_gradients(grads, -want, params)
+    a = model.score(x, words).logprobs                                    # scoring drops nothing
+    assert (a.double() - logp64(model, x)[1][row, words.tokens.long()]).abs().max() <= 1e-4
+
+
+def test_policy_gradients():
+    model, x, words, row, g = made(seed=4)
+    n = len(words.tokens)
+    params, logp = logp64(model, x)
+    l = logp[row, words.tokens.long()]
+    old = (l.detach() + 0.3 * torch.randn(n, generator=g, device="cuda")).float()
+    reference = (l.detach() + 0.3 * torch.randn(n, generator=g, device="cuda")).float()
+    advantages = torch.randn(n, generator=g, device="cuda")
+    got, grads = model.policy_gradients(x, words, old, advantages, reference=reference, low=0.2, high=0.3, kl=0.1, entropy=0.05)
+    ratio, d = torch.exp(l - old.double()), reference.double() - l
+    least = torch.minimum(ratio * advantages.double(), ratio.clamp(0.8, 1.3) * advantages.double())
+    loss = (0.1 * (torch.exp(d) - d - 1) - least).mean()
+    entropy = -(logp.exp() * logp).sum(1).mean()
+    # log-probabilities of about 7 are off by 1e-6: so are ratios, of which n are averaged
+    assert abs(float(got.loss) - loss.item()) <= 1e-5
+    border = torch.minimum((l - old - math.log(0.8)).abs(), (l - old - math.log(1.3)).abs())
+    assert border.min() > 1e-5
+    same_gradients(grads, loss - 0.05 * entropy, params)
+
+
+def test_packed_scores_are_those_of_the_packed_weights():
+    from paper_1803_04631_amd import operators
+    model, x, words, row, _ = made(rows=100, K=70, V=1003, seed=5)
+    packed = model.packed(dtype=torch.float32)
+    y = operators.layer_norm(x, model.scale, model.shift)[0]
+    held = operators.mx4_dequantize(operators.mx4_quantize(y)).double()
+    logits = held @ operators.mx4_dequantize(packed.weight).double().t() + model.bias.double()
+    want = torch.log_softmax(logits, 1)[row, words.tokens.long()]
+    got = packed.score(x, words, alternatives=5)
+    # sums of 70 terms of up to 3 in fp32, logits of up to 10
+    assert (got.logprobs.double() - want).abs().max() <= 2e-5
+    full = model.score(x, words)
+    # a product of 4-bit numbers: an eighth of a feature and an eighth of a weight off, some 0.16 of logits that spread by 0.8, 100 rows of 30 words averaged
+    assert abs(float((got.logprobs - full.logprobs).mean())) < 0.1
+    assert got.top_ids.shape == (100, 5) and (got.entropy > 0).all()
+    model.weight.zero_()                                                   # (the packed model is as it was)
+    assert torch.equal(packed.score(x, words).logprobs, got.logprobs)
+
+
+def test_a_step_in_a_graph_draws_new_masks():
+    """Forward, loss and backward of a step captured once: each replay has the mask of the step's number that it finds on the GPU."""
+    from paper_1803_04631_amd import operators
+    model, x, words, row, _ = made(seed=6)
+    weights = torch.full((len(words.tokens),), -1.0 / len(words.tokens), device="cuda")
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def gradient(step):
+        y, mean, rstd = operators.layer_norm(x, model.scale, model.shift)
+        operators.dropout(y, 0.4, 9, step, out=y)
+        logits = torch.addmm(model.bias, y, model.weight.t())
+        grad = operators.token_logprobs_grad(logits, words.tokens, weights, words.row_ptr, out=logits)[1]
+        grad_y = operators.dropout_backward(grad @ model.weight, 0.4, 9, step)
+        return operators.layer_norm_backward(grad_y, x, mean, rstd, model.scale)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        gradient(step)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = gradient(step)
+        step += 1
+    seen = []
+    for k in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = gradient(k)
+        # (the library products of a captured stream may be others: 701 terms in fp32)
+        assert all((a - b).abs().max() <= 1e-4 * b.abs().max() for a, b in zip(out, want))
+        seen.append(out[0].clone())
+    assert all(not torch.equal(a, b) for i, a in enumerate(seen) for b in seen[:i])
+
+
+def test_training_with_dropout_suggestions_and_packed_weights(tmp_path, capsys):
+    import corpus_synth
+    from paper_1803_04631_amd import bow, doc_model
+    c = corpus_synth.tiny(D=80, V=90, K=4, mean_len=40, seed=2)
+    path = tmp_path / "docword.small.txt"
+    bow.save_docword(path, c.doc_ptr, c.word_ids, 90)
+    doc_model.main([str(path), "--topics", "4", "--iters", "5", "--epochs", "2", "--batch", "30", "--show", "2", "--dropout", "0.2", "--suggest", "2", "--packed"])
+    out = capsys.readouterr().out
+    assert "round held kl clipped" in out and "in 4 bits" in out and "document 2: entropy" in out
+    a = doc_model.train(c.doc_ptr, c.word_ids, 90, 4, iters=5, epochs=2, batch=30, dropout=0.2)
+    b = doc_model.train(c.doc_ptr, c.word_ids, 90, 4, iters=5, epochs=2, batch=30, dropout=0.2)
+    assert abs(a[3][-1][2] - b[3][-1][2]) <= 1e-4 and a[0].steps == b[0].steps == 6        # the same masks in both runs
