@@ -215,7 +215,7 @@ __device__ __forceinline__ uint64_t placed_scales(uint64_t s, int32_t first, int
     return short_by == 0 ? s : short_by == 64 ? 0x7f7f7f7f7f7f7f7full : s >> short_by | 0x7f7f7f7f7f7f7f7full << (64 - short_by);
 }
 
-// Few rows.  A wave has 32 words and 32 kTiles rows.  Its words' codes come straight from memory, 128 bytes of a word at a time (a line, or two that
+// Few rows (or words).  A wave has 32 words and 32 rows.  Its words' codes come straight from memory, 128 bytes of a word at a time (a line, or two that
 // the next slab meets again) and kFewAhead such slabs on their way, and through LDS into the instructions' order: bound by reading them.  Rows that are few enough are put into 4 bits by each workgroup for itself, while its words' codes are on their way (X: their type); others
 // (X = void) are laid out by mx4_fragments_kernel and come from the L2 cache.  With kSplit the four waves of a workgroup share their words'
 // slabs, and their sums are joined in a fixed order.
@@ -223,15 +223,15 @@ constexpr int kFewBlocks = 8;            // of a slab
 constexpr int kFewWaves = 4;
 constexpr int kFewWords = 32;            // of a wave
 
-template <class T, class X, int kTiles, bool kSplit, int kFewAhead>
+template <class T, class X, bool kSplit, int kFewAhead>
 __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs a, MxArgs q, int32_t steps) {
     constexpr bool kOwn = !std::is_void_v<X>;
     extern __shared__ Codes few_room[];                    // own rows: [block][row], then their scales; the parts of the sums
     __shared__ Codes turned[kFewWaves][kFewWords * kFewBlocks];            // a word's blocks turned by its number, so that eight lanes that read a block of eight words meet all banks
-    __shared__ Acc sums[kSplit ? kFewWaves - 1 : 1][kSplit ? kTiles : 1][kWave];
+    __shared__ Acc sums[kSplit ? kFewWaves - 1 : 1][kWave];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), col = lane % 32, part = lane / 32;
     const int64_t row0 = (int64_t)blockIdx.y * 32;
-    const int rows = (int)min(kOwn ? (int64_t)32 : (int64_t)32 * kTiles, a.rows - row0);
+    const int rows = (int)min((int64_t)32, a.rows - row0);
     const int64_t word0 = ((int64_t)blockIdx.x * (kSplit ? 1 : kFewWaves) + (kSplit ? 0 : wave)) * kFewWords;
     const int64_t word = min(word0 + col, (int64_t)a.words - 1);           // (what comes of the lanes past the end is not stored)
     const uint8_t* scales = a.scales + word * a.blocks;
@@ -239,17 +239,14 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
     const uint8_t* from[4];                                // of the lane's four words
 #pragma unroll
     for (int i = 0; i < 4; ++i) from[i] = a.codes + min(word0 + 8 * i + lane / kFewBlocks, (int64_t)a.words - 1) * a.blocks * kMxBytes;
-    Codes x[2][4][kTiles];                                 // rows that are laid out: of this slab and the next
-    uint32_t xs[2][kTiles];
+    Codes x[2][4];                                         // rows that are laid out: of this slab and the next
+    uint32_t xs[2];
     auto fetch_rows = [&](int buffer, int32_t slab) {
         if (kOwn || slab >= slabs) return;
+        const Codes* const from_rows = reinterpret_cast<const Codes*>(a.x_codes) + ((int64_t)blockIdx.y * steps + slab * 4) * kWave + lane;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            const int64_t tile = min((int64_t)t, (a.rows - 1) / 32);
-#pragma unroll
-            for (int s = 0; s < 4; ++s) x[buffer][s][t] = reinterpret_cast<const Codes*>(a.x_codes)[(tile * steps + slab * 4 + s) * kWave + lane];
-            xs[buffer][t] = reinterpret_cast<const uint32_t*>(a.x_scales)[(tile * (steps / 4) + slab) * kWave + lane];
-        }
+        for (int s = 0; s < 4; ++s) x[buffer][s] = from_rows[s * kWave];
+        xs[buffer] = reinterpret_cast<const uint32_t*>(a.x_scales)[((int64_t)blockIdx.y * (steps / 4) + slab) * kWave + lane];
     };
     static_assert(kFewAhead % 2 == 0 || kOwn, "rows that are laid out take turns in two places");
     fetch_rows(0, begin);
@@ -260,7 +257,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
         if (slab >= slabs) return;
         const int64_t at = (int64_t)min(slab * kFewBlocks + block, a.blocks - 1) * kMxBytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[buffer][i] = __builtin_nontemporal_load(reinterpret_cast<const Codes*>(from[i] + at));
+        for (int i = 0; i < 4; ++i) w[buffer][i] = *reinterpret_cast<const Codes*>(from[i] + at);
         ws[buffer] = load_scales(scales, slab * kFewBlocks, a.blocks);
     };
 #pragma unroll
@@ -283,7 +280,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
         __syncthreads();
     }
 
-    Acc acc[kTiles] = {};
+    Acc acc = {};
     auto use = [&](int buffer, int32_t slab) {
         if (slab >= slabs) return;
         const int32_t first = slab * kFewBlocks;
@@ -296,20 +293,17 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
             constexpr int s = decltype(which)::value;
             if (first + 2 * s >= a.blocks) return;
             const Codes wc = turned[wave][col * kFewBlocks + ((2 * s + part) ^ (col & 7))];
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                Codes xc;
-                uint32_t row_scale;
-                if constexpr (kOwn) {
-                    const int at = min(first + 2 * s + part, a.blocks - 1) * rows + min(col, rows - 1);
-                    xc = few_room[at];
-                    row_scale = own_scales[at];
-                } else {
-                    xc = x[buffer % 2][s][t];
-                    row_scale = xs[buffer % 2][t];
-                }
-                acc[t] = mx4_mfma<kOwn ? 0 : s, s % 2 * 2>(xc, row_scale, wc, (uint32_t)(word_scales >> s / 2 * 32), acc[t]);
+            Codes xc;
+            uint32_t row_scale;
+            if constexpr (kOwn) {
+                const int at = min(first + 2 * s + part, a.blocks - 1) * rows + min(col, rows - 1);
+                xc = few_room[at];
+                row_scale = own_scales[at];
+            } else {
+                xc = x[buffer % 2][s];
+                row_scale = xs[buffer % 2];
             }
+            acc = mx4_mfma<kOwn ? 0 : s, s % 2 * 2>(xc, row_scale, wc, (uint32_t)(word_scales >> s / 2 * 32), acc);
         };
         step(std::integral_constant<int, 0>());
         step(std::integral_constant<int, 1>());
@@ -325,39 +319,34 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
         }
     }
     if constexpr (kSplit) {
-        if (wave > 0) {
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) sums[wave - 1][t][lane] = acc[t];
-        }
+        if (wave > 0) sums[wave - 1][lane] = acc;
         __syncthreads();
         if (wave > 0) return;
 #pragma unroll
-        for (int k = 0; k < kFewWaves - 1; ++k)
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) acc[t] += sums[k][t][lane];
+        for (int k = 0; k < kFewWaves - 1; ++k) acc += sums[k][lane];
     }
     if (word0 + col >= a.words) return;
     const float bias = bias_at<T>(a, (int32_t)word);
     T* const y = static_cast<T*>(a.y) + row0 * a.y_stride + word0 + col;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int row = 32 * t + 8 * (j / 4) + 4 * part + j % 4;
-            if (row < rows) y[row * a.y_stride] = (T)(acc[t][j] + bias);
-        }
+    for (int j = 0; j < 16; ++j) {
+        const int row = 8 * (j / 4) + 4 * part + j % 4;
+        if (row < rows) y[row * a.y_stride] = (T)(acc[j] + bias);
     }
 }
 
-// Many rows.  A workgroup holds its words in LDS, as the matrix instructions want them, and goes through the rows: a wave has 128 words
-// and 32 kTiles rows at a time, whose codes (laid out by mx4_fragments_kernel) come straight from the L2 cache, kAhead steps ahead.  So
-// the waves wait for each other only where the words change, and a row costs the L2 its codes once for 128 kHalves words.  (Words and
-// rows both through LDS, 256 x 128 a workgroup: 2,048 x 141,000 x 1,000 bf16 took 270 us, LDS and matrix instructions in turn, so 239.)
+// Many rows.  A workgroup holds the codes of 128 words in LDS, as the matrix instructions want them, and goes through the rows: a wave has 32 of them at a
+// time, whose codes (laid out by mx4_fragments_kernel) come straight from the L2 cache, three steps ahead.  So the waves wait for each other only where
+// the words change, and the next words are on their way before.  (Words and rows both through LDS, 256 x 128 a workgroup: 2,048 x 141,000 x 1,000 bf16 took 270 us,
+// LDS and matrix instructions in turn; words held, 239, or 229 with the next ones sent for.)
 //
 // The columns of an instruction's result are the words 4 c + i of its four matrices i: a lane has four neighbouring words of a row, and a
 // wave stores 256 bytes or more of it at once.
+//
+// Bound, at 1,000 columns, by writing: a line that two workgroups write a part of costs memory more than two, so that 141,000 bf16 words (rows 16 bytes off a line
+// from one to the next) take 180 us to store and 140,800 116; the matrix instructions take 90 us, which power limits.
 constexpr int kAhead = 4;                // steps of two blocks, which share a word of scales
-constexpr int kWaveWords = 128;
+constexpr int kTileWords = 128;
 
 // Four neighbouring elements, of which `n` or all are there.
 template <class T>
@@ -378,133 +367,133 @@ __device__ __forceinline__ void store_four(T* p, const float (&v)[4], int64_t n,
 struct MxTilesArgs {
     MxLinearArgs m;                      // x in the order above
     int32_t steps;                       // of two blocks, a multiple of kAhead
-    int32_t held;                        // steps that LDS holds, likewise
     uint32_t passes;                     // through all rows
     uint32_t units;                      // word tiles times passes
-    Divisor pass, slab;                  // by passes; by 2 held
+    Divisor pass;                        // by passes
     bool once;
 };
 
-template <class T, int kTiles, int kHalves, int kWaves, int kPerSimd = 2, int kBuffers = 2>
-__global__ __launch_bounds__(kWaves * kWave, kPerSimd) void mx4_tiles_kernel(MxTilesArgs a) {
-    constexpr int kThreads = kWaves * kWave, kWords = kWaveWords * kHalves, kRows = kWaves / kHalves * kTiles * 32;
-    extern __shared__ Codes held[];                        // [step][half][i][lane]; a lane's place is turned by its block's number, so that neighbouring blocks of a word do not meet in a bank
-    uint32_t* const held_scales = reinterpret_cast<uint32_t*>(held + a.held * kHalves * 4 * kWave);      // [step][half][lane], a byte for each i
+// kChunk: steps that are held at a time, twice: those that are multiplied, and those that were before or will be next.
+template <class T, int kWaves, int kChunk>
+__global__ __launch_bounds__(kWaves * kWave, 2) void mx4_tiles_kernel(MxTilesArgs a) {
+    constexpr int kThreads = kWaves * kWave, kPieces = kTileWords * 2 * kChunk / kThreads;
+    static_assert(kTileWords * kChunk / 4 == kThreads, "a thread has the scales of eight blocks");
+    // [slot][step][i][lane]; a lane's place is turned by its block's number, so that neighbouring blocks of a word do not meet in a bank
+    extern __shared__ Codes held[];
     const MxLinearArgs& m = a.m;
-    const int thread = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(thread / kWave), half = wave % kHalves, mine = wave / kHalves * kTiles;
-    const int col = lane % 32, part = lane / 32;
+    const int32_t slot_steps = min(kChunk, a.steps), chunks = (a.steps + kChunk - 1) / kChunk;
+    uint32_t* const held_scales = reinterpret_cast<uint32_t*>(held + 2 * slot_steps * 4 * kWave);        // [slot][step][lane], a byte for each i
+    const int thread = (int)threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(thread / kWave), col = lane % 32, part = lane / 32;
     // Whole rounds of tiles first, neighbouring tiles in neighbouring workgroups of an XCD, so that all that is written at a time is long runs of the same
     // rows; what is left of the tiles is cut into equal parts.
     const uint32_t groups = gridDim.x, group = groups % 8 ? blockIdx.x : blockIdx.x % 8 * (groups / 8) + blockIdx.x / 8;
     const uint32_t rounds = a.units / a.passes / groups, whole = rounds * a.passes, left = a.units - whole * groups;
-    const uint32_t begin = (uint32_t)((uint64_t)left * group / groups), end = (uint32_t)((uint64_t)left * (group + 1) / groups);
-    const int64_t last_tile = (m.rows - 1) / 32;
-
-    auto hold = [&](int64_t word0, int32_t first) {        // steps from the first on
-        const int words = (int)min((int64_t)kWords, m.words - word0);
-        const uint8_t* codes = m.codes + word0 * m.blocks * kMxBytes;
-        for (uint32_t at = (uint32_t)thread; at < (uint32_t)(kWords * 2 * a.held); at += kThreads) {
-            const int word = (int)a.slab(at), in = (int)(at - (uint32_t)word * a.slab.by), block = 2 * first + in;
-            const Codes c = *reinterpret_cast<const Codes*>(codes + ((int64_t)min(word, words - 1) * m.blocks + min(block, m.blocks - 1)) * kMxBytes);
-            held[((in / 2 * kHalves + word / kWaveWords) * 4 + word % 4) * kWave + in % 2 * 32 + (word % kWaveWords / 4 ^ (in & 7))] =
-                block < m.blocks ? c : Codes{0, 0, 0, 0};
-        }
-        for (int at = thread; at < kWords * (a.held / 4); at += kThreads) {
-            const int word = at % kWords, in = at / kWords * 8;
-            const uint64_t s = placed_scales(load_scales(m.scales + (word0 + min(word, words - 1)) * m.blocks, 2 * first + in, m.blocks), 2 * first + in, m.blocks);
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                reinterpret_cast<uint8_t*>(held_scales + (((in + c) / 2 * kHalves + word / kWaveWords) * kWave + c % 2 * 32 + word % kWaveWords / 4))[word % 4] =
-                    (uint8_t)(s >> 8 * c);
-        }
-    };
-
+    const uint32_t begin = (uint32_t)((uint64_t)left * group / groups), end = (uint32_t)((uint64_t)left * (group + 1) / groups), count = whole + (end - begin);
+    if (count == 0) return;
     auto tile_of = [&](uint32_t n, uint32_t& pass) {
         const uint32_t unit = n < whole ? n : begin + (n - whole), in_round = a.pass(unit);
         pass = unit - in_round * a.passes;
-        return n < whole ? in_round * groups + group : rounds * groups + in_round;
+        return (int32_t)(n < whole ? in_round * groups + group : rounds * groups + in_round);
     };
-    const Codes* x[kTiles];
-    const uint32_t* x_scales[kTiles];
-    Codes next[kAhead][kTiles];                            // of the next three steps
-    uint32_t next_scales[kTiles];                          // of the next four
-    auto fetch = [&](int s, int32_t step) {
+
+    // The words' codes and scales of a chunk: on their way, then held.
+    Codes way[kPieces];
+    uint64_t way_scales;
+    const int scale_word = thread % kTileWords, scale_block = thread / kTileWords * 8;
+    auto send_for = [&](int32_t tile, int32_t chunk) {
+        const int64_t word0 = (int64_t)tile * kTileWords;
+        const int words = (int)min((int64_t)kTileWords, m.words - word0);
+        const uint8_t* codes = m.codes + word0 * m.blocks * kMxBytes;
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) next[s][t] = x[t][step * kWave];
-    };
-    auto fetch_first = [&](uint32_t pass) {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            const int64_t at = min((int64_t)pass * (kRows / 32) + mine + t, last_tile);
-            x[t] = reinterpret_cast<const Codes*>(m.x_codes) + at * a.steps * kWave + lane;
-            x_scales[t] = reinterpret_cast<const uint32_t*>(m.x_scales) + at * (a.steps / 4) * kWave + lane;
-            next_scales[t] = x_scales[t][0];
+        for (int j = 0; j < kPieces; ++j) {
+            const int at = j * kThreads + thread, word = at / (2 * kChunk), block = chunk * 2 * kChunk + at % (2 * kChunk);
+            way[j] = *reinterpret_cast<const Codes*>(codes + ((int64_t)min(word, words - 1) * m.blocks + min(block, m.blocks - 1)) * kMxBytes);
         }
+        way_scales = load_scales(m.scales + (word0 + min(scale_word, words - 1)) * m.blocks, chunk * 2 * kChunk + scale_block, m.blocks);
+    };
+    auto hold = [&](int slot, int32_t chunk) {
+        Codes* const to = held + slot * slot_steps * 4 * kWave;
+        uint32_t* const scales_to = held_scales + slot * slot_steps * kWave;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const int at = j * kThreads + thread, word = at / (2 * kChunk), in = at % (2 * kChunk);
+            if (in / 2 < slot_steps)
+                to[(in / 2 * 4 + word % 4) * kWave + in % 2 * 32 + (word / 4 ^ (in & 7))] = chunk * 2 * kChunk + in < m.blocks ? way[j] : Codes{0, 0, 0, 0};
+        }
+        const uint64_t s = placed_scales(way_scales, chunk * 2 * kChunk + scale_block, m.blocks);
+        if (scale_block / 2 < slot_steps) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                reinterpret_cast<uint8_t*>(scales_to + (scale_block + c) / 2 * kWave + c % 2 * 32 + scale_word / 4)[scale_word % 4] = (uint8_t)(s >> 8 * c);
+        }
+    };
+
+    const int64_t last_tile = (m.rows - 1) / 32;
+    const Codes* x = nullptr;
+    const uint32_t* x_scales = nullptr;
+    Codes next[kAhead];                                    // of the next three steps
+    uint32_t next_scales = 0;                              // of the next four
+    auto fetch = [&](int s, int32_t step) { next[s] = x[step * kWave + lane]; };
+    auto fetch_first = [&](uint32_t pass) {
+        const int64_t at = min((int64_t)pass * kWaves + wave, last_tile);
+        x = reinterpret_cast<const Codes*>(m.x_codes) + at * a.steps * kWave;
+        x_scales = reinterpret_cast<const uint32_t*>(m.x_scales) + at * (a.steps / 4) * kWave;
+        next_scales = x_scales[lane];
 #pragma unroll
         for (int s = 0; s < kAhead - 1; ++s) fetch(s, s);
     };
 
-    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    int64_t word0 = -1;
-    const uint32_t count = whole + (end - begin);
-    uint32_t pass, tile = tile_of(0, pass);
-    if (count) fetch_first(pass);
+    uint32_t pass;
+    int32_t tile = tile_of(0, pass), slot = 0;
+    int32_t other_tile = -1, other_chunk = -1;             // what the other slot holds
+    send_for(tile, 0);
+    fetch_first(pass);
+    hold(0, 0);
+    __syncthreads();
+    float bias[4];
+    int32_t bias_of = -1;
     for (uint32_t n = 0; n < count; ++n) {
-        const bool fresh = word0 != (int64_t)tile * kWords;
-        if (fresh) {
-            word0 = (int64_t)tile * kWords;
+        const int64_t word = (int64_t)tile * kTileWords + 4 * col;
+        if (bias_of != tile) {
+            bias_of = tile;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t word = word0 + half * kWaveWords + 4 * col + i;
-                bias[i] = word < m.words ? bias_at<T>(m, (int32_t)word) : 0.0f;
-            }
+            for (int i = 0; i < 4; ++i) bias[i] = word + i < m.words ? bias_at<T>(m, (int32_t)(word + i)) : 0.0f;
         }
-        // (16-bit results: the bias is the sums' first term; fp32 results have it added at the end, one rounding instead of as many as there are steps)
-        Acc acc[kTiles][4];
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) acc[t][i][j] = sizeof(T) == 2 ? bias[i] : 0.0f;
-        for (int32_t first = 0; first < a.steps; first += a.held) {
-            if (fresh || a.held < a.steps) {
-                __syncthreads();
-                hold(word0, first);
-                __syncthreads();
-            }
-            const int32_t steps = min(a.held, a.steps - first);
-            Codes w[kBuffers][4];                          // of this step and the next
-            uint32_t ws[kBuffers];
+        uint32_t next_pass = pass;
+        const int32_t next_tile = n + 1 < count ? tile_of(n + 1, next_pass) : tile;
+        Acc acc[4] = {};
+        for (int32_t chunk = 0; chunk < chunks; ++chunk) {
+            // what comes after this chunk, and whether it has to be sent for
+            const bool last = chunk + 1 == chunks;
+            const int32_t after_tile = last ? next_tile : tile, after_chunk = last ? 0 : chunk + 1;
+            const bool stay = after_tile == tile && after_chunk == chunk, there = after_tile == other_tile && after_chunk == other_chunk;
+            const bool send = !stay && !there && !(last && n + 1 == count);
+            if (send) send_for(after_tile, after_chunk);
+            const int32_t first = chunk * kChunk, steps = min(kChunk, a.steps - first);
+            const Codes* const mine = held + slot * slot_steps * 4 * kWave + part * 32;
+            const uint32_t* const mine_scales = held_scales + slot * slot_steps * kWave + lane;
+            Codes w[2][4];                                 // of this step and the next
+            uint32_t ws[2];
             auto read = [&](int buffer, int s, int32_t step) {     // s: step % 4
-                const Codes* at = held + (step * kHalves + half) * 4 * kWave + part * 32 + (col ^ ((2 * s + part) & 7));
+                const Codes* at = mine + step * 4 * kWave + (col ^ ((2 * s + part) & 7));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[buffer][i] = at[i * kWave];
-                ws[buffer] = held_scales[(step * kHalves + half) * kWave + lane];
+                ws[buffer] = mine_scales[step * kWave];
             };
-            if (kBuffers == 2) read(0, 0, 0);
+            read(0, 0, 0);
             for (int32_t in = 0; in < steps; in += kAhead) {
-                uint32_t xs[kTiles];
                 const int32_t ahead = min(first + in + kAhead, a.steps - kAhead);          // (the last ones are loaded again)
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t) {
-                    xs[t] = next_scales[t];
-                    next_scales[t] = x_scales[t][ahead / 4 * kWave];
-                }
+                const uint32_t xs = next_scales;
+                next_scales = x_scales[ahead / 4 * kWave + lane];
                 auto step = [&](auto which) {
                     constexpr int s = decltype(which)::value;
-                    if (kBuffers == 2) read((s + 1) & 1, (s + 1) % 4, min(in + s + 1, steps - 1));
-                    else read(0, s, in + s);
+                    read((s + 1) & 1, (s + 1) % 4, min(in + s + 1, steps - 1));
                     fetch((s + 3) % 4, s ? ahead + s - 1 : min(first + in + 3, a.steps - 1));
                     __builtin_amdgcn_sched_barrier(0);     // (or the loads are moved to where they are needed)
-                    auto column = [&](auto i) {
-#pragma unroll
-                        for (int t = 0; t < kTiles; ++t) acc[t][i.value] = mx4_mfma<s, i.value>(next[s][t], xs[t], w[s % kBuffers][i.value], ws[s % kBuffers], acc[t][i.value]);
-                    };
-                    column(std::integral_constant<int, 0>());
-                    column(std::integral_constant<int, 1>());
-                    column(std::integral_constant<int, 2>());
-                    column(std::integral_constant<int, 3>());
+                    acc[0] = mx4_mfma<s, 0>(next[s], xs, w[s & 1][0], ws[s & 1], acc[0]);
+                    acc[1] = mx4_mfma<s, 1>(next[s], xs, w[s & 1][1], ws[s & 1], acc[1]);
+                    acc[2] = mx4_mfma<s, 2>(next[s], xs, w[s & 1][2], ws[s & 1], acc[2]);
+                    acc[3] = mx4_mfma<s, 3>(next[s], xs, w[s & 1][3], ws[s & 1], acc[3]);
                     __builtin_amdgcn_sched_barrier(0);
                 };
                 step(std::integral_constant<int, 0>());
@@ -512,30 +501,35 @@ __global__ __launch_bounds__(kWaves * kWave, kPerSimd) void mx4_tiles_kernel(MxT
                 step(std::integral_constant<int, 2>());
                 step(std::integral_constant<int, 3>());
             }
+            if (last && n + 1 < count) fetch_first(next_pass);
+            if (send) {
+                __syncthreads();                           // (the other slot's readers are done)
+                hold(1 - slot, after_chunk);
+                __syncthreads();
+            }
+            if (!stay) {
+                other_tile = tile;
+                other_chunk = chunk;
+                slot = 1 - slot;
+            }
         }
-        const int64_t tile0 = (int64_t)pass * (kRows / 32) + mine;
-        if (n + 1 < count) {
-            tile = tile_of(n + 1, pass);
-            fetch_first(pass);
-        }
-        __builtin_amdgcn_sched_barrier(0);                 // (the loads before the stores: they are waited for in order)
-        const int64_t word = word0 + half * kWaveWords + 4 * col, row0 = tile0 * 32 + 4 * part;
+        __builtin_amdgcn_sched_barrier(0);                 // (the next rows' loads before the stores: they are waited for in order)
+        const int64_t row0 = ((int64_t)pass * kWaves + wave) * 32 + 4 * part;
         T* const y = static_cast<T*>(m.y) + row0 * m.y_stride + word;
         auto store = [&](bool all) {
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
+            for (int j = 0; j < 16; ++j) {
+                const int down = 8 * (j / 4) + j % 4;
+                float v[4];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int down = 32 * t + 8 * (j / 4) + j % 4;
-                    float v[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = sizeof(T) == 2 ? acc[t][i][j] : acc[t][i][j] + bias[i];
-                    if (all || row0 + down < m.rows) store_four(y + down * m.y_stride, v, all ? 4 : m.words - word, a.once);
-                }
+                for (int i = 0; i < 4; ++i) v[i] = acc[i][j] + bias[i];
+                if (all || row0 + down < m.rows) store_four(y + down * m.y_stride, v, all ? 4 : m.words - word, a.once);
             }
         };
-        if ((tile0 + kTiles) * 32 <= m.rows && word0 + kWords <= m.words) store(true);
+        if (((int64_t)pass * kWaves + wave + 1) * 32 <= m.rows && (int64_t)(tile + 1) * kTileWords <= m.words) store(true);
         else store(false);
+        tile = next_tile;
+        pass = next_pass;
     }
 }
 

@@ -7,13 +7,16 @@ namespace {
 
 int64_t blocks_of(int32_t cols) { return ((int64_t)cols + mlda::kMxBlock - 1) / mlda::kMxBlock; }
 
-constexpr int kLdsBytes = 163840;
 constexpr int32_t kMostProductCols = 1 << 24;    // tiles of rows have 32-bit numbers of pieces
 
 // How a product's rows are held in 4 bits: few, and short ones of a small product, by each workgroup for itself (1 x 1,000 x 141,000 fp32 with a launch for the row 27 us, so 19;
 // 1,000 x 32 x 5,000 fp32 14.3 and 8.6; but 2,048 x 128 x 141,000 bf16 181 us, so 614), others in the workspace, in whole tiles of rows and whole stretches of steps.
 bool few_rows(int64_t rows, int32_t cols) { return rows <= 16 && rows * blocks_of(cols) <= 1024; }
 bool short_rows(int64_t rows, int32_t cols, int32_t words) { return blocks_of(cols) <= 2 && rows <= ((int64_t)1 << 23) / words; }
+// Which products are few enough for a wave for each 32 x 32 of them; the others take tiles of 128 words and as many rows as a workgroup's waves have, 128
+// where there are few, else 256 (1,000 columns, bf16, us: wave for each, 128, 256).  300 x 5,000: 11.1, 13.1, 13.5; 500 x 5,000: 16.3, 13.4, 14.3; 32 x 141,000: 28, 31,
+// 42; 65 x 141,000: 66, 33, 46; 500 x 141,000: 312, 70, 75; 2,048 x 141,000: -, 268, 246.
+bool few_products(int64_t rows, int32_t words) { return rows <= 32 || (rows + 31) / 32 <= 2048 / (((int64_t)words + 31) / 32); }
 int64_t held_rows(int64_t rows) { return (rows + 31) / 32 * 32; }
 int64_t held_blocks(int32_t cols) {
     constexpr int64_t kEach = 2 * mlda::kAhead;
@@ -78,66 +81,59 @@ int lay_out(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, in
     return MLDA_OK;
 }
 
-template <class T, class X, int kTiles>
+template <class T, class X>
 int multiply_few_of(mlda::MxLinearArgs a, mlda::MxArgs q, int32_t steps, hipStream_t stream) {
     constexpr bool kOwn = !std::is_void_v<X>;
     const unsigned lds = kOwn ? (unsigned)(std::min<int64_t>(a.rows, 32) * a.blocks * (mlda::kMxBytes + 1)) : 0;
     const int64_t waves = ((int64_t)a.words + mlda::kFewWords - 1) / mlda::kFewWords;
     // With fewer waves than SIMDs, and more slabs than a wave has on their way, four share their words.
-    const bool split = waves < 4 * kCus && a.blocks > 4 * mlda::kFewBlocks;
+    const bool split = waves * ((a.rows + 31) / 32) < 4 * kCus && a.blocks > 4 * mlda::kFewBlocks;
     const unsigned groups = (unsigned)(split ? waves : (waves + mlda::kFewWaves - 1) / mlda::kFewWaves);
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, kMostGroups / groups)) * 32, rows = a.rows;       // of a launch
+    constexpr int kRows = 32;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, kMostGroups / groups)) * kRows, rows = a.rows;       // of a launch
     for (int64_t row = 0; row < rows; row += most) {
         a.rows = std::min(most, rows - row);
-        const dim3 grid(groups, (unsigned)(kOwn ? (a.rows + 31) / 32 : 1)), threads(mlda::kFewWaves * mlda::kWave);
-        if (split) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, kTiles, true, 4>), grid, threads, lds, stream, a, q, steps);
-        else if (kOwn && a.blocks <= mlda::kFewBlocks) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, kTiles, false, kOwn ? 1 : 4>), grid, threads, lds, stream, a, q, steps);
-        else hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, kTiles, false, 4>), grid, threads, lds, stream, a, q, steps);
+        const dim3 grid(groups, (unsigned)((a.rows + kRows - 1) / kRows)), threads(mlda::kFewWaves * mlda::kWave);
+        if (split) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, true, 4>), grid, threads, lds, stream, a, q, steps);
+        else if (kOwn && a.blocks <= mlda::kFewBlocks) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, false, kOwn ? 1 : 4>), grid, threads, lds, stream, a, q, steps);
+        else hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, false, 4>), grid, threads, lds, stream, a, q, steps);
         RC_TRY(launched("mx4_few_kernel"));
         if constexpr (kOwn) q.x = static_cast<const X*>(q.x) + a.rows * q.stride;
+        a.x_codes += a.rows * steps * 2 * mlda::kMxBytes;
+        a.x_scales += a.rows * steps * 2;
         a.y = static_cast<T*>(a.y) + a.rows * a.y_stride;
     }
     return MLDA_OK;
 }
 
-template <class T, int kTiles, int kHalves, int kWaves>
-int multiply_tiles_of(mlda::MxTilesArgs a, hipStream_t stream) {
-    constexpr int kWords = mlda::kWaveWords * kHalves, kRows = kWaves / kHalves * kTiles * 32, kStepBytes = kHalves * 4 * mlda::kWave * (mlda::kMxBytes + 1);
-    const int32_t fit = (kLdsBytes - kWords * 4) / kStepBytes / mlda::kAhead * mlda::kAhead;
-    a.held = std::min(a.steps, fit);
-    a.slab = mlda::divisor((uint32_t)(2 * a.held));
-    const int64_t tiles = ((int64_t)a.m.words + kWords - 1) / kWords, rows = a.m.rows;
+template <class T, int kWaves, int kChunk>
+int multiply_tiles_of(const mlda::MxLinearArgs& m, int32_t steps, hipStream_t stream) {
+    mlda::MxTilesArgs a{};
+    a.m = m;
+    a.steps = steps;
+    a.once = passes_caches((double)m.rows * m.words * (double)sizeof(T));
+    constexpr int kRows = kWaves * 32, kStepBytes = mlda::kTileWords * 2 * (mlda::kMxBytes + 1);
+    const int64_t tiles = ((int64_t)m.words + mlda::kTileWords - 1) / mlda::kTileWords;
     const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / tiles) * kRows;       // of a launch
-    const unsigned lds = (unsigned)(a.held * kStepBytes + kWords * 4);
-    const auto kernel = mlda::mx4_tiles_kernel<T, kTiles, kHalves, kWaves>;
+    const unsigned lds = (unsigned)(2 * std::min(kChunk, steps) * kStepBytes);
+    const auto kernel = mlda::mx4_tiles_kernel<T, kWaves, kChunk>;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return set_error(MLDA_EHIP, "mx4_tiles_kernel's LDS", hipGetErrorString(e));
     }
-    for (int64_t row = 0; row < rows; row += most) {
-        a.m.rows = std::min(most, rows - row);
+    for (int64_t row = 0; row < m.rows; row += most) {
+        a.m.rows = std::min(most, m.rows - row);
         a.passes = (uint32_t)((a.m.rows + kRows - 1) / kRows);
         a.pass = mlda::divisor(a.passes);
         a.units = (uint32_t)(tiles * a.passes);
-        const int64_t fits = kCus * std::max<int64_t>(1, std::min<int64_t>(8 / kWaves, kLdsBytes / std::max(lds, 1u)));
-        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(a.units, fits)), dim3(kWaves * mlda::kWave), lds, stream, a);
+        constexpr int64_t kFits = kCus * (8 / kWaves);           // workgroups that the registers of the chip hold
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(a.units, kFits)), dim3(kWaves * mlda::kWave), lds, stream, a);
         RC_TRY(launched("mx4_tiles_kernel"));
         a.m.x_codes += a.m.rows * a.steps * 2 * mlda::kMxBytes;
         a.m.x_scales += a.m.rows * a.steps * 2;
         a.m.y = static_cast<T*>(a.m.y) + a.m.rows * a.m.y_stride;
     }
     return MLDA_OK;
-}
-
-template <class T>
-int multiply_tiles(const mlda::MxLinearArgs& m, int32_t steps, hipStream_t stream) {
-    mlda::MxTilesArgs a{};
-    a.m = m;
-    a.steps = steps;
-    a.once = passes_caches((double)m.rows * m.words * (double)sizeof(T));
-    const int64_t big = (((int64_t)m.words + 255) / 256) * ((m.rows + 255) / 256);
-    if (big >= kCus) return multiply_tiles_of<T, 2, 2, 8>(a, stream);
-    return multiply_tiles_of<T, 1, 1, 4>(a, stream);
 }
 
 }  // namespace
@@ -197,7 +193,7 @@ int mlda_mx_linear(const void* x, int64_t x_stride, const uint8_t* codes, const 
     if (!need || short_rows(rows, cols, words)) {
         const mlda::MxArgs q{x, x_stride, nullptr, nullptr, 0, cols, mlda::divisor((uint32_t)(blocks_of(cols) * mlda::kMxBlock * (int64_t)type_bytes(type) / 16)), false};
         return with_type(out_type, [&](auto t) {
-            return with_type(type, [&](auto u) { return multiply_few_of<decltype(t), decltype(u), 1>(a, q, 0, stream); });
+            return with_type(type, [&](auto u) { return multiply_few_of<decltype(t), decltype(u)>(a, q, 0, stream); });
         });
     }
     const int64_t blocks = held_blocks(cols);
@@ -209,9 +205,9 @@ int mlda_mx_linear(const void* x, int64_t x_stride, const uint8_t* codes, const 
     a.x_scales = x_scales;
     return with_type(out_type, [&](auto t) {
         typedef decltype(t) T;
-        if (rows <= 32) return multiply_few_of<T, void, 1>(a, mlda::MxArgs{}, steps, stream);
-        if (rows <= 64) return multiply_few_of<T, void, 2>(a, mlda::MxArgs{}, steps, stream);
-        return multiply_tiles<T>(a, steps, stream);
+        if (few_products(rows, words)) return multiply_few_of<T, void>(a, mlda::MxArgs{}, steps, stream);
+        if (rows <= 512) return multiply_tiles_of<T, 4, 8>(a, steps, stream);
+        return multiply_tiles_of<T, 8, 16>(a, steps, stream);
     });
 }
 
