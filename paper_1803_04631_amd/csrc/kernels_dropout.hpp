@@ -49,37 +49,43 @@ __device__ __forceinline__ void philox_words(uint32_t c0, uint32_t c1, uint32_t 
     out[3] = c3;
 }
 
+// Bound by memory: 300,000 x 1,000 bf16 with residual 284 us, 6.3 TB/s; ten rounds take some 100 instructions, 13 an element.  A lane draws for eight
+// neighbouring columns; where those are two pieces of 16 bytes (fp32) the lanes change them, so that a wave's loads and stores are whole lines
+// (5,682 x 9,236 fp32 133 us without, so 72).
 template <class T, bool kResidual>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
     constexpr int P = kPack<T>, kPieces = kDropCols / P;
-    const uint32_t unit = blockIdx.x * (uint32_t)kDropThreads + threadIdx.x;
-    if (unit >= a.units) return;
-    const uint32_t row = a.per_row(unit), group = unit - row * a.per_row.by;
-    const T* x = static_cast<const T*>(a.x) + (int64_t)row * a.x_stride;
-    const T* residual = static_cast<const T*>(a.residual) + (int64_t)row * a.residual_stride;
-    T* y = static_cast<T*>(a.y) + (int64_t)row * a.y_stride;
+    const uint32_t wave_unit = blockIdx.x * (uint32_t)kDropThreads + threadIdx.x / kWave * kWave, unit = wave_unit + lane_id();
+    // piece j of a lane: of unit j 64 / kPieces + lane / kPieces of the wave
+    uint32_t row[kPieces];
+    int32_t col[kPieces];
+    bool there[kPieces];
     Raw rx[kPieces], rr[kPieces];
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
-        const int32_t col = (int32_t)group * kDropCols + j * P;
-        rx[j] = load_piece(x, col, 0, a.cols, 0.0f, a.once);
-        if (kResidual) rr[j] = load_piece(residual, col, 0, a.cols, 0.0f, a.once);
+        const uint32_t of = wave_unit + j * (kWave / kPieces) + lane_id() / kPieces;
+        there[j] = of < a.units;
+        row[j] = a.per_row(min(of, a.units - 1));
+        col[j] = (int32_t)(of - row[j] * a.per_row.by) * kDropCols + lane_id() % kPieces * P;
+        if (!there[j]) continue;
+        rx[j] = load_piece(static_cast<const T*>(a.x) + (int64_t)row[j] * a.x_stride, col[j], 0, a.cols, 0.0f, a.once);
+        if (kResidual) rr[j] = load_piece(static_cast<const T*>(a.residual) + (int64_t)row[j] * a.residual_stride, col[j], 0, a.cols, 0.0f, a.once);
     }
     const uint32_t step = a.step + (a.more_steps ? (uint32_t)*a.more_steps : 0);
     const uint32_t upper = (uint32_t)(a.threshold >> 16), lower = (uint32_t)a.threshold & 0xffffu;
+    const uint32_t drawn_row = a.per_row(min(unit, a.units - 1)), group = unit - drawn_row * a.per_row.by;
     uint32_t bits[4], number[kDropCols];
-    philox_words(group, a.first_row + row, step, 1, a.key0, a.key1, bits);
+    philox_words(group, a.first_row + drawn_row, step, 1, a.key0, a.key1, bits);
     bool drawn = false;
+    uint32_t kept = 0;
 #pragma unroll
     for (int e = 0; e < kDropCols; ++e) {
         number[e] = e % 2 ? bits[e / 2] >> 16 : bits[e / 2] & 0xffffu;
         drawn |= number[e] == upper;
+        kept |= (uint32_t)(number[e] >= upper) << e;
     }
-    uint32_t kept = 0;
-#pragma unroll
-    for (int e = 0; e < kDropCols; ++e) kept |= (uint32_t)(number[e] >= upper) << e;
     if (drawn) {
-        philox_words(group, a.first_row + row, step, 2, a.key0, a.key1, bits);
+        philox_words(group, a.first_row + drawn_row, step, 2, a.key0, a.key1, bits);
 #pragma unroll
         for (int e = 0; e < kDropCols; ++e) {
             const uint32_t low = e % 2 ? bits[e / 2] >> 16 : bits[e / 2] & 0xffffu;
@@ -88,15 +94,18 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropoutArgs a) {
     }
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
+        uint32_t mine = kept;
+        if constexpr (kPieces > 1) mine = (uint32_t)__shfl((int)kept, j * (kWave / kPieces) + lane_id() / kPieces, kWave) >> lane_id() % kPieces * P;
+        if (!there[j]) continue;
         float v[P], w[P];
         unpack(rx[j], v, T());
         if (kResidual) unpack(rr[j], w, T());
 #pragma unroll
         for (int e = 0; e < P; ++e) {
-            v[e] = kept >> (j * P + e) & 1 ? v[e] * a.scale : 0.0f;       // (whatever is dropped, NaN too, is 0)
+            v[e] = mine >> e & 1 ? v[e] * a.scale : 0.0f;                 // (whatever is dropped, NaN too, is 0)
             if (kResidual) v[e] += w[e];
         }
-        store_piece(y, (int32_t)group * kDropCols + j * P, 0, a.cols, pack(v, T()), a.once);
+        store_piece(static_cast<T*>(a.y) + (int64_t)row[j] * a.y_stride, col[j], 0, a.cols, pack(v, T()), a.once);
     }
 }
 

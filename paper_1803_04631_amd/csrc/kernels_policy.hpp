@@ -6,15 +6,17 @@
 //   grad = w (kl (1 - exp(f - l)) - A (0 where clipped, else exp(d)))
 // A word of weight 0 is none: nothing of it counts, whatever its numbers are.
 //
-// Everything is in fp64: the border is then the same for every way of computing it, the KL term, a difference of nearly equal numbers, keeps
-// its bits, and sums of millions of words theirs.  Bound by memory all the same: 50e6 words, 20 bytes each, 197 us (one word to a thread at a time 277).  Few words are one workgroup's and one
-// launch; more leave partial sums, which a second launch joins in a fixed order.
+// Differences, products and sums are in fp64: the border is then the same for every way of computing it, and sums of millions of words keep their bits.
+// The exponentials are fp32's, corrected for what the difference has beyond fp32: within 3 units of roundoff (2^-24); the KL term, a difference of nearly equal
+// numbers, is a series near 0: within 12.  (In fp64 they bound the kernel: 26,154 documents of 113 words with a KL term 28.5 us, so 26.)  Bound by memory: 50e6
+// words, 20 bytes each, 197 us (one word to a thread at a time 277).  Few words are one workgroup's and one launch; more leave partial sums, which a second launch
+// joins in a fixed order.
 #pragma once
 #include "vec_io.hpp"
 
 namespace mlda {
 
-constexpr int kPolicyGroups = 1024;      // of a launch at most, each of which leaves three sums
+constexpr int kPolicyGroups = 4096;      // of a launch at most, each of which leaves three sums
 
 struct PolicyArgs {
     const float* logprobs;
@@ -50,19 +52,29 @@ __device__ __forceinline__ void rows_of_wave(const int64_t* row_ptr, int64_t row
     hi = max(a0, b0);
 }
 
-// exp(x) - x - 1 near 0, where the difference would lose bits: the first five terms of x^2 / 2 + x^3 / 6 + ..; what is left out is below 4e-13 of it, as what
-// the difference loses is below 2^-39 of it beyond. 
-constexpr double kKlNear = 0x1p-6;
-__device__ __forceinline__ double kl_near(double x) {
-    double s = __builtin_fma(x, 1.0 / 720.0, 1.0 / 120.0);
-    s = __builtin_fma(x, s, 1.0 / 24.0);
-    s = __builtin_fma(x, s, 1.0 / 6.0);
-    s = __builtin_fma(x, s, 0.5);
+// exp(d), for a d of more bits than fp32 has.
+__device__ __forceinline__ float exp_of(double d) {
+    const float high = (float)d, e = expf(high);
+    // (an infinite difference has no remainder)
+    return fabsf(high) < 128.0f ? __builtin_fmaf(e, (float)(d - (double)high), e) : e;
+}
+
+// exp(x) - x - 1 up to 1, where the difference would lose bits: ten terms of x^2 / 2 + x^3 / 6 + ..; what is left out is below 2^-27 of it.
+__device__ __forceinline__ float kl_near(float x) {
+    float s = __builtin_fmaf(x, 1.0f / 39916800.0f, 1.0f / 3628800.0f);
+    s = __builtin_fmaf(x, s, 1.0f / 362880.0f);
+    s = __builtin_fmaf(x, s, 1.0f / 40320.0f);
+    s = __builtin_fmaf(x, s, 1.0f / 5040.0f);
+    s = __builtin_fmaf(x, s, 1.0f / 720.0f);
+    s = __builtin_fmaf(x, s, 1.0f / 120.0f);
+    s = __builtin_fmaf(x, s, 1.0f / 24.0f);
+    s = __builtin_fmaf(x, s, 1.0f / 6.0f);
+    s = __builtin_fmaf(x, s, 0.5f);
     return x * x * s;
 }
 
-// kPolicyEach: neighbouring words of a thread.  A word is some 300 instructions one after the other: those of a single workgroup have a thread each if they can (330 of
-// them with a KL term 4.9 us by four, 2.8 apart).
+// kPolicyEach: neighbouring words of a thread.  A word is a long chain of instructions: those of a single workgroup have a thread each if they can (330 of them, in fp64
+// with a KL term, 4.9 us by four, 2.8 apart).
 template <int kThreads, int kPolicyEach, bool kReference>
 __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
     constexpr int kChunk = kThreads * kPolicyEach;
@@ -130,13 +142,13 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
             const bool counts = used[e] && w != 0.0;
             const double d = (double)l[e] - (double)old[e], advantage = adv[e];
             const bool over = advantage > 0.0 && d > a.high, under = advantage < 0.0 && d < a.low;
-            const double ratio = exp(d);
+            const double ratio = exp_of(d);
             double term = -(over ? a.at_high : under ? a.at_low : ratio) * advantage;
             double grad = over || under ? 0.0 : -ratio * advantage;
             clipped += counts && (over || under) ? w : 0.0;
             if (kReference) {
-                const double x = (double)ref[e] - (double)l[e], near = kl_near(x), much = exp(x) - 1.0;
-                const bool is_near = fabs(x) < kKlNear;
+                const double x = (double)ref[e] - (double)l[e], near = kl_near((float)x), much = (double)exp_of(x) - 1.0;
+                const bool is_near = fabs(x) < 1.0;
                 const double part = is_near ? near : much - x;
                 kl += counts ? w * part : 0.0;
                 term += a.kl * part;
@@ -167,17 +179,24 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
     }
 }
 
-constexpr int kPolicySumThreads = 3 * kWave;               // a wave for each sum
+constexpr int kPolicySumThreads = 1024;
 
+// A workgroup for each sum.
 __global__ __launch_bounds__(kPolicySumThreads) void policy_sums_kernel(const double* partial, int32_t groups, float* sums) {
-    const int k = threadIdx.x / kWave;
-    double part[kPolicyGroups / kWave], v = 0.0;
+    constexpr int kEach = kPolicyGroups / kPolicySumThreads;
+    __shared__ double slots[kPolicySumThreads / kWave];
+    const double* const mine = partial + blockIdx.x * kPolicyGroups;
+    double part[kEach], v = 0.0;
 #pragma unroll
-    for (int i = 0; i < kPolicyGroups / kWave; ++i) part[i] = partial[k * kPolicyGroups + min(i * kWave + lane_id(), groups - 1)];
+    for (int i = 0; i < kEach; ++i) part[i] = mine[min(i * kPolicySumThreads + (int)threadIdx.x, groups - 1)];
 #pragma unroll
-    for (int i = 0; i < kPolicyGroups / kWave; ++i) v += i * kWave + lane_id() < groups ? part[i] : 0.0;
+    for (int i = 0; i < kEach; ++i) v += i * kPolicySumThreads + (int)threadIdx.x < groups ? part[i] : 0.0;
     v = wave_sum(v);
-    if (lane_id() == 0) sums[k] = (float)v;
+    if (lane_id() == 0) slots[threadIdx.x / kWave] = v;
+    __syncthreads();
+    if (threadIdx.x >= kWave) return;
+    v = wave_sum(lane_id() < kPolicySumThreads / kWave ? slots[lane_id()] : 0.0);
+    if (lane_id() == 0) sums[blockIdx.x] = (float)v;
 }
 
 }  // namespace mlda

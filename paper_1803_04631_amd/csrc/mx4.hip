@@ -13,10 +13,13 @@ constexpr int32_t kMostProductCols = 1 << 24;    // tiles of rows have 32-bit nu
 // 1,000 x 32 x 5,000 fp32 14.3 and 8.6; but 2,048 x 128 x 141,000 bf16 181 us, so 614), others in the workspace, in whole tiles of rows and whole stretches of steps.
 bool few_rows(int64_t rows, int32_t cols) { return rows <= 16 && rows * blocks_of(cols) <= 1024; }
 bool short_rows(int64_t rows, int32_t cols, int32_t words) { return blocks_of(cols) <= 2 && rows <= ((int64_t)1 << 23) / words; }
-// Which products are few enough for a wave for each 32 x 32 of them; the others take tiles of 128 words and as many rows as a workgroup's waves have, 128
-// where there are few, else 256 (1,000 columns, bf16, us: wave for each, 128, 256).  300 x 5,000: 11.1, 13.1, 13.5; 500 x 5,000: 16.3, 13.4, 14.3; 32 x 141,000: 28, 31,
-// 42; 65 x 141,000: 66, 33, 46; 500 x 141,000: 312, 70, 75; 2,048 x 141,000: -, 268, 246.
+// Which products are few enough for a wave for each 32 x 32 of them; the others take tiles of 128 words and as many rows as a workgroup's waves have: 128, or
+// 256 where there are that many tiles and rows (1,000 columns, bf16, us: a wave for each, 128, 256).  300 x 5,000: 11.1, 13.1, 13.5; 500 x 5,000: 16.3, 13.4, 14.3;
+// 32 x 141,000: 28, 31, 42; 65 x 141,000: 66, 33, 46; 500 x 141,000: 312, 70, 75; 2,048 x 141,000: -, 268, 246; 2,932 x 1,120 of 9,205 columns: 96, 71, 76.
 bool few_products(int64_t rows, int32_t words) { return rows <= 32 || (rows + 31) / 32 <= 2048 / (((int64_t)words + 31) / 32); }
+bool many_products(int64_t rows, int32_t words) {
+    return rows > 512 && (rows + 255) / 256 * (((int64_t)words + mlda::kTileWords - 1) / mlda::kTileWords) >= 4 * kCus;
+}
 int64_t held_rows(int64_t rows) { return (rows + 31) / 32 * 32; }
 int64_t held_blocks(int32_t cols) {
     constexpr int64_t kEach = 2 * mlda::kAhead;
@@ -206,8 +209,8 @@ int mlda_mx_linear(const void* x, int64_t x_stride, const uint8_t* codes, const 
     return with_type(out_type, [&](auto t) {
         typedef decltype(t) T;
         if (few_products(rows, words)) return multiply_few_of<T, void>(a, mlda::MxArgs{}, steps, stream);
-        if (rows <= 512) return multiply_tiles_of<T, 4, 8>(a, steps, stream);
-        return multiply_tiles_of<T, 8, 16>(a, steps, stream);
+        if (many_products(rows, words)) return multiply_tiles_of<T, 8, 16>(a, steps, stream);
+        return multiply_tiles_of<T, 4, 8>(a, steps, stream);
     });
 }
 

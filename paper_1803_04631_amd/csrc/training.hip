@@ -108,7 +108,7 @@ int mlda_policy_loss(const float* logprobs, const float* old_logprobs, const flo
     else of(std::false_type());
     RC_TRY(launched("policy_kernel"));
     if (groups == 1) return MLDA_OK;
-    hipLaunchKernelGGL(mlda::policy_sums_kernel, dim3(1), dim3(mlda::kPolicySumThreads), 0, stream, a.partial, (int32_t)groups, sums);
+    hipLaunchKernelGGL(mlda::policy_sums_kernel, dim3(3), dim3(mlda::kPolicySumThreads), 0, stream, a.partial, (int32_t)groups, sums);
     return launched("policy_sums_kernel");
 }
 

@@ -1,7 +1,7 @@
 """Dropout and the policy loss on the GPU, through the public entry points, against the same in 64 bits by elementary operations.
 
 Masks have no tolerance.  A kept element is a product with a scale that is rounded to fp32, and a sum with its residual: 3 u, u = 2^-24, of the magnitudes, and one
-rounding to the type.  The policy loss is computed in fp64 and rounded once to fp32; exponentials are off by 2^-50 of themselves before that, a KL term by 2^-39 of itself.
+rounding to the type.  The policy loss has exponentials that are off by 3 u of themselves and KL terms that are off by 12 u of themselves; what is made of them in fp64 is rounded once to fp32.
 """
 import math
 
@@ -190,7 +190,7 @@ def test_dropout_refusals(ops):
 
 # ------------------------------------------------------------------------------------------ policy loss
 def policy64(l, old, advantages, weights, reference, low, high, kl):
-    """(loss, KL term, clipped weight, gradient, what the gradient may be off before it is rounded), words of weight 0 left out."""
+    """(loss, KL term, clipped weight, gradient, what the gradient may be off before it is rounded, what the sums may be), words of weight 0 left out."""
     l, old, a, w = l.double(), old.double(), advantages.double(), weights.double()
     used = w != 0
     zero = torch.zeros_like(l)
@@ -201,17 +201,20 @@ def policy64(l, old, advantages, weights, reference, low, high, kl):
     bound = torch.where(a > 0, torch.full_like(a, 1.0 + high), torch.full_like(a, 1.0 - low))     # (of two numbers it would be fp32)
     loss = -torch.where(clipped, bound, ratio) * a
     grad = torch.where(clipped, zero, -ratio * a)
-    size = grad.abs()
     term = zero
     if reference is not None:
         e = torch.where(used, reference.double(), zero) - l
         term = torch.expm1(e) - e
         loss = loss + kl * term
         grad = grad - kl * torch.expm1(e)
-        size = size + abs(kl) * torch.expm1(e).abs()
-    each = [torch.where(used, w * v, zero) for v in (loss, term, clipped.double(), grad, size)]
+    each = [torch.where(used, w * v, zero) for v in (loss, term, clipped.double(), grad)]
     terms = each[1].abs().sum()
-    return each[0].sum(), each[1].sum(), each[2].sum(), each[3], each[4].abs(), [2.0 ** -45 * each[0].abs().sum() + 2.0 ** -39 * abs(kl) * terms, 2.0 ** -39 * terms, 2.0 ** -45 * each[2].abs().sum()]
+    policies = torch.where(used & ~clipped, (w * ratio * a).abs(), zero).sum()
+    # the gradient's parts: the policy's, and the KL term's, an exponential less 1 (near 0 the difference and the KL term)
+    by_ratio = torch.where(used & ~clipped, (w * ratio * a).abs(), zero)
+    by_kl = torch.where(used, (w * kl).abs() * torch.where(e.abs() < 1, term, torch.exp(e)), zero) if reference is not None else zero
+    off = U * (3 * by_ratio + 12 * by_kl)
+    return each[0].sum(), each[1].sum(), each[2].sum(), each[3], off, [3 * U * policies + 12 * U * abs(kl) * terms + 2.0 ** -45 * each[0].abs().sum(), 12 * U * terms, 2.0 ** -45 * each[2].abs().sum()]
 
 
 def check_policy(ops, n, seed, row_ptr=None, weights=None, reference=True, low=0.2, high=0.25, kl=0.05, given=True):
@@ -230,10 +233,10 @@ def check_policy(ops, n, seed, row_ptr=None, weights=None, reference=True, low=0
         out = (at < 0) | (at >= rows)
         w = w.masked_fill(out, 0)
         a = a[at.clamp(0, max(rows - 1, 0))] if rows else torch.zeros(n, device="cuda")
-    loss, term, clipped, grad, size, sums = policy64(l, old, a, w, f, low, high, kl if reference else 0.0)
+    loss, term, clipped, grad, off, sums = policy64(l, old, a, w, f, low, high, kl if reference else 0.0)
     for x, y, s in ((got.loss, loss, sums[0]), (got.kl, term, sums[1]), (got.clipped, clipped, sums[2])):
         assert x.shape == () and abs(float(x) - float(y)) <= U * abs(float(y)) + float(s) + 2.0 ** -149
-    assert ((got.grad_logprobs.double() - grad).abs() <= U * grad.abs() + 2.0 ** -48 * size + 2.0 ** -149).all()
+    assert ((got.grad_logprobs.double() - grad).abs() <= U * (grad.abs() + off) + off + 2.0 ** -149).all()
     return got
 
 
@@ -256,9 +259,10 @@ def test_kl_term_of_like_and_unlike_models(ops, apart):
     series = sum(x ** k / math.factorial(k) for k in range(2, 13))
     term = torch.where(x.abs() < 0.16, series, torch.exp(x) - x - 1)
     want, grad = (w.double() * term).sum(), 0.5 * w.double() * -torch.where(x.abs() < 0.16, x + series, torch.exp(x) - 1)
-    assert abs(float(got.kl) - float(want)) <= (U + 2.0 ** -38) * float(want) + 2.0 ** -149
-    assert abs(float(got.loss) - 0.5 * float(want)) <= (U + 2.0 ** -38) * float(want) + 2.0 ** -149
-    assert ((got.grad_logprobs.double() - grad).abs() <= (U + 2.0 ** -38) * grad.abs() + 2.0 ** -149).all()
+    assert abs(float(got.kl) - float(want)) <= 13 * U * float(want) + 2.0 ** -149
+    assert abs(float(got.loss) - 0.5 * float(want)) <= 13 * U * float(want) + 2.0 ** -149
+    off = 0.5 * w.double() * 12 * U * torch.where(x.abs() < 1, term, torch.exp(x))
+    assert ((got.grad_logprobs.double() - grad).abs() <= U * grad.abs() + 1.01 * off + 2.0 ** -149).all()
 
 
 @pytest.mark.parametrize("lengths", [[5], [0, 0, 3, 0], [1] * 100, [300, 0, 7, 1, 0, 0, 2000, 5], [0], [], [40000] + [1, 0] * 3000])
