@@ -55,8 +55,8 @@ __device__ __forceinline__ void rows_of_wave(const int64_t* row_ptr, int64_t row
 // exp(d), for a d of more bits than fp32 has.
 __device__ __forceinline__ float exp_of(double d) {
     const float high = (float)d, e = expf(high);
-    // (an infinite difference has no remainder)
-    return fabsf(high) < 128.0f ? __builtin_fmaf(e, (float)(d - (double)high), e) : e;
+    // (an infinite difference has no remainder, and an infinite exponential nothing to correct)
+    return e < INFINITY && high > -200.0f ? __builtin_fmaf(e, (float)(d - (double)high), e) : e;
 }
 
 // exp(x) - x - 1 up to 1, where the difference would lose bits: ten terms of x^2 / 2 + x^3 / 6 + ..; what is left out is below 2^-27 of it.
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
             if (kReference) {
                 const double x = (double)ref[e] - (double)l[e], near = kl_near((float)x), much = (double)exp_of(x) - 1.0;
                 const bool is_near = fabs(x) < 1.0;
-                const double part = is_near ? near : much - x;
+                const double part = is_near ? near : much < INFINITY ? much - x : much;     // (infinity also where both are)
                 kl += counts ? w * part : 0.0;
                 term += a.kl * part;
                 grad -= a.kl * (is_near ? x + near : much);

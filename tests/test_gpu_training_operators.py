@@ -299,6 +299,22 @@ def test_words_without_weight_are_none(ops):
     assert torch.isfinite(ops.policy_loss(l, old, a, w).loss)
 
 
+def test_far_words(ops):
+    """Differences at which exponentials are infinite, subnormal or zero."""
+    d = torch.tensor([88.0, 88.72, 88.8, 100.0, 127.0, 200.0, 1e30, INF, -80.0, -88.0, -95.0, -104.0, -150.0, -300.0, -1e30, -INF], device="cuda")
+    zero, one = torch.zeros_like(d), torch.ones_like(d)
+    got = ops.policy_loss(d, zero, -one, one, high=INF, low=1.0)            # grad = exp(d)
+    want = torch.exp(d.double())
+    inside = want < 3.4e38
+    assert (got.grad_logprobs[~inside] == INF).all() and float(got.loss) == INF
+    assert ((got.grad_logprobs.double() - want).abs() <= 4 * U * want + 2.0 ** -149)[inside].all()
+    got = ops.policy_loss(d, zero, one, one)                                # clipped above, nothing is infinite
+    assert float(got.clipped) == 8 and (got.grad_logprobs[:8] == 0).all() and torch.isfinite(got.loss)
+    got = ops.policy_loss(zero, zero, zero, one, d, kl=1.0)                 # grad = 1 - exp(d)
+    assert float(got.kl) == INF and (got.grad_logprobs[~inside] == -INF).all()
+    assert ((got.grad_logprobs.double() - (1 - want)).abs() <= 4 * U * want + U + 2.0 ** -149)[inside].all()
+
+
 def test_policy_gradient_is_that_of_differences(ops):
     g = gen(9)
     n = 40
