@@ -69,7 +69,7 @@ int quantize(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, i
 
 // A product's rows, in steps of two blocks.
 int lay_out(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, int64_t rows, int32_t cols, int32_t type, int32_t steps, hipStream_t stream) {
-    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / steps) * 32;      // of a launch
+    const int64_t most = std::max<int64_t>(1, 4 * kMostGroups / steps) * 32;         // of a launch
     for (int64_t row = 0; row < rows; row += most) {
         const int64_t n = std::min(most, rows - row), units = (n + 31) / 32 * steps;
         const mlda::MxArgs a{static_cast<const char*>(x) + row * x_stride * (int64_t)type_bytes(type), x_stride, codes + row * steps * 2 * mlda::kMxBytes,
