@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
         for (int i = 0; i < 4; ++i)
             turned[wave][(8 * i + lane / kFewBlocks) * kFewBlocks + (block ^ (lane / kFewBlocks))] = first + block < a.blocks ? w[buffer][i] : Codes{0, 0, 0, 0};
         const uint64_t word_scales = placed_scales(ws[buffer], first, a.blocks) >> 8 * part;
-        // (a wave's own room: its reads and writes are in order)
+        __builtin_amdgcn_wave_barrier();                   // (a wave's own room: its reads and writes are in order)
         auto step = [&](auto which) {
             constexpr int s = decltype(which)::value;
             if (first + 2 * s >= a.blocks) return;
@@ -309,6 +309,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
         step(std::integral_constant<int, 1>());
         step(std::integral_constant<int, 2>());
         step(std::integral_constant<int, 3>());
+        __builtin_amdgcn_wave_barrier();
     };
     for (int32_t slab = begin; slab < slabs; slab += kFewAhead * stride) {
 #pragma unroll

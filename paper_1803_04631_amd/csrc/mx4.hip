@@ -92,18 +92,17 @@ int multiply_few_of(mlda::MxLinearArgs a, mlda::MxArgs q, int32_t steps, hipStre
     // With fewer waves than SIMDs, and more slabs than a wave has on their way, four share their words.
     const bool split = waves * ((a.rows + 31) / 32) < 4 * kCus && a.blocks > 4 * mlda::kFewBlocks;
     const unsigned groups = (unsigned)(split ? waves : (waves + mlda::kFewWaves - 1) / mlda::kFewWaves);
-    constexpr int kRows = 32;
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, kMostGroups / groups)) * kRows, rows = a.rows;       // of a launch
-    for (int64_t row = 0; row < rows; row += most) {
-        a.rows = std::min(most, rows - row);
-        const dim3 grid(groups, (unsigned)((a.rows + kRows - 1) / kRows)), threads(mlda::kFewWaves * mlda::kWave);
+    constexpr int64_t kMost = 65535 * 32;                    // rows of a launch
+    const int64_t rows = a.rows;
+    for (int64_t row = 0; row < rows; row += kMost) {
+        a.rows = std::min(kMost, rows - row);
+        const dim3 grid(groups, (unsigned)((a.rows + 31) / 32)), threads(mlda::kFewWaves * mlda::kWave);
         if (split) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, true, 4>), grid, threads, lds, stream, a, q, steps);
         else if (kOwn && a.blocks <= mlda::kFewBlocks) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, false, kOwn ? 1 : 4>), grid, threads, lds, stream, a, q, steps);
         else hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, false, 4>), grid, threads, lds, stream, a, q, steps);
         RC_TRY(launched("mx4_few_kernel"));
+        // (rows that are laid out are few enough for one launch)
         if constexpr (kOwn) q.x = static_cast<const X*>(q.x) + a.rows * q.stride;
-        a.x_codes += a.rows * steps * 2 * mlda::kMxBytes;
-        a.x_scales += a.rows * steps * 2;
         a.y = static_cast<T*>(a.y) + a.rows * a.y_stride;
     }
     return MLDA_OK;
@@ -117,26 +116,19 @@ int multiply_tiles_of(const mlda::MxLinearArgs& m, int32_t steps, hipStream_t st
     a.once = passes_caches((double)m.rows * m.words * (double)sizeof(T));
     constexpr int kRows = kWaves * 32, kStepBytes = mlda::kTileWords * 2 * (mlda::kMxBytes + 1);
     const int64_t tiles = ((int64_t)m.words + mlda::kTileWords - 1) / mlda::kTileWords;
-    const int64_t most = std::max<int64_t>(1, ((int64_t)1 << 30) / tiles) * kRows;       // of a launch
+    a.passes = (uint32_t)((m.rows + kRows - 1) / kRows);
+    if ((m.rows + kRows - 1) / kRows > ((int64_t)1 << 30) / tiles) return refuse("4-bit product: more than 2^30 tiles of rows and words");
+    a.pass = mlda::divisor(a.passes);
+    a.units = (uint32_t)(tiles * a.passes);
     const unsigned lds = (unsigned)(2 * std::min(kChunk, steps) * kStepBytes);
     const auto kernel = mlda::mx4_tiles_kernel<T, kWaves, kChunk>;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return set_error(MLDA_EHIP, "mx4_tiles_kernel's LDS", hipGetErrorString(e));
     }
-    for (int64_t row = 0; row < m.rows; row += most) {
-        a.m.rows = std::min(most, m.rows - row);
-        a.passes = (uint32_t)((a.m.rows + kRows - 1) / kRows);
-        a.pass = mlda::divisor(a.passes);
-        a.units = (uint32_t)(tiles * a.passes);
-        constexpr int64_t kFits = kCus * (8 / kWaves);           // workgroups that the registers of the chip hold
-        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(a.units, kFits)), dim3(kWaves * mlda::kWave), lds, stream, a);
-        RC_TRY(launched("mx4_tiles_kernel"));
-        a.m.x_codes += a.m.rows * a.steps * 2 * mlda::kMxBytes;
-        a.m.x_scales += a.m.rows * a.steps * 2;
-        a.m.y = static_cast<T*>(a.m.y) + a.m.rows * a.m.y_stride;
-    }
-    return MLDA_OK;
+    constexpr int64_t kFits = kCus * (8 / kWaves);           // workgroups that the registers of the chip hold
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(a.units, kFits)), dim3(kWaves * mlda::kWave), lds, stream, a);
+    return launched("mx4_tiles_kernel");
 }
 
 }  // namespace

@@ -221,6 +221,55 @@ def test_a_row_does_not_depend_on_its_neighbours(ops):
     assert torch.equal(turned.flip(0), whole)
 
 
+def test_more_than_32_bits_of_offsets(ops):
+    """Results, codes and rows whose places in memory do not fit 32 bits, and rows of several launches."""
+    g = gen(12)
+    words = 70_000_003                                                     # 33 rows of them: 4.6 GB
+    weight = ops.mx4_quantize(randn(g, 1, 32).expand(1000, 32) * torch.exp(randn(g, 1000, 1)))
+    weight = ops.Mx4(weight.codes.repeat(words // 1000 + 1, 1)[:words].contiguous(), weight.scales.repeat(words // 1000 + 1, 1)[:words].contiguous(), 32)
+    for rows in (2, 33):
+        x = randn(g, rows, 32, dtype=torch.bfloat16)
+        got = ops.mx4_linear(x, weight)
+        want = ops.mx4_linear(x, ops.Mx4(weight.codes[:1000], weight.scales[:1000], 32))
+        for a in (0, 33_000_000, 69_999_000):
+            assert torch.equal(got[:, a:a + 1000], want)
+        assert torch.equal(got[:, 70_000_000:], want[:, :3])
+        del got
+    x = randn(g, 34_000_003, 33, dtype=torch.bfloat16)                     # laid out by several launches
+    weight = weights(ops, g, 3, 33)
+    got = ops.mx4_linear(x, weight)
+    for a in (0, 17_000_000, 33_554_400, 34_000_003 - 100):
+        check_linear(ops, x[a:a + 100], weight, None, got[a:a + 100])
+    x = randn(g, 3_000_001, 5)                                             # short rows: as many as several launches have
+    weight = weights(ops, g, 2, 5)
+    got = ops.mx4_linear(x, weight)
+    for a in (0, 2_097_000, 3_000_001 - 100):
+        check_linear(ops, x[a:a + 100], weight, None, got[a:a + 100])
+    del x, got
+    x = torch.zeros(1_050_000, 8200, dtype=torch.bfloat16, device="cuda")  # 17 GB, more than 2^30 pieces
+    some = [0, 524_000, 1_047_530, 1_049_950]
+    for a in some:
+        x[a:a + 50] = randn(g, 50, 8200, dtype=torch.bfloat16)
+    q = ops.mx4_quantize(x)
+    for a in some:
+        part = ops.mx4_quantize(x[a:a + 50])
+        assert torch.equal(q.codes[a:a + 50], part.codes) and torch.equal(q.scales[a:a + 50], part.scales)
+    back = ops.mx4_dequantize(q, out=x)
+    for a in some:
+        assert torch.equal(back[a:a + 50], ops.mx4_dequantize(ops.Mx4(q.codes[a:a + 50], q.scales[a:a + 50], 8200), torch.bfloat16))
+    assert not back[100:524_000:997].any()
+
+
+def test_in_inference_mode(ops):
+    g = gen(13)
+    with torch.inference_mode():
+        x, weight = randn(g, 70, 100), weights(ops, g, 300, 100)
+        out = torch.empty(70, 300, device="cuda")
+        ops.mx4_linear(x, weight, out=out)
+        check_linear(ops, x, weight, None, out)
+        assert ops.mx4_dequantize(ops.mx4_quantize(x, out=ops.mx4_quantize(x))).shape == (70, 100)
+
+
 def test_nothing_to_do(ops):
     g = gen(1)
     weight = weights(ops, g, 20, 40)

@@ -169,6 +169,30 @@ def test_dropout_draws_another_mask_at_each_replay(ops):
     assert torch.equal(z, y)
 
 
+def test_dropout_of_more_than_32_bits_of_elements(ops):
+    x = torch.ones(1_050_000, 8200, dtype=torch.bfloat16, device="cuda")   # 17 GB: rows of two launches
+    y = ops.dropout(x, 0.25, 5, 6, first_row=7)
+    for a in (0, 300_000, 1_047_500, 1_049_950):
+        check_dropout(y[a:a + 50], x[a:a + 50], kept((50, 8200), 0.25, 5, 6, 7 + a), 0.25)
+
+
+def test_in_inference_mode(ops):
+    g = gen(13)
+    with torch.inference_mode():
+        x = randn(g, 30, 50)
+        y = ops.dropout(x, 0.5, 1, residual=x)
+        ops.dropout(x, 0.5, 1, residual=x, out=x)
+        assert torch.equal(x, y)
+        l, old, a = randn(g, 5000), randn(g, 5000), randn(g, 5000)
+        got = ops.policy_loss(l, old, a)
+        loss = float(got.loss)
+        got.kl.add_(1)
+        assert float(got.loss) == loss and float(got.kl) == 1
+    got = ops.policy_loss(l.clone(), old.clone(), a.clone())
+    total = got.loss + got.kl
+    assert float(total) == float(got.loss) and got.loss.is_contiguous() and got.loss.storage_offset() == 0 and got.clipped.storage_offset() == 2
+
+
 def test_dropout_refusals(ops):
     from paper_1803_04631_amd import MldaError
     x = torch.ones(4, 10, device="cuda")
