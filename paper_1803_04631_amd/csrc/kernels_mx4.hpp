@@ -349,24 +349,18 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
 constexpr int kAhead = 4;                // steps of two blocks, which share a word of scales
 constexpr int kTileWords = 128;
 
-// Four neighbouring elements, of which `n` or all are there.
+// Four neighbouring elements, wherever they lie.
 template <class T>
-__device__ __forceinline__ void store_four(T* p, const float (&v)[4], int64_t n, bool once) {
+__device__ __forceinline__ void store_four(T* p, const float (&v)[4], bool once) {
     typedef T Four __attribute__((ext_vector_type(4)));
     typedef Four Anywhere __attribute__((aligned(sizeof(T)), may_alias));
     const Four four = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-    if (n >= 4) {
-        if (once) __builtin_nontemporal_store(four, reinterpret_cast<Anywhere*>(p));
-        else *reinterpret_cast<Anywhere*>(p) = four;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < n) p[i] = (T)v[i];
-    }
+    if (once) __builtin_nontemporal_store(four, reinterpret_cast<Anywhere*>(p));
+    else *reinterpret_cast<Anywhere*>(p) = four;
 }
 
 struct MxTilesArgs {
-    MxLinearArgs m;                      // x in the order above
+    MxLinearArgs m;                      // x in the order above, kTileWords words at least
     int32_t steps;                       // of two blocks, a multiple of kAhead
     uint32_t passes;                     // through all rows
     uint32_t units;                      // word tiles times passes
@@ -397,20 +391,23 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void mx4_tiles_kernel(MxTilesArg
         return (int32_t)(n < whole ? in_round * groups + group : rounds * groups + in_round);
     };
 
+    // The last tile ends with the words, and does some of the one before again, the same bits: the workgroup that has it is what a launch waits for (2,048 x
+    // 20,095 words of 100 columns bf16 41 us with a question for each row's last words, so 28).
+    auto first_word = [&](int32_t tile) { return min((int64_t)tile * kTileWords, (int64_t)m.words - kTileWords); };
+
     // The words' codes and scales of a chunk: on their way, then held.
     Codes way[kPieces];
     uint64_t way_scales;
     const int scale_word = thread % kTileWords, scale_block = thread / kTileWords * 8;
     auto send_for = [&](int32_t tile, int32_t chunk) {
-        const int64_t word0 = (int64_t)tile * kTileWords;
-        const int words = (int)min((int64_t)kTileWords, m.words - word0);
+        const int64_t word0 = first_word(tile);
         const uint8_t* codes = m.codes + word0 * m.blocks * kMxBytes;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             const int at = j * kThreads + thread, word = at / (2 * kChunk), block = chunk * 2 * kChunk + at % (2 * kChunk);
-            way[j] = *reinterpret_cast<const Codes*>(codes + ((int64_t)min(word, words - 1) * m.blocks + min(block, m.blocks - 1)) * kMxBytes);
+            way[j] = *reinterpret_cast<const Codes*>(codes + ((int64_t)word * m.blocks + min(block, m.blocks - 1)) * kMxBytes);
         }
-        way_scales = load_scales(m.scales + (word0 + min(scale_word, words - 1)) * m.blocks, chunk * 2 * kChunk + scale_block, m.blocks);
+        way_scales = load_scales(m.scales + (word0 + scale_word) * m.blocks, chunk * 2 * kChunk + scale_block, m.blocks);
     };
     auto hold = [&](int slot, int32_t chunk) {
         Codes* const to = held + slot * slot_steps * 4 * kWave;
@@ -454,11 +451,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void mx4_tiles_kernel(MxTilesArg
     float bias[4];
     int32_t bias_of = -1;
     for (uint32_t n = 0; n < count; ++n) {
-        const int64_t word = (int64_t)tile * kTileWords + 4 * col;
+        const int64_t word = first_word(tile) + 4 * col;
         if (bias_of != tile) {
             bias_of = tile;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) bias[i] = word + i < m.words ? bias_at<T>(m, (int32_t)(word + i)) : 0.0f;
+            for (int i = 0; i < 4; ++i) bias[i] = bias_at<T>(m, (int32_t)(word + i));
         }
         uint32_t next_pass = pass;
         const int32_t next_tile = n + 1 < count ? tile_of(n + 1, next_pass) : tile;
@@ -517,6 +514,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void mx4_tiles_kernel(MxTilesArg
         __builtin_amdgcn_sched_barrier(0);                 // (the next rows' loads before the stores: they are waited for in order)
         const int64_t row0 = ((int64_t)pass * kWaves + wave) * 32 + 4 * part;
         T* const y = static_cast<T*>(m.y) + row0 * m.y_stride + word;
+        const int64_t rows_here = m.rows - row0;
         auto store = [&](bool all) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
@@ -524,10 +522,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void mx4_tiles_kernel(MxTilesArg
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = acc[i][j] + bias[i];
-                if (all || row0 + down < m.rows) store_four(y + down * m.y_stride, v, all ? 4 : m.words - word, a.once);
+                if (all || down < rows_here) store_four(y + down * m.y_stride, v, a.once);
             }
         };
-        if (((int64_t)pass * kWaves + wave + 1) * 32 <= m.rows && (int64_t)(tile + 1) * kTileWords <= m.words) store(true);
+        if (((int64_t)pass * kWaves + wave + 1) * 32 <= m.rows) store(true);
         else store(false);
         tile = next_tile;
         pass = next_pass;

@@ -16,7 +16,7 @@ bool short_rows(int64_t rows, int32_t cols, int32_t words) { return blocks_of(co
 // Which products are few enough for a wave for each 32 x 32 of them; the others take tiles of 128 words and as many rows as a workgroup's waves have: 128, or
 // 256 where there are that many tiles and rows (1,000 columns, bf16, us: a wave for each, 128, 256).  300 x 5,000: 11.1, 13.1, 13.5; 500 x 5,000: 16.3, 13.4, 14.3;
 // 32 x 141,000: 28, 31, 42; 65 x 141,000: 66, 33, 46; 500 x 141,000: 312, 70, 75; 2,048 x 141,000: -, 268, 246; 2,932 x 1,120 of 9,205 columns: 96, 71, 76.
-bool few_products(int64_t rows, int32_t words) { return rows <= 32 || (rows + 31) / 32 <= 2048 / (((int64_t)words + 31) / 32); }
+bool few_products(int64_t rows, int32_t words) { return rows <= 32 || words < mlda::kTileWords || (rows + 31) / 32 <= 2048 / (((int64_t)words + 31) / 32); }
 bool many_products(int64_t rows, int32_t words) {
     return rows > 512 && (rows + 255) / 256 * (((int64_t)words + mlda::kTileWords - 1) / mlda::kTileWords) >= 4 * kCus;
 }
@@ -101,8 +101,9 @@ int multiply_few_of(mlda::MxLinearArgs a, mlda::MxArgs q, int32_t steps, hipStre
         else if (kOwn && a.blocks <= mlda::kFewBlocks) hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, false, kOwn ? 1 : 4>), grid, threads, lds, stream, a, q, steps);
         else hipLaunchKernelGGL((mlda::mx4_few_kernel<T, X, false, 4>), grid, threads, lds, stream, a, q, steps);
         RC_TRY(launched("mx4_few_kernel"));
-        // (rows that are laid out are few enough for one launch)
         if constexpr (kOwn) q.x = static_cast<const X*>(q.x) + a.rows * q.stride;
+        a.x_codes += a.rows * steps * 2 * mlda::kMxBytes;
+        a.x_scales += a.rows * steps * 2;
         a.y = static_cast<T*>(a.y) + a.rows * a.y_stride;
     }
     return MLDA_OK;
