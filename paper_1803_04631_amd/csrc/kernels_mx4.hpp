@@ -344,8 +344,9 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
 // The columns of an instruction's result are the words 4 c + i of its four matrices i: a lane has four neighbouring words of a row, and a
 // wave stores 256 bytes or more of it at once.
 //
-// Bound, at 1,000 columns, by writing: a line that two workgroups write a part of costs memory more than two, so that 141,000 bf16 words (rows 16 bytes off a line
-// from one to the next) take 180 us to store and 140,800 116; the matrix instructions take 90 us, which power limits.
+// Bound, at 1,000 columns, by power: the clock falls from 2.4 to 1.1 .. 1.4 GHz (2.2 where all words are zeros, and 212 us); the matrix instructions alone would take 90 us. At
+// 100 columns by writing: a line that two workgroups write a part of costs memory more than two lines do, so that 2,048 rows of 141,000 bf16 words, each 16 bytes further
+// off a line than the one before, take 172 us and rows of 140,928, which are whole lines, 131.
 constexpr int kAhead = 4;                // steps of two blocks, which share a word of scales
 constexpr int kTileWords = 128;
 
