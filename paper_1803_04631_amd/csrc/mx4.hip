@@ -9,10 +9,14 @@ int64_t blocks_of(int32_t cols) { return ((int64_t)cols + mlda::kMxBlock - 1) / 
 
 constexpr int32_t kMostProductCols = 1 << 24;    // tiles of rows have 32-bit numbers of pieces
 
-// How a product's rows are held in 4 bits: few, and short ones of a small product, by each workgroup for itself (1 x 1,000 x 141,000 fp32 with a launch for the row 27 us, so 19;
-// 1,000 x 32 x 5,000 fp32 14.3 and 8.6; but 2,048 x 128 x 141,000 bf16 181 us, so 614), others in the workspace, in whole tiles of rows and whole stretches of steps.
+// How a product's rows are held in 4 bits: few, and short ones of a small product, by each workgroup for itself, others in the workspace, in whole tiles of rows
+// and whole stretches of steps.  With a launch for the rows, and so, us: 1 x 1,000 x 141,000 fp32 27, 19; 1,000 x 32 x 5,000 fp32 12.6, 8.4; 65 x 128 x 64,000 bf16
+// 9.8, 9.3; 1,000 x 128 x 4,000 bf16 9.3, 8.2; 1,000 x 224 x 2,300 bf16 9.3, 8.3; 250 x 256 x 8,000 fp16 8.6, 7.1.  But 1,000 x 32 x 16,000 bf16 15.6, 19.3;
+// 2,000 x 128 x 4,000 bf16 11.4, 13.7; 2,000 x 200 x 4,000 bf16 12.1, 16.8; 300 x 500 x 3,000 bf16 9.4, 10.5.
 bool few_rows(int64_t rows, int32_t cols) { return rows <= 16 && rows * blocks_of(cols) <= 1024; }
-bool short_rows(int64_t rows, int32_t cols, int32_t words) { return blocks_of(cols) <= 2 && rows <= ((int64_t)1 << 23) / words; }
+bool short_rows(int64_t rows, int32_t cols, int32_t words) {
+    return blocks_of(cols) <= 8 && rows <= ((int64_t)1 << 24) / std::max(blocks_of(cols), (int64_t)2) / words;
+}
 // Which products are few enough for a wave for each 32 x 32 of them; the others take tiles of 128 words and as many rows as a workgroup's waves have: 128, or
 // 256 where there are that many tiles and rows (1,000 columns, bf16, us: a wave for each, 128, 256).  300 x 5,000: 11.1, 13.1, 13.5; 500 x 5,000: 16.3, 13.4, 14.3;
 // 32 x 141,000: 28, 31, 42; 65 x 141,000: 66, 33, 46; 500 x 141,000: 312, 70, 75; 2,048 x 141,000: -, 268, 246; 2,932 x 1,120 of 9,205 columns: 96, 71, 76.

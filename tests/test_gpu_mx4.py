@@ -158,7 +158,8 @@ def weights(ops, g, words, cols):
 LINEAR = [(1, 1, 1), (1, 1000, 5000), (1, 33, 17), (2, 32, 16), (3, 129, 65), (15, 127, 63), (16, 128, 64), (17, 1537, 409), (33, 513, 130), (64, 256, 129),
           (65, 95, 257), (100, 1000, 1003), (128, 2048, 128), (129, 640, 255), (200, 32, 5000), (255, 300, 300), (257, 160, 513), (1, 40001, 33), (7, 65535, 5),
           (300, 5000, 70), (1000, 8, 60), (513, 1100, 1030), (1100, 100, 15003), (601, 1500, 30011), (300, 1000, 40009),
-          (65, 700, 70001), (2100, 40, 4001), (1025, 3000, 2500), (300, 5000, 9001), (4099, 130, 2049), (70000, 70, 128), (20000, 300, 127), (33000, 100, 129), (3000, 65, 1001)]
+          (65, 700, 70001), (2100, 40, 4001), (1025, 3000, 2500), (300, 5000, 9001), (4099, 130, 2049), (70000, 70, 128), (20000, 300, 127), (33000, 100, 129), (3000, 65, 1001),
+          (700, 256, 2900), (999, 225, 255), (2600, 200, 900), (31, 250, 9000), (130, 161, 3001), (512, 91, 300)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -193,6 +194,20 @@ def test_linear_of_odd_numbers(ops, rows):
     assert torch.isnan(got[rows // 2]).all() and torch.isnan(got[:, [7, 330]]).all()
     if rows > 2:
         assert not torch.isnan(got[1, 8:330]).any() or rows // 2 == 1
+
+
+@pytest.mark.parametrize("cols", [31, 64, 200, 256])
+def test_short_rows_of_odd_numbers(ops, cols):
+    """As above, for rows that a product's workgroups turn into 4 bits for themselves."""
+    g = gen(cols)
+    x, w = randn(g, 77, cols), randn(g, 331, cols)
+    x[38, cols - 1], x[40, 0] = INF, NAN
+    w[7, 0], w[330, cols - 1] = NAN, -INF
+    x[0], w[3], w[5], w[6] = 0.0, 0.0, w[5] * 2.0 ** -140, w[6] * 2.0 ** 100
+    weight = ops.mx4_quantize(w)
+    got = ops.mx4_linear(x, weight)
+    check_linear(ops, x, weight, None, got)
+    assert torch.isnan(got[[38, 40]]).all() and torch.isnan(got[:, [7, 330]]).all() and not torch.isnan(got[1:38, 8:330]).any()
 
 
 @pytest.mark.parametrize("rows", [1, 16, 65, 300])
