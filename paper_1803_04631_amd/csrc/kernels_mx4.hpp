@@ -216,7 +216,7 @@ __device__ __forceinline__ uint64_t placed_scales(uint64_t s, int32_t first, int
 }
 
 // Few rows (or words).  A wave has 32 words and 32 rows.  Its words' codes come straight from memory, 128 bytes of a word at a time (a line, or two that
-// the next slab meets again) and kFewAhead such slabs on their way, and through LDS into the instructions' order: bound by reading them.  Rows that are few enough are put into 4 bits by each workgroup for itself, while its words' codes are on their way (X: their type); others
+// the next slab meets again) and kFewAhead such slabs on their way, and through LDS into the instructions' order: bound by reading them.  Rows that are few or short enough are put into 4 bits by each workgroup for itself, while its words' codes are on their way (X: their type); others
 // (X = void) are laid out by mx4_fragments_kernel and come from the L2 cache.  With kSplit the four waves of a workgroup share their words'
 // slabs, and their sums are joined in a fixed order.
 constexpr int kFewBlocks = 8;            // of a slab
@@ -344,9 +344,11 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_kernel(MxLinearArgs
 // The columns of an instruction's result are the words 4 c + i of its four matrices i: a lane has four neighbouring words of a row, and a
 // wave stores 256 bytes or more of it at once.
 //
-// Bound, at 1,000 columns, by power: the clock falls from 2.4 to 1.1 .. 1.4 GHz (2.2 where all words are zeros, and 212 us); the matrix instructions alone would take 90 us. At
-// 100 columns by writing: a line that two workgroups write a part of costs memory more than two lines do, so that 2,048 rows of 141,000 bf16 words, each 16 bytes further
-// off a line than the one before, take 172 us and rows of 140,928, which are whole lines, 131.
+// Bound, at 1,000 columns, by products and stores that overlap only in part: 2,048 x 141,000 bf16 takes 233 us (212 with weights that are all zeros, for which the clock stays
+// higher), the products without stores 176, stores alone 169, matrix instructions alone 90.  At 100 columns by writing: a line that two workgroups write a part of
+// costs memory more than two lines do, so that rows of 141,000 words, each 16 bytes further off a line than the one before, take 169 us and rows of 140,928, which are
+// whole lines, 129.  (Rows held in registers by waves that go along the words and write whole lines only, as what is left of a line is kept in LDS, write at 110, but
+// with the products it took 284 .. 318: what the lines cost in instructions is more than they save.  Rows' codes 7 steps ahead: no difference.)
 constexpr int kAhead = 4;                // steps of two blocks, which share a word of scales
 constexpr int kTileWords = 128;
 

@@ -18,9 +18,9 @@ bool short_rows(int64_t rows, int32_t cols, int32_t words) {
     return blocks_of(cols) <= 8 && rows <= ((int64_t)1 << 24) / std::max(blocks_of(cols), (int64_t)2) / words;
 }
 // Which products are few enough for a wave for each 32 x 32 of them; the others take tiles of 128 words and as many rows as a workgroup's waves have: 128, or
-// 256 where there are that many tiles and rows (1,000 columns, bf16, us: a wave for each, 128, 256).  300 x 5,000: 11.1, 13.1, 13.5; 500 x 5,000: 16.3, 13.4, 14.3;
-// 32 x 141,000: 28, 31, 42; 65 x 141,000: 66, 33, 46; 500 x 141,000: 312, 70, 75; 2,048 x 141,000: -, 268, 246; 2,932 x 1,120 of 9,205 columns: 96, 71, 76.
-bool few_products(int64_t rows, int32_t words) { return rows <= 32 || words < mlda::kTileWords || (rows + 31) / 32 <= 2048 / (((int64_t)words + 31) / 32); }
+// 256 where there are that many tiles and rows (1,000 columns, bf16, us: a wave for each, 128, 256).  300 x 3,000: 9.9, 10.1, -; 100 x 8,516: 10.0, 9.5, -; 300 x 5,000: 11.4, 10.5,
+// 11.0; 32 x 141,000: 28.6, 27.7, 39.9; 65 x 141,000: 55, 29, 41; 500 x 141,000: 246, 66, 70; 2,048 x 141,000: 958, 246, 232; 2,932 x 1,120 of 9,205 columns: 85, 62, 63.
+bool few_products(int64_t rows, int32_t words) { return rows <= 32 || words < mlda::kTileWords || (rows + 31) / 32 <= 1024 / (((int64_t)words + 31) / 32); }
 bool many_products(int64_t rows, int32_t words) {
     return rows > 512 && (rows + 255) / 256 * (((int64_t)words + mlda::kTileWords - 1) / mlda::kTileWords) >= 4 * kCus;
 }

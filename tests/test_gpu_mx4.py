@@ -159,7 +159,7 @@ LINEAR = [(1, 1, 1), (1, 1000, 5000), (1, 33, 17), (2, 32, 16), (3, 129, 65), (1
           (65, 95, 257), (100, 1000, 1003), (128, 2048, 128), (129, 640, 255), (200, 32, 5000), (255, 300, 300), (257, 160, 513), (1, 40001, 33), (7, 65535, 5),
           (300, 5000, 70), (1000, 8, 60), (513, 1100, 1030), (1100, 100, 15003), (601, 1500, 30011), (300, 1000, 40009),
           (65, 700, 70001), (2100, 40, 4001), (1025, 3000, 2500), (300, 5000, 9001), (4099, 130, 2049), (70000, 70, 128), (20000, 300, 127), (33000, 100, 129), (3000, 65, 1001),
-          (700, 256, 2900), (999, 225, 255), (2600, 200, 900), (31, 250, 9000), (130, 161, 3001), (512, 91, 300)]
+          (700, 256, 2900), (999, 225, 255), (2600, 200, 900), (31, 250, 9000), (130, 161, 3001), (512, 91, 300), (40, 700, 20001), (40, 1000, 25000), (1000, 600, 1500)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
