@@ -336,9 +336,9 @@ int mlda_clip_grads(const void* const* tensors, void* const* out, const int64_t*
                     double max_norm, float* norm, void* dev_workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
- * Matrices in microscaled 4-bit floating point: rows of cols columns (1 .. 2^30) in blocks of 32, whose last may be short.  With a the greatest
- * magnitude of a block its scale is the least 2^s, s >= -127, with a < 7 2^s, and x is held as x / 2^s rounded to nearest, ties to even, among
- * 0, 1/2, 1, 3/2, 2, 3, 4, 6 (the codes 0 .. 7; 8 more: negative).  What is held is within a fifth of x, or within 2^s / 4.
+ * Matrices in microscaled 4-bit floating point: rows of cols columns (1 .. 2^30; up to 2^54 elements) in blocks of 32, whose last may be short.
+ * With a the greatest magnitude of a block its scale is the least 2^s, s >= -127, with a < 7 2^s, and x is held as x / 2^s rounded to nearest, ties
+ * to even, among 0, 1/2, 1, 3/2, 2, 3, 4, 6 (the codes 0 .. 7; 8 more: negative).  What is held is within a fifth of x, or within 2^s / 4.
  *   codes    rows x blocks x 16 bytes, 16-byte aligned: column 2j of a row is the lower half of its byte j, 2j + 1 the upper; columns behind
  *            the last have the code 0 (mlda_mx_linear relies on that)
  *   scales   rows x blocks bytes: s + 127; 255: the block holds NaN or infinity, and stands for NaN as a whole

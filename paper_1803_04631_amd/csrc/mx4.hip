@@ -35,6 +35,7 @@ size_t held_bytes(int64_t rows, int32_t cols) {
 
 int check_mx4(int64_t rows, int32_t cols, int32_t type) {
     if (rows < 0 || cols < 1 || cols > kMostCols) return refuse("4-bit matrix: need rows >= 0 and 1 <= cols <= 2^30");
+    if (rows > ((int64_t)1 << 54) / cols) return refuse("4-bit matrix: need rows * cols <= 2^54");            // (whose bytes 64 bits count)
     if (!known_type(type)) return refuse("4-bit matrix: unknown type");
     return MLDA_OK;
 }

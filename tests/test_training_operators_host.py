@@ -42,6 +42,18 @@ def test_quantize_refusals(lib):
         assert call(rows=0, x=None, codes=None, scales=None) == 0
 
 
+@pytest.mark.parametrize("rows,cols", [(2 ** 62, 2 ** 20), (2 ** 63 - 1, 1), (2 ** 54 + 1, 1), (2 ** 31, 2 ** 24)])
+def test_no_size_runs_over(lib, rows, cols):
+    """More elements than any memory has, whose bytes 64 bits could not count."""
+    n = ctypes.c_size_t(5)
+    refused(lib, lib.mlda_mx_linear_workspace_bytes(rows, cols, ctypes.addressof(n)), word="4-bit")
+    refused(lib, lib.mlda_mx_quantize(P, cols, P, P, rows, cols, FP32, None), word="4-bit")
+    refused(lib, lib.mlda_mx_dequantize(P, P, P, cols, rows, cols, FP32, None), word="4-bit")
+    refused(lib, lib.mlda_mx_linear(P, cols, P, P, None, 2 * P, 50, rows, cols, 50, FP32, FP32, FP32, P, 2 ** 63, None), word="4-bit")
+    assert n.value == 5
+    assert lib.mlda_mx_linear_workspace_bytes(2 ** 54 // cols, cols, ctypes.addressof(n)) == 0 and n.value >= 2 ** 53
+
+
 def test_product_refusals(lib):
     n = ctypes.c_size_t()
     assert lib.mlda_mx_linear_workspace_bytes(3, 40, ctypes.addressof(n)) == 0 and n.value == 0
