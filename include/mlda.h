@@ -396,8 +396,8 @@ int mlda_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
  *   kl              finite
  *   sums            3 entries: the loss, the sum of w (exp(f - l) - (f - l) - 1), and the sum of w of the words that are clipped
  *   grad_logprobs   n_tokens entries; may be logprobs
- * Exponentials are within 3 units of fp32's roundoff (2^-24), exp(f - l) - (f - l) - 1 within 12, all else is fp64 and rounded once.  The workspace is
- * 8-byte aligned.
+ * All of it is fp64 and rounded once; exponentials have fp64's range and are within 2^-40 of themselves, exp(f - l) - (f - l) - 1 is within 2^-36.  The
+ * workspace is 8-byte aligned.
  */
 int mlda_policy_loss_workspace_bytes(int64_t n_tokens, size_t* bytes);
 int mlda_policy_loss(const float* logprobs, const float* old_logprobs, const float* reference, const float* advantages, const float* weights,

@@ -6,11 +6,11 @@
 //   grad = w (kl (1 - exp(f - l)) - A (0 where clipped, else exp(d)))
 // A word of weight 0 is none: nothing of it counts, whatever its numbers are.
 //
-// Differences, products and sums are in fp64: the border is then the same for every way of computing it, and sums of millions of words keep their bits.
-// The exponentials are fp32's, corrected for what the difference has beyond fp32: within 3 units of roundoff (2^-24); the KL term, a difference of nearly equal
-// numbers, is a series near 0: within 12.  (In fp64 they bound the kernel: 26,154 documents of 113 words with a KL term 28.5 us, so 26.)  Bound by memory: 50e6
-// words, 20 bytes each, 197 us (one word to a thread at a time 277).  Few words are one workgroup's and one launch; more leave partial sums, which a second launch
-// joins in a fixed order.
+// All of it is in fp64 and rounded once: the border is then the same for every way of computing it, sums of millions of words keep their bits, and a ratio that fp32
+// cannot hold does no harm under a weight that makes it small again.  Exponentials are a series, within 2^-40 of themselves, and the KL term, a difference of nearly
+// equal numbers, within 2^-36.  (With fp32's exponentials, which end at exp(88.7), it takes as long: 26,154 documents of 113 words with a KL term 26.7 us, so 26.1; 50e6 words 190 and 190,
+// with a KL term 242 and 231.)  Bound by memory: 50e6 words, 20 bytes each, 5.3 TB/s (one word to a thread at a time 277 us).  Few words are one workgroup's and one launch; more
+// leave partial sums, which a second launch joins in a fixed order.
 #pragma once
 #include "vec_io.hpp"
 
@@ -52,25 +52,31 @@ __device__ __forceinline__ void rows_of_wave(const int64_t* row_ptr, int64_t row
     hi = max(a0, b0);
 }
 
-// exp(d), for a d of more bits than fp32 has.
-__device__ __forceinline__ float exp_of(double d) {
-    const float high = (float)d, e = expf(high);
-    // (an infinite difference has no remainder, and an infinite exponential nothing to correct)
-    return e < INFINITY && high > -200.0f ? __builtin_fmaf(e, (float)(d - (double)high), e) : e;
-}
-
-// exp(x) - x - 1 up to 1, where the difference would lose bits: ten terms of x^2 / 2 + x^3 / 6 + ..; what is left out is below 2^-27 of it.
-__device__ __forceinline__ float kl_near(float x) {
-    float s = __builtin_fmaf(x, 1.0f / 39916800.0f, 1.0f / 3628800.0f);
-    s = __builtin_fmaf(x, s, 1.0f / 362880.0f);
-    s = __builtin_fmaf(x, s, 1.0f / 40320.0f);
-    s = __builtin_fmaf(x, s, 1.0f / 5040.0f);
-    s = __builtin_fmaf(x, s, 1.0f / 720.0f);
-    s = __builtin_fmaf(x, s, 1.0f / 120.0f);
-    s = __builtin_fmaf(x, s, 1.0f / 24.0f);
-    s = __builtin_fmaf(x, s, 1.0f / 6.0f);
-    s = __builtin_fmaf(x, s, 0.5f);
-    return x * x * s;
+// exp(x) of any x in fp64 as 2^k (1 + r + far), k whole and |r| <= ln 2 / 2.  The series of exp(r) ends with r^10 / 10!: what is left out is below 2^-42 of exp(r), and so is what
+// the terms from r^6 on lose in fp32; of `far`, exp(r) - 1 - r, both are below 2^-37.  Up to ln 2 / 2 k is 0, and `far` there exp(x) - 1 - x, whose difference would lose bits.
+struct Exp {
+    double value, far, most;                               // most: x, or about 720 where x is more: exp(x) is infinite there
+    bool near;
+};
+__device__ __forceinline__ Exp exp_of(double x) {
+    // Limits, 720 and -800 (exp(x) is 0 there), by the upper words, whose order is that of numbers of one sign (comparisons of fp64 numbers: 50e6 words 283 us with rows, so 277).
+    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+    const uint32_t most = (uint32_t)min((int32_t)(bits >> 32), 0x40868000), within = x == x ? min(most, 0xc0890000u) : 0x7ff80000u;
+    const double c = __builtin_bit_cast(double, (uint64_t)within << 32 | (uint32_t)bits);
+    // 1.5 x 2^52 more, and a number is whole, with itself in the lower bits
+    const double whole = __builtin_fma(c, 1.4426950408889634, 6755399441055744.0), k = whole - 6755399441055744.0, r = __builtin_fma(-k, 0.6931471805599453, c);
+    const float q = (float)r;
+    float h = __builtin_fmaf(q, 1.0f / 3628800.0f, 1.0f / 362880.0f);
+    h = __builtin_fmaf(q, h, 1.0f / 40320.0f);
+    h = __builtin_fmaf(q, h, 1.0f / 5040.0f);
+    h = __builtin_fmaf(q, h, 1.0f / 720.0f);
+    double s = __builtin_fma(r, (double)h, 1.0 / 120.0);
+    s = __builtin_fma(r, s, 1.0 / 24.0);
+    s = __builtin_fma(r, s, 1.0 / 6.0);
+    s = __builtin_fma(r, s, 0.5);
+    const double e = __builtin_fma(r, __builtin_fma(r, s, 1.0), 1.0);
+    return {__builtin_amdgcn_ldexp(e, (int)(uint32_t)__builtin_bit_cast(uint64_t, whole)), r * r * s,
+            __builtin_bit_cast(double, (uint64_t)most << 32 | (uint32_t)bits), k == 0.0};
 }
 
 // kPolicyEach: neighbouring words of a thread.  A word is a long chain of instructions: those of a single workgroup have a thread each if they can (330 of them, in fp64
@@ -142,17 +148,18 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
             const bool counts = used[e] && w != 0.0;
             const double d = (double)l[e] - (double)old[e], advantage = adv[e];
             const bool over = advantage > 0.0 && d > a.high, under = advantage < 0.0 && d < a.low;
-            const double ratio = exp_of(d);
+            const double ratio = exp_of(d).value;
             double term = -(over ? a.at_high : under ? a.at_low : ratio) * advantage;
             double grad = over || under ? 0.0 : -ratio * advantage;
             clipped += counts && (over || under) ? w : 0.0;
             if (kReference) {
-                const double x = (double)ref[e] - (double)l[e], near = kl_near((float)x), much = (double)exp_of(x) - 1.0;
-                const bool is_near = fabs(x) < 1.0;
-                const double part = is_near ? near : much < INFINITY ? much - x : much;     // (infinity also where both are)
+                const double x = (double)ref[e] - (double)l[e];
+                const Exp f = exp_of(x);
+                const double more = f.near ? x + f.far : f.value - 1.0;    // exp(x) - 1
+                const double part = f.near ? f.far : more - f.most;
                 kl += counts ? w * part : 0.0;
                 term += a.kl * part;
-                grad -= a.kl * (is_near ? x + near : much);
+                grad -= a.kl * more;
             }
             loss += counts ? w * term : 0.0;
             grad = counts ? w * grad : 0.0;

@@ -15,6 +15,7 @@ ROUND = {torch.float32: U, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 TINY = {torch.float32: 2.0 ** -149, torch.bfloat16: 2.0 ** -133, torch.float16: 2.0 ** -24}
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
 INF, NAN = math.inf, math.nan
+FINE = 2.0 ** -36                                                           # what exponentials and KL terms are off before they are rounded, of themselves
 
 
 @pytest.fixture(scope="module")
@@ -338,6 +339,44 @@ def test_far_words(ops):
     assert float(got.kl) == INF and (got.grad_logprobs[~inside] == -INF).all()
     assert ((got.grad_logprobs.double() - (1 - want)).abs() <= 4 * U * want + U + 2.0 ** -149)[inside].all()
 
+
+def test_exponentials_beyond_32_bits(ops):
+    """Ratios and KL terms that fp32 cannot hold, or holds with few bits, under weights that bring them back into its range."""
+    d = torch.tensor([89.0, 100.0, 150.0, 87.5, -88.0, -95.0, -103.0, -104.5, -150.0, 5e-21, -3e-25], device="cuda")
+    w = torch.tensor([1e-5, 1e-20, 1e-37, 1e-39, 1e6, 1e20, 1e30, 1e30, 1e38, 1e20, 1e25], device="cuda")
+    zero, one = torch.zeros_like(d), torch.ones_like(d)
+    x, w64 = d.double(), w.double()
+
+    def near(y, want):                                                      # (what fp32 cannot hold is infinite)
+        off = (U + FINE) * abs(want) + 2.0 ** -149
+        return abs(float(y) - want) <= off if abs(want) + off < 2.0 ** 128 else float(y) == math.copysign(INF, want)
+
+    for k in range(len(d)):                                                 # each word's sums by themselves
+        a = slice(k, k + 1)
+        got = ops.policy_loss(d[a], zero[a], -one[a], w[a], low=1.0)        # loss = gradient = w exp(d)
+        want = float(w64[k] * torch.exp(x[k]))
+        assert near(got.loss, want) and near(got.grad_logprobs[0], want)
+        got = ops.policy_loss(zero[a], zero[a], zero[a], w[a], d[a], kl=1.0)
+        term = float(w64[k] * (x[k] ** 2 / 2 if abs(x[k]) < 1e-9 else torch.exp(x[k]) - x[k] - 1))
+        assert near(got.loss, term) and near(got.kl, term) and near(got.grad_logprobs[0], -float(w64[k] * torch.expm1(x[k])))
+
+
+@pytest.mark.parametrize("n", [1000, 4000, 300000])
+def test_each_result_is_rounded_once(ops, n):
+    g = gen(n)
+    old, a, w = -5 * torch.rand(n, generator=g, device="cuda"), randn(g, n), torch.rand(n, generator=g, device="cuda")
+    apart = torch.exp(8 * torch.rand(n, generator=g, device="cuda") - 6)    # 0.0025 .. 7.4
+    l, f = old + apart * randn(g, n), old + apart * randn(g, n)
+    got = ops.policy_loss(l, old, a, w, f, low=1.0, high=INF, kl=0.3)
+    d, x, a, w = l.double() - old.double(), f.double() - l.double(), a.double(), w.double()
+    ratio, less = torch.exp(d), torch.expm1(x)
+    grad, parts = w * (-0.3 * less - a * ratio), w * (0.3 * less.abs() + (a * ratio).abs())
+    assert ((got.grad_logprobs.double() - grad).abs() <= U * grad.abs() + FINE * parts + 2.0 ** -149).all()
+    # by the series where the difference would lose bits: its next term is below 2^-50 of the whole
+    term = torch.where(x.abs() < 0.5, sum(x ** k / math.factorial(k) for k in range(2, 15)), less - x)
+    assert abs(float(got.kl) - float((w * term).sum())) <= (U + FINE) * float((w * term).sum())
+    parts = (w * (0.3 * term + (a * ratio).abs())).sum()
+    assert abs(float(got.loss) - float((w * (0.3 * term - a * ratio)).sum())) <= U * abs(float(got.loss)) + FINE * float(parts)
 
 def test_policy_gradient_is_that_of_differences(ops):
     g = gen(9)
