@@ -392,6 +392,7 @@ int mlda_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
  *   row_ptr         rows + 1 entries as in mlda_token_logprobs; advantages has an entry for each row.  Null: one for each word, rows = n_tokens.
  *   weights         n_tokens entries; null: 1 / n_tokens each.  A word of weight 0 is none: its numbers are of no matter, its gradient is 0.  So are
  *                   words before row_ptr[0] and from row_ptr[rows] on.
+ *   advantages      where it is 0 a word has no policy part, also where exp(d) is infinite (NaN stays NaN)
  *   low, high       0 <= low <= 1, high >= 0 (1 and infinity: never clipped)
  *   kl              finite
  *   sums            3 entries: the loss, the sum of w (exp(f - l) - (f - l) - 1), and the sum of w of the words that are clipped

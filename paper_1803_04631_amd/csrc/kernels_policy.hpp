@@ -4,7 +4,7 @@
 //   the word is clipped where A > 0 and d > ln(1 + high), or A < 0 and d < ln(1 - low)
 //   loss = sum of w (kl (exp(f - l) - (f - l) - 1) - A (its bound, 1 + high or 1 - low, where clipped, else exp(d)))
 //   grad = w (kl (1 - exp(f - l)) - A (0 where clipped, else exp(d)))
-// A word of weight 0 is none: nothing of it counts, whatever its numbers are.
+// A word of weight 0 is none: nothing of it counts, whatever its numbers are.  One whose advantage is 0 has no policy part, however large its ratio is.
 //
 // All of it is in fp64 and rounded once: the border is then the same for every way of computing it, sums of millions of words keep their bits, and a ratio that fp32
 // cannot hold does no harm under a weight that makes it small again.  Exponentials are a series, within 2^-40 of themselves, and the KL term, a difference of nearly
@@ -149,8 +149,10 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
             const double d = (double)l[e] - (double)old[e], advantage = adv[e];
             const bool over = advantage > 0.0 && d > a.high, under = advantage < 0.0 && d < a.low;
             const double ratio = exp_of(d).value;
-            double term = -(over ? a.at_high : under ? a.at_low : ratio) * advantage;
-            double grad = over || under ? 0.0 : -ratio * advantage;
+            // (an advantage of 0 makes 0 of an infinite ratio too, not NaN: the word tells nothing)
+            const double gain = advantage == 0.0 && ratio == INFINITY ? 0.0 : ratio * advantage;
+            double term = over ? -a.at_high * advantage : under ? -a.at_low * advantage : -gain;
+            double grad = over || under ? 0.0 : -gain;
             clipped += counts && (over || under) ? w : 0.0;
             if (kReference) {
                 const double x = (double)ref[e] - (double)l[e];

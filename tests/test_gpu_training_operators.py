@@ -378,6 +378,23 @@ def test_each_result_is_rounded_once(ops, n):
     parts = (w * (0.3 * term + (a * ratio).abs())).sum()
     assert abs(float(got.loss) - float((w * (0.3 * term - a * ratio)).sum())) <= U * abs(float(got.loss)) + FINE * float(parts)
 
+@pytest.mark.parametrize("n", [12, 3000, 70000])
+def test_a_word_without_advantage_has_no_ratio(ops, n):
+    """An advantage of 0 makes the policy's part of a word 0 however far it is from where it was drawn; NaN stays NaN."""
+    g = gen(n)
+    l, old, f, a = randn(g, n), randn(g, n), randn(g, n), randn(g, n)
+    a[::4] = 0
+    want = ops.policy_loss(l, old, a, None, f, kl=0.1)
+    far = old.clone()
+    far[0], far[4], far[8] = -100, -1000, -INF
+    got = ops.policy_loss(l, far, a, None, f, kl=0.1)
+    assert torch.isfinite(want.loss) and all(torch.equal(x, y) for x, y in zip(got, want))
+    got = ops.policy_loss(l, far, a)
+    assert torch.isfinite(got.loss) and not got.grad_logprobs[::4].any()
+    l[4] = NAN
+    got = ops.policy_loss(l, far, a, None, f, kl=0.1)
+    assert torch.isnan(got.loss) and torch.isnan(got.grad_logprobs).sum() == 1
+
 def test_policy_gradient_is_that_of_differences(ops):
     g = gen(9)
     n = 40
