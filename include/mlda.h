@@ -394,7 +394,7 @@ int mlda_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
  *                   words before row_ptr[0] and from row_ptr[rows] on.
  *   advantages      where it is 0 a word has no policy part, also where exp(d) is infinite (NaN stays NaN)
  *   low, high       0 <= low <= 1, high >= 0 (1 and infinity: never clipped)
- *   kl              finite
+ *   kl              finite; with 0 the KL term is given in sums, and no part of loss and gradient whatever it is
  *   sums            3 entries: the loss, the sum of w (exp(f - l) - (f - l) - 1), and the sum of w of the words that are clipped
  *   grad_logprobs   n_tokens entries; may be logprobs
  * All of it is fp64 and rounded once; exponentials have fp64's range and are within 2^-40 of themselves, exp(f - l) - (f - l) - 1 is within 2^-36.  The

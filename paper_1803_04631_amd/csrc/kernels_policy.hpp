@@ -160,8 +160,10 @@ __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
                 const double more = f.near ? x + f.far : f.value - 1.0;    // exp(x) - 1
                 const double part = f.near ? f.far : more - f.most;
                 kl += counts ? w * part : 0.0;
-                term += a.kl * part;
-                grad -= a.kl * more;
+                if (a.kl != 0.0) {                                         // (only watched, it is no part of them, infinite or NaN)
+                    term += a.kl * part;
+                    grad -= a.kl * more;
+                }
             }
             loss += counts ? w * term : 0.0;
             grad = counts ? w * grad : 0.0;

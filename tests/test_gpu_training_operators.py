@@ -395,6 +395,21 @@ def test_a_word_without_advantage_has_no_ratio(ops, n):
     got = ops.policy_loss(l, far, a, None, f, kl=0.1)
     assert torch.isnan(got.loss) and torch.isnan(got.grad_logprobs).sum() == 1
 
+@pytest.mark.parametrize("n", [12, 3000, 70000])
+def test_a_reference_that_is_only_watched(ops, n):
+    """With a weight of 0 the KL term is given, and no part of the loss or the gradient whatever it is."""
+    g = gen(n)
+    l, old, f, a = randn(g, n), randn(g, n), randn(g, n), randn(g, n)
+    l[7] = -INF                                                             # a word that is not allowed: its ratio is 0
+    want = ops.policy_loss(l, old, a)
+    got = ops.policy_loss(l, old, a, reference=torch.where(torch.isinf(l), -INF, l))
+    assert torch.isnan(got.kl) and all(torch.equal(x, y) for x, y in zip((got.loss, got.clipped, got.grad_logprobs), (want.loss, want.clipped, want.grad_logprobs)))
+    for k, away in ((1, 100.0), (2, 1000.0), (3, INF), (5, -INF), (6, NAN)):
+        f[k] = l[k] + away
+        got = ops.policy_loss(l, old, a, reference=f)
+        assert torch.isfinite(got.loss) and torch.equal(got.loss, want.loss) and torch.equal(got.grad_logprobs, want.grad_logprobs)
+        assert torch.isnan(got.kl) if k == 6 else float(got.kl) == INF     # (l[7]'s alone is infinite)
+
 def test_policy_gradient_is_that_of_differences(ops):
     g = gen(9)
     n = 40
