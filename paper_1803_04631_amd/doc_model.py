@@ -179,11 +179,24 @@ def suggest_words(model: DocModel, x, documents: Documents, rounds: int, draws: 
     return said
 
 
-def train(doc_ptr, word_ids, V: int, K: int, iters: int, epochs: int, batch: int = 1024, rate: float = 1.0, max_norm: float = 1.0,
-          share: float = 0.2, seed: int = 4631, out=None, dropout: float = 0.0):
+class Trained(NamedTuple):
+    model: DocModel
+    features: torch.Tensor         # of all documents
+    seen: Documents                # the tokens that topics were sampled of, and that the model was trained on
+    held: Documents                # the others
+    epochs: list                   # rows of epoch, trained, held out, gradient's norm
+
+
+def train(*args, **how):
+    """train_documents, of which it returns the model, the features, the held-out documents and the epochs' rows."""
+    t = train_documents(*args, **how)
+    return t.model, t.features, t.held, t.epochs
+
+
+def train_documents(doc_ptr, word_ids, V: int, K: int, iters: int, epochs: int, batch: int = 1024, rate: float = 1.0, max_norm: float = 1.0,
+                    share: float = 0.2, seed: int = 4631, out=None, dropout: float = 0.0) -> Trained:
     """Samples topics of the documents' tokens but a held-out share (alpha = 50/K, beta = 0.01), trains the model on those tokens, and
-    prints after each epoch (to `out`, or standard output) the mean log-probability of the tokens it was trained on and of those held out.  Returns (the
-    model, the features, the held-out documents, rows of epoch, trained, held out, gradient's norm)."""
+    prints after each epoch (to `out`, or standard output) the mean log-probability of the tokens it was trained on and of those held out."""
     from . import Mlda
     (ptr, words), (held_ptr, held_words) = hold_out(doc_ptr, word_ids, share, seed)
     alpha = 50.0 / K
@@ -208,7 +221,7 @@ def train(doc_ptr, word_ids, V: int, K: int, iters: int, epochs: int, batch: int
         logprob, norm = torch.stack([torch.stack(s) for s in steps]).mean(0).tolist()
         rows.append((epoch, logprob, held_out(), norm))
         print("%d %.4f %.4f %.3g" % rows[-1], file=out, flush=True)
-    return model, x, held, rows
+    return Trained(model, x, seen, held, rows)
 
 
 def main(argv=None):
@@ -227,20 +240,20 @@ def main(argv=None):
     ap.add_argument("--seed", type=int, default=4631)
     args = ap.parse_args(argv)
     doc_ptr, word_ids, V = load_docword(args.docword)
-    model, x, held, _ = train(doc_ptr, word_ids, V, args.topics, args.iters, args.epochs, batch=args.batch, rate=args.rate, seed=args.seed, dropout=args.dropout)
-    bounds = held.row_ptr.tolist()
+    model, x, seen, held, _ = train_documents(doc_ptr, word_ids, V, args.topics, args.iters, args.epochs, batch=args.batch, rate=args.rate, seed=args.seed,
+                                              dropout=args.dropout)
     if args.suggest and len(x):
-        n = min(args.batch, len(x))
-        suggest_words(model, x[:n], held.batch(0, n, bounds), args.suggest, seed=args.seed)
+        n = min(args.batch, len(x))                    # (what is held out stays so: no word of it is rewarded)
+        suggest_words(model, x[:n], seen.batch(0, n, seen.row_ptr[:n + 1].tolist()), args.suggest, seed=args.seed)
     if args.packed and len(x):
-        small = model.packed()
+        small, bounds = model.packed(), held.row_ptr.tolist()
         both = [sum(float(m.score(x[a:a + args.batch], held.batch(a, min(a + args.batch, len(x)), bounds)).logprobs.double().sum())
                     for a in range(0, len(x), args.batch)) / max(len(held.tokens), 1) for m in (model, small)]
         print("held_out in 32 bits %.4f, in 4 bits %.4f" % tuple(both))
         model = small
     n = min(args.show, len(x))
     if n:
-        top = model.score(x[:n], held.batch(0, n, bounds), alternatives=min(10, V))
+        top = model.score(x[:n], held.batch(0, n, held.row_ptr[:n + 1].tolist()), alternatives=min(10, V))
         for d in range(n):
             print("document %d: entropy %.2f, likeliest words %s" % (d + 1, top.entropy[d], (top.top_ids[d] + 1).tolist()))
 

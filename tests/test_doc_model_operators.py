@@ -137,3 +137,31 @@ def test_training_with_dropout_suggestions_and_packed_weights(tmp_path, capsys):
     a = doc_model.train(c.doc_ptr, c.word_ids, 90, 4, iters=5, epochs=2, batch=30, dropout=0.2)
     b = doc_model.train(c.doc_ptr, c.word_ids, 90, 4, iters=5, epochs=2, batch=30, dropout=0.2)
     assert abs(a[3][-1][2] - b[3][-1][2]) <= 1e-4 and a[0].steps == b[0].steps == 6        # the same masks in both runs
+
+
+def test_what_is_held_out_is_not_rewarded(tmp_path, capsys, monkeypatch):
+    """The command rewards words of the tokens that it sampled, and its last figures are of tokens that no step has seen."""
+    import corpus_synth
+    from paper_1803_04631_amd import bow, doc_model
+    c = corpus_synth.tiny(D=80, V=90, K=4, mean_len=40, seed=2)
+    path = tmp_path / "docword.small.txt"
+    bow.save_docword(path, c.doc_ptr, c.word_ids, 90)
+    doc_ptr, word_ids, _ = bow.load_docword(str(path))
+    (ptr, words), (held_ptr, held_words) = doc_model.hold_out(doc_ptr, word_ids, 0.2, 4631)
+    given, suggest = [], doc_model.suggest_words
+
+    def watched(model, x, documents, *args, **how):
+        given.append((model, x, documents))
+        return suggest(model, x, documents, *args, **how)
+
+    monkeypatch.setattr(doc_model, "suggest_words", watched)
+    doc_model.main([str(path), "--topics", "4", "--iters", "5", "--epochs", "1", "--batch", "30", "--suggest", "2", "--packed"])
+    model, x, documents = given[0]
+    assert len(given) == 1 and len(x) == 30
+    assert np.array_equal(documents.row_ptr.cpu().numpy(), ptr[:31]) and np.array_equal(documents.tokens.cpu().numpy(), words[:ptr[30]])
+    trained = doc_model.train_documents(doc_ptr, word_ids, 90, 4, iters=5, epochs=1, batch=30)
+    assert np.array_equal(trained.held.tokens.cpu().numpy(), held_words) and np.array_equal(trained.held.row_ptr.cpu().numpy(), held_ptr)
+    assert np.array_equal(trained.seen.tokens.cpu().numpy(), words) and torch.equal(trained.features[:30], x)
+    held = model.score(trained.features, trained.held).logprobs.double().mean()
+    said = capsys.readouterr().out.split("held_out in 32 bits ")[1].split(",")[0]
+    assert abs(float(said) - float(held)) <= 1e-4                          # four places; scores in other batches
