@@ -396,7 +396,7 @@ int mlda_dropout(const void* x, int64_t x_stride, const void* residual, int64_t 
  *   low, high       0 <= low <= 1, high >= 0 (1 and infinity: never clipped)
  *   kl              finite; with 0 the KL term is given in sums, and no part of loss and gradient whatever it is
  *   sums            3 entries: the loss, the sum of w (exp(f - l) - (f - l) - 1), and the sum of w of the words that are clipped
- *   grad_logprobs   n_tokens entries; may be logprobs
+ *   grad_logprobs   n_tokens entries; may be logprobs, or another array of a number for each word, but not in the place of rows' advantages
  * All of it is fp64 and rounded once; exponentials have fp64's range and are within 2^-40 of themselves, exp(f - l) - (f - l) - 1 is within 2^-36.  The
  * workspace is 8-byte aligned.
  */

@@ -20,6 +20,11 @@ PolicyForm policy_form(int64_t n) {
 }
 constexpr size_t kPolicyBytes = (size_t)mlda::kPolicyGroups * 3 * 8;
 
+bool overlap(const void* p, int64_t p_bytes, const void* q, int64_t q_bytes) {
+    const char *const a = static_cast<const char*>(p), *const b = static_cast<const char*>(q);
+    return p_bytes > 0 && q_bytes > 0 && a < b + q_bytes && b < a + p_bytes;
+}
+
 int check_tokens(int64_t n) {
     return n < 0 || n >= ((int64_t)1 << 31) ? refuse("policy loss: need 0 <= n_tokens < 2^31") : MLDA_OK;
 }
@@ -93,6 +98,9 @@ int mlda_policy_loss(const float* logprobs, const float* old_logprobs, const flo
         if (workspace_bytes < kPolicyBytes)
             return set_error(MLDA_ENOMEM, "policy loss: the workspace is smaller than mlda_policy_loss_workspace_bytes");
     }
+    // (a row's advantage is read for other words' gradients too, and its bounds)
+    if (row_ptr && (overlap(grad_logprobs, n_tokens * 4, advantages, rows * 4) || overlap(grad_logprobs, n_tokens * 4, row_ptr, (rows + 1) * 8)))
+        return refuse("policy loss: grad_logprobs cannot be in the place of rows' advantages or of row_ptr");
     const mlda::PolicyArgs a{logprobs, old_logprobs, reference, advantages, weights, row_ptr, rows, n_tokens, log1p(-low), log1p(high),
                              1.0 - low, 1.0 + high, kl, n_tokens ? 1.0 / (double)n_tokens : 0.0, grad_logprobs,
                              groups > 1 ? nullptr : sums, static_cast<double*>(dev_workspace),

@@ -142,5 +142,5 @@ def policy_loss(logprobs, old_logprobs, advantages, weights=None, reference=None
     the words of weights (1 / n_tokens each without) times -min(ratio A, clip(ratio, 1 - low, 1 + high) A), ratio = exp(logprobs -
     old_logprobs), plus kl times exp(d) - d - 1 with d = reference - logprobs (with kl = 0 a reference is only watched); and its gradient for token_logprobs_backward.  The
     advantages A are the words' own, or with row_ptr (as token_logprobs takes it) those of their rows.  A word of weight 0 and one of no row
-    count for nothing, whatever their numbers are.  `out` (logprobs, for instance) takes the gradient."""
+    count for nothing, whatever their numbers are.  `out` (logprobs, for instance, but not rows' advantages) takes the gradient."""
     return PolicyLoss(*_tensors.policy_loss(logprobs, old_logprobs, advantages, weights, reference, row_ptr, low, high, kl, out))

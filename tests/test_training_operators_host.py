@@ -106,6 +106,16 @@ def test_policy_refusals(lib):
     refused(lib, lib.mlda_policy_loss_workspace_bytes(5, None), word="null")
 
 
+@pytest.mark.parametrize("total", [40, 2 ** 20])
+def test_the_gradient_is_not_written_over_what_other_words_read(lib, total):
+    n = ctypes.c_size_t()
+    assert lib.mlda_policy_loss_workspace_bytes(total, ctypes.addressof(n)) == 0
+    rows, far = 10, 2 ** 30
+    l, advantages, row_ptr = 3 * far, far, 2 * far
+    for grad in (advantages, advantages + 4 * rows - 4, advantages - 4 * total + 4, row_ptr, row_ptr + 8 * rows + 4, row_ptr - 4 * total + 4):
+        refused(lib, lib.mlda_policy_loss(l, l, None, advantages, None, row_ptr, rows, total, 0.2, 0.2, 0.0, P, grad, P if n.value else None, n.value, None), word="advantages")
+
+
 def test_the_binding_wants_tensors_on_a_gpu():
     x, v = torch.zeros(2, 40), torch.zeros(2)
     q = operators.Mx4(torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.uint8), 40)
