@@ -156,6 +156,8 @@ def suggest_words(model: DocModel, x, documents: Documents, rounds: int, draws: 
     where the document holds it, else 0, and its advantage is that less the mean; then `steps` steps on the policy loss of those
     words, with a KL term to the model as it was at first.  Prints (to `out`, or standard output) and returns rows of round, share of the drawn words that documents hold,
     KL term and clipped share of the last step."""
+    if rounds < 0 or draws < 1 or steps < 1:
+        raise ValueError("suggest_words: need rounds >= 0, and at least one draw and one step to each")
     rows, vocab = len(x), model.weight.shape[0]
     holds = torch.zeros(rows, vocab, dtype=torch.bool, device=x.device)
     lengths = documents.row_ptr.diff()

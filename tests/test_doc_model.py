@@ -20,6 +20,13 @@ def test_hold_out_parts_the_tokens_of_each_document():
     assert np.array_equal(ptr, doc_ptr) and len(held) == 0 and not held_ptr.any()
 
 
+@pytest.mark.parametrize("how", [{"rounds": -1}, {"rounds": 1, "draws": 0}, {"rounds": 1, "steps": 0}, {"rounds": 2, "steps": -1}])
+def test_suggesting_without_steps_is_refused(how):
+    from paper_1803_04631_amd.doc_model import suggest_words
+    with pytest.raises(ValueError, match="suggest_words"):
+        suggest_words(None, None, None, **how)
+
+
 @pytest.mark.gpu
 def test_gradients_are_those_of_the_mean_log_probability():
     import torch
