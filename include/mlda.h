@@ -342,7 +342,8 @@ int mlda_clip_grads(const void* const* tensors, void* const* out, const int64_t*
  *   codes    rows x blocks x 16 bytes, 16-byte aligned: column 2j of a row is the lower half of its byte j, 2j + 1 the upper; columns behind
  *            the last have the code 0 (mlda_mx_linear relies on that)
  *   scales   rows x blocks bytes: s + 127; 255: the block holds NaN or infinity, and stands for NaN as a whole
- * mlda_mx_dequantize writes x, what codes and scales stand for, rounded to its type (fp32 and bf16 hold all of it).
+ * mlda_mx_dequantize writes x, what codes and scales stand for, rounded to its type: fp32 and bf16 hold all of it but 2^128 and more, which is infinity.  A
+ * finite x of magnitude 1.75 2^127 or more is such a number: it is held as 2^128 (and multiplied as that by mlda_mx_linear).
  */
 int mlda_mx_quantize(const void* x, int64_t x_stride, uint8_t* codes, uint8_t* scales, int64_t rows, int32_t cols, int32_t type,
                       void* hip_stream);

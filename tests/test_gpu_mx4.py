@@ -119,6 +119,33 @@ def test_every_code_under_every_scale(ops):
         assert same(ops.mx4_dequantize(ops.Mx4(codes, scales, 512), dtype), want.to(dtype))
 
 
+def test_the_greatest_numbers(ops):
+    """From 1.75 x 2^127 on a number is held as 2^128: infinity once it is fp32 or bf16 again, and 2^128 in a product."""
+    most = torch.finfo(torch.float32).max
+    border = 1.75 * 2.0 ** 127
+    below = float(torch.nextafter(torch.tensor(border), torch.tensor(0.0)))
+    x = torch.zeros(6, 32, device="cuda")
+    x[0, 3], x[1, 3], x[2, 3], x[3, 3], x[4, 3], x[5, 3] = below, border, 3.0e38, most, -most, 2.0 ** 127
+    q = ops.mx4_quantize(x)
+    check_held(ops, x)
+    held = torch.tensor([1.5 * 2.0 ** 127, INF, INF, INF, -INF, 2.0 ** 127], device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        assert torch.equal(ops.mx4_dequantize(q, dtype)[:, 3], held.to(dtype))
+    assert int(q.scales[3, 0]) == 253
+    w = torch.zeros(40, 32, device="cuda")
+    w[:, 3] = torch.tensor([2.0 ** -(k + 1) for k in range(40)], device="cuda")
+    weight = ops.mx4_quantize(w)
+    values = torch.tensor([1.5, 2.0, 2.0, 2.0, -2.0, 1.0], dtype=torch.float64, device="cuda") * 2.0 ** 127
+    want = (values[:, None] * w[:, 3].double()).float()
+    for rows in (1, 20, 200):                                               # each form of the product
+        got = ops.mx4_linear(x.repeat(rows, 1), weight)
+        assert torch.equal(got, want.repeat(rows, 1))
+    wide = torch.zeros(200, 600, device="cuda")
+    wide[:, 3] = most
+    weight = ops.mx4_quantize(torch.nn.functional.pad(w.repeat(10, 1), (0, 568)))
+    assert torch.equal(ops.mx4_linear(wide, weight), want[3].repeat(200, 10))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_strides_and_places(ops, dtype):
     g = gen(5)
