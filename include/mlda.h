@@ -340,7 +340,7 @@ int mlda_clip_grads(const void* const* tensors, void* const* out, const int64_t*
  * With a the greatest magnitude of a block its scale is the least 2^s, s >= -127, with a < 7 2^s, and x is held as x / 2^s rounded to nearest, ties
  * to even, among 0, 1/2, 1, 3/2, 2, 3, 4, 6 (the codes 0 .. 7; 8 more: negative).  What is held is within a fifth of x, or within 2^s / 4.
  *   codes    rows x blocks x 16 bytes, 16-byte aligned: column 2j of a row is the lower half of its byte j, 2j + 1 the upper; columns behind
- *            the last have the code 0 (mlda_mx_linear relies on that)
+ *            the last are written as the code 0, and whatever is there is of no matter to what reads them
  *   scales   rows x blocks bytes: s + 127; 255: the block holds NaN or infinity, and stands for NaN as a whole
  * mlda_mx_dequantize writes x, what codes and scales stand for, rounded to its type: fp32 and bf16 hold all of it but 2^128 and more, which is infinity.  A
  * finite x of magnitude 1.75 2^127 or more is such a number: it is held as 2^128 (and multiplied as that by mlda_mx_linear).

@@ -237,6 +237,24 @@ def test_short_rows_of_odd_numbers(ops, cols):
     assert torch.isnan(got[[38, 40]]).all() and torch.isnan(got[:, [7, 330]]).all() and not torch.isnan(got[1:38, 8:330]).any()
 
 
+FORMS = [(1, 1000, 300), (16, 65, 70), (300, 33, 70), (31, 300, 200), (20, 2000, 65), (1100, 300, 129), (700, 300, 2100), (1500, 1001, 22000)]
+
+
+@pytest.mark.parametrize("rows,cols,words", FORMS)
+def test_codes_behind_the_last_column_are_of_no_matter(ops, rows, cols, words):
+    g = gen(rows + cols)
+    x, weight = randn(g, rows, cols, dtype=torch.bfloat16), weights(ops, g, words, cols)
+    codes = torch.randint(256, weight.codes.shape, generator=g, device="cuda", dtype=torch.uint8)
+    whole, half = cols // 2, cols % 2
+    codes[:, :whole] = weight.codes[:, :whole]
+    if half:
+        codes[:, whole] = weight.codes[:, whole] & 15 | codes[:, whole] & 0xf0
+    other = ops.Mx4(codes, weight.scales, cols)
+    assert not torch.equal(codes, weight.codes)
+    assert torch.equal(ops.mx4_linear(x, other), ops.mx4_linear(x, weight))
+    assert torch.equal(ops.mx4_dequantize(other), ops.mx4_dequantize(weight))
+
+
 @pytest.mark.parametrize("rows", [1, 16, 65, 300])
 def test_linear_into_part_of_a_matrix(ops, rows):
     g = gen(rows)
