@@ -356,8 +356,8 @@ int mlda_mx_dequantize(const uint8_t* codes, const uint8_t* scales, void* x, int
  *   codes, scales   the matrix W of words rows (1 .. 2^30) and cols columns
  *   bias            words entries of bias_type (out_type, or MLDA_FP32); null: zeros
  *   y               rows x words of out_type; not in the place of x
- * Sums are fp32: within (cols / 64 + 8) 2^-24 of the sum of its terms' (and the bias') magnitudes before y is rounded.  A row or word with a block of NaN has
- * NaN.  The workspace (16-byte aligned) is for Q(x).
+ * Sums are fp32: within (cols / 64 + 8) 2^-24 of the sum of its terms' (and the bias') magnitudes, or of 2^-126 where that is less, before y is rounded.  A row or
+ * word with a block of NaN has NaN.  The workspace (16-byte aligned) is for Q(x).
  */
 int mlda_mx_linear_workspace_bytes(int64_t rows, int32_t cols, size_t* bytes);
 int mlda_mx_linear(const void* x, int64_t x_stride, const uint8_t* codes, const uint8_t* scales, const void* bias, void* y, int64_t y_stride,

@@ -255,6 +255,18 @@ def test_codes_behind_the_last_column_are_of_no_matter(ops, rows, cols, words):
     assert torch.equal(ops.mx4_dequantize(other), ops.mx4_dequantize(weight))
 
 
+@pytest.mark.parametrize("rows,cols,words", FORMS)
+def test_products_below_the_normal_numbers(ops, rows, cols, words):
+    """There a sum's rounding is a half of 2^-149, that of 2^-126 beside it."""
+    g = gen(rows)
+    for down in (60, 66, 70, 74):
+        x, w = randn(g, rows, cols) * 2.0 ** -down, randn(g, words, cols) * 2.0 ** -down
+        weight = ops.mx4_quantize(w)
+        q, w = held64(x)[2], ops.mx4_dequantize(weight).double()
+        bound = (cols / 64 + 8) * U * (q.abs() @ w.abs().t()).clamp(min=2.0 ** -126)
+        assert ((ops.mx4_linear(x, weight).double() - q @ w.t()).abs() <= bound + 2.0 ** -150).all()
+
+
 @pytest.mark.parametrize("rows", [1, 16, 65, 300])
 def test_linear_into_part_of_a_matrix(ops, rows):
     g = gen(rows)
