@@ -61,8 +61,9 @@ def features(row_ptr, topics, counts, n_topics: int, alpha: float, device="cuda:
 
 class DocModel:
     """The model's parameters, fp32.  The bias starts at the words' frequencies, so that the untrained
-    model knows those and nothing of the documents.  `dropout`: the share of the normed features that each step of training
-    leaves out, other ones at each step, drawn from `seed` and the step's number."""
+    model knows those and nothing of the documents.  `dropout`: the share of the normed features that each step()
+    leaves out, other ones at each step, drawn from `seed` and the step's number.  policy_step() leaves none out: its ratios are to
+    log-probabilities that words were drawn with, of all features."""
 
     def __init__(self, n_topics: int, word_counts, device="cuda:0", dropout: float = 0.0, seed: int = 0):
         counts = torch.as_tensor(word_counts, dtype=torch.float32, device=device)

@@ -71,6 +71,16 @@ def test_policy_gradients():
     same_gradients(grads, loss - 0.05 * entropy, params)
 
 
+def test_policy_steps_leave_no_features_out():
+    model, x, words, _, g = made(dropout=0.5, seed=4)
+    whole = made(seed=4)[0]
+    old, advantages = model.score(x, words).logprobs, torch.randn(len(words.tokens), generator=g, device="cuda")
+    a, b = (m.policy_gradients(x, words, old, advantages) for m in (model, whole))
+    assert torch.equal(a[0].grad_logprobs, b[0].grad_logprobs) and all(torch.equal(u, v) for u, v in zip(a[1], b[1]))
+    assert float(a[0].clipped) == 0.0                                      # every ratio is 1
+    assert not torch.equal(model.gradients(x, words)[1][0], whole.gradients(x, words)[1][0])
+
+
 def test_packed_scores_are_those_of_the_packed_weights():
     from paper_1803_04631_amd import operators
     model, x, words, row, _ = made(rows=100, K=70, V=1003, seed=5)
