@@ -81,6 +81,62 @@ def test_policy_steps_leave_no_features_out():
     assert not torch.equal(model.gradients(x, words)[1][0], whole.gradients(x, words)[1][0])
 
 
+@pytest.mark.parametrize("max_norm", [1e-3, 1e3])
+def test_a_policy_step_descends_its_gradient(max_norm):
+    model, x, words, _, g = made(seed=8)
+    n = len(words.tokens)
+    old = model.score(x, words).logprobs + 0.1 * torch.randn(n, generator=g, device="cuda")
+    advantages = torch.randn(n, generator=g, device="cuda")
+    want, grads = model.policy_gradients(x, words, old, advantages, entropy=0.01)
+    before = [p.clone() for p in (model.weight, model.bias, model.scale, model.shift)]
+    got = model.policy_step(x, words, old, advantages, 0.25, max_norm, entropy=0.01)
+    assert model.steps == 1 and all(torch.equal(u, v) for u, v in zip(got, want))
+    norm = math.sqrt(sum(float(v.double().square().sum()) for v in grads))
+    factor = min(1.0, max_norm / norm)
+    assert (factor < 1) == (max_norm < 1)
+    for p, was, grad in zip((model.weight, model.bias, model.scale, model.shift), before, grads):
+        step = 0.25 * factor * grad.double()
+        # a factor and a product in fp32, another product and a difference: 2^-24 of what is made, a few times
+        assert (p.double() - (was.double() - step)).abs().max() <= (2.0 ** -24 * (was.abs() + 8 * step.abs())).max()
+        assert float(step.abs().max()) > 0
+
+
+def test_suggested_words_and_what_they_are_worth():
+    """What each step is given: words of the right documents, an advantage of 1 where the document holds the word less the mean, log-probabilities of
+    the model that drew them and of the model as it was at first."""
+    from paper_1803_04631_amd.doc_model import suggest_words
+    said, given = [], []
+    for run in range(2):
+        model, x, words, row, _ = made(rows=25, seed=9)
+        first, step = logp64(model, x)[1].detach(), model.policy_step
+
+        def watched(x_, w, old, advantages, rate, max_norm, reference=None, kl=0.0):
+            given.append((w, old, advantages, reference, kl, logp64(model, x)[1].detach()))
+            return step(x_, w, old, advantages, rate, max_norm, reference=reference, kl=kl)
+
+        model.policy_step = watched
+        said.append(suggest_words(model, x, words, rounds=3, draws=7, steps=2, rate=0.5, kl=0.03, seed=5))
+    assert said[0] == said[1] and [r[0] for r in said[0]] == [1, 2, 3] and len(given) == 12
+    holds = set(zip(row.tolist(), words.tokens.tolist()))
+    for k, (w, old, advantages, reference, kl, logp) in enumerate(given[:6]):
+        assert torch.equal(w.row_ptr, 7 * torch.arange(26, device="cuda")) and kl == 0.03
+        document = torch.arange(25, device="cuda").repeat_interleave(7)
+        worth = torch.tensor([(d, t) in holds for d, t in zip(document.tolist(), w.tokens.tolist())], dtype=torch.float64, device="cuda")
+        assert (advantages.double() - (worth - worth.mean())).abs().max() <= 1e-6
+        assert abs(said[0][k // 2][1] - float(worth.mean())) <= 1e-6
+        at = document, w.tokens.long()
+        assert (reference.double() - first[at]).abs().max() <= 1e-4
+        if k % 2 == 0:                                                     # the model that drew them
+            assert (old.double() - logp[at]).abs().max() <= 1e-4
+        else:                                                              # the same words and log-probabilities, by a model that is a step further
+            assert torch.equal(w.tokens, given[k - 1][0].tokens) and torch.equal(old, given[k - 1][1]) and not torch.equal(logp, given[k - 1][5])
+    for _, held, kl, clipped in said[0]:
+        assert 0 <= held <= 1 and 0 <= clipped <= 1 and kl > 0
+    model, x, words, _, _ = made(rows=25, seed=9)
+    (_, _, kl, clipped), = suggest_words(model, x, words, rounds=1, draws=7, steps=1)
+    assert abs(kl) <= 1e-9 and clipped == 0                                # before the first step the model is as it was
+
+
 def test_packed_scores_are_those_of_the_packed_weights():
     from paper_1803_04631_amd import operators
     model, x, words, row, _ = made(rows=100, K=70, V=1003, seed=5)
