@@ -156,6 +156,23 @@ def test_packed_scores_are_those_of_the_packed_weights():
     assert torch.equal(packed.score(x, words).logprobs, got.logprobs)
 
 
+def test_logits_of_packed_weights_are_rounded_once_more():
+    """The scores of a packed model are those of its fp32 logits, each rounded to bf16."""
+    from paper_1803_04631_amd import operators
+    model, x, words, row, _ = made(rows=100, K=70, V=1003, seed=5)
+    fine, coarse = model.packed(torch.float32), model.packed()
+    assert fine.dtype == torch.float32 and coarse.dtype == torch.bfloat16 and torch.equal(fine.weight.codes, coarse.weight.codes)
+    y = operators.layer_norm(x, model.scale, model.shift)[0]
+    logits = operators.mx4_linear(y, fine.weight, fine.bias)
+    assert torch.equal(operators.mx4_linear(y, coarse.weight, coarse.bias, dtype=torch.bfloat16), logits.bfloat16())
+    at = row, words.tokens.long()
+    want = torch.log_softmax(logits.bfloat16().double(), 1)[at]
+    assert (coarse.score(x, words).logprobs.double() - want).abs().max() <= 2e-5
+    # a logit is off by 2^-8 of itself at the most, and so is the logarithm of the sum
+    off = 2.0 ** -8 * (logits[at].abs() + logits.abs().amax(1)[row])
+    assert ((coarse.score(x, words).logprobs - fine.score(x, words).logprobs).abs() <= off + 1e-4).all()
+
+
 def test_a_step_in_a_graph_draws_new_masks():
     """Forward, loss and backward of a step captured once: each replay has the mask of the step's number that it finds on the GPU."""
     from paper_1803_04631_amd import operators
