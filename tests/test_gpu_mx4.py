@@ -378,6 +378,41 @@ def test_on_another_stream_and_in_a_graph(ops):
         assert torch.equal(back, ops.mx4_dequantize(ops.mx4_quantize(fixed[1])))
 
 
+@pytest.mark.parametrize("rows,cols,words", [(31, 1000, 3000), (16, 3000, 200), (300, 700, 9001), (1100, 1000, 15003)])
+def test_each_form_in_two_graphs_and_on_two_streams(ops, rows, cols, words):
+    g = gen(rows)
+    weight, bias = weights(ops, g, words, cols), randn(g, words)
+    inputs = [randn(g, rows, cols) for _ in range(2)]
+    want = [ops.mx4_linear(x, weight, bias) for x in inputs]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    for stream in streams:
+        stream.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(3):                                                     # both at once
+        for k, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[k].append(ops.mx4_linear(inputs[k], weight, bias))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[k]) for k in range(2) for y in got[k])
+    graphs, out = [], []
+    fixed = [x.clone() for x in inputs]
+    for x in fixed:
+        graphs.append(torch.cuda.CUDAGraph())
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graphs[-1]):
+            out.append(ops.mx4_linear(x, weight, bias))
+    for k in range(3):
+        for x, y in zip(fixed, inputs):
+            x.copy_(y * (k + 1))
+        for graph, stream in zip(graphs, streams):
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(fixed, out):
+            assert torch.equal(ops.mx4_linear(x, weight, bias), y)
+
+
 def test_refusals(ops):
     g = gen(3)
     x, weight = randn(g, 4, 40), weights(ops, g, 20, 40)
