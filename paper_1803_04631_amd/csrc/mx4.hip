@@ -10,16 +10,20 @@ int64_t blocks_of(int32_t cols) { return ((int64_t)cols + mlda::kMxBlock - 1) / 
 constexpr int32_t kMostProductCols = 1 << 24;    // tiles of rows have 32-bit numbers of pieces
 
 // How a product's rows are held in 4 bits: few, and short ones of a small product, by each workgroup for itself, others in the workspace, in whole tiles of rows
-// and whole stretches of steps.  With a launch for the rows, and so, us: 1 x 1,000 x 141,000 fp32 27, 19; 1,000 x 32 x 5,000 fp32 12.6, 8.4; 65 x 128 x 64,000 bf16
+// and whole stretches of steps.  With a launch for the rows, and so, us.  Up to 16 rows and 512 blocks (rows x columns x words, bf16): 1 x 1,000 x 141,000 24.3, 17.9;
+// 8 x 1,000 x 40,009 10.8, 9.5; 16 x 500 x 40,009 8.6, 8.1; 16 x 1,000 x 3,000 8.5, 8.2, x 40,009 11.4, 12.0, x 141,000 27.9, 27.8; 1 x 16,384 x 3,000 16.0, 16.0.  But with
+// more blocks 16 x 1,537 x 40,009 16.1, 18.8; 16 x 2,048 x 40,009 15.6, 19.4; 4 x 8,192 x 3,000 11.4, 14.8; 1 x 32,768 x 2,000 24.7, 27.8; with more rows 17 x 500 x 3,000 7.5, 8.1;
+// 24 x 500 x 3,000 7.8, 9.4, x 40,009 9.3, 9.6; 32 x 500 x 40,009 10.1, 11.2.  Short rows: 24 x 256 x 40,009 7.6, 6.2; 1,000 x 32 x 5,000 fp32 12.6, 8.4; 65 x 128 x 64,000 bf16
 // 9.8, 9.3; 1,000 x 128 x 4,000 bf16 9.3, 8.2; 1,000 x 224 x 2,300 bf16 9.3, 8.3; 250 x 256 x 8,000 fp16 8.6, 7.1.  But 1,000 x 32 x 16,000 bf16 15.6, 19.3;
 // 2,000 x 128 x 4,000 bf16 11.4, 13.7; 2,000 x 200 x 4,000 bf16 12.1, 16.8; 300 x 500 x 3,000 bf16 9.4, 10.5.
-bool few_rows(int64_t rows, int32_t cols) { return rows <= 16 && rows * blocks_of(cols) <= 1024; }
+bool few_rows(int64_t rows, int32_t cols) { return rows <= 16 && rows * blocks_of(cols) <= 512; }
 bool short_rows(int64_t rows, int32_t cols, int32_t words) {
     return blocks_of(cols) <= 8 && rows <= ((int64_t)1 << 24) / std::max(blocks_of(cols), (int64_t)2) / words;
 }
 // Which products are few enough for a wave for each 32 x 32 of them; the others take tiles of 128 words and as many rows as a workgroup's waves have: 128, or
-// 256 where there are that many tiles and rows (1,000 columns, bf16, us: a wave for each, 128, 256).  300 x 3,000: 9.9, 10.1, -; 100 x 8,516: 10.0, 9.5, -; 300 x 5,000: 11.4, 10.5,
-// 11.0; 32 x 141,000: 28.6, 27.7, 39.9; 65 x 141,000: 55, 29, 41; 500 x 141,000: 246, 66, 70; 2,048 x 141,000: 958, 246, 232; 2,932 x 1,120 of 9,205 columns: 85, 62, 63.
+// 256 where there are that many tiles and rows.  1,000 columns, bf16, us, a wave for each, 128: 17 x 40,009 11.7, 14.0; 17 x 141,000 28.2, 34.2; 32 x 3,000 9.2, 9.2; 32 x 40,009 12.9, 13.7;
+// 32 x 141,000 31.4, 32.1 (32 x 3,000 of 500 columns 8.4, 8.2, of 4,096 9.8, 17.9).  A wave for each, 128, 256: 300 x 3,000: 9.9, 10.1, -; 100 x 8,516: 10.0, 9.5, -; 300 x 5,000: 11.4, 10.5,
+// 11.0; 65 x 141,000: 55, 29, 41; 500 x 141,000: 246, 66, 70; 2,048 x 141,000: 958, 246, 232; 2,932 x 1,120 of 9,205 columns: 85, 62, 63.
 bool few_products(int64_t rows, int32_t words) { return rows <= 32 || words < mlda::kTileWords || (rows + 31) / 32 <= 1024 / (((int64_t)words + 31) / 32); }
 bool many_products(int64_t rows, int32_t words) {
     return rows > 512 && (rows + 255) / 256 * (((int64_t)words + mlda::kTileWords - 1) / mlda::kTileWords) >= 4 * kCus;

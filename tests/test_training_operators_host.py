@@ -76,6 +76,13 @@ def test_product_refusals(lib):
     refused(lib, lib.mlda_mx_linear_workspace_bytes(1, 5, None), word="null")
 
 
+@pytest.mark.parametrize("rows,cols,laid", [(1, 16384, False), (1, 16385, True), (16, 1024, False), (16, 1025, True), (15, 1088, False), (17, 32, True)])
+def test_which_rows_need_room(lib, rows, cols, laid):
+    """Up to 16 rows and 512 blocks are put into 4 bits where they are used."""
+    n = ctypes.c_size_t()
+    assert lib.mlda_mx_linear_workspace_bytes(rows, cols, ctypes.addressof(n)) == 0 and (n.value > 0) == laid
+
+
 def test_dropout_refusals(lib):
     def call(x=P, x_stride=8, residual=None, residual_stride=0, y=2 * P, y_stride=8, rows=2, cols=8, p=0.1, dev_step=None, first_row=0, kind=FP32):
         return lib.mlda_dropout(x, x_stride, residual, residual_stride, y, y_stride, rows, cols, p, 1, 0, dev_step, first_row, kind, None)
