@@ -8,8 +8,9 @@
 //
 // All of it is in fp64 and rounded once: the border is then the same for every way of computing it, sums of millions of words keep their bits, and a ratio that fp32
 // cannot hold does no harm under a weight that makes it small again.  Exponentials are a series, within 2^-40 of themselves, and the KL term, a difference of nearly
-// equal numbers, within 2^-36.  (With fp32's exponentials, which end at exp(88.7), it takes as long: 26,154 documents of 113 words with a KL term 26.7 us, so 26.1; 50e6 words 190 and 190,
-// with a KL term 242 and 231.)  Bound by memory: 50e6 words, 20 bytes each, 5.3 TB/s (one word to a thread at a time 277 us).  Few words are one workgroup's and one launch; more
+// equal numbers, within 2^-36.  (With fp32's exponentials, which end at exp(88.7), it takes as long: 26,154 documents of 113 words with a KL term 26.7 us, so 26.5; 50e6 words 190 and 191,
+// with a KL term 242 and 233.)  Many words are bound by memory: 50e6 words, 20 bytes each, 5.2 TB/s (one word to a thread at a time 277 us).  In between it is instructions: 26,154
+// documents with a KL term take 220 for each word, 50 of them for its row, which keep the vector units busy for 71% of the time.  Few words are one workgroup's and one launch; more
 // leave partial sums, which a second launch joins in a fixed order.
 #pragma once
 #include "vec_io.hpp"
@@ -79,8 +80,8 @@ __device__ __forceinline__ Exp exp_of(double x) {
             __builtin_bit_cast(double, (uint64_t)most << 32 | (uint32_t)bits), k == 0.0};
 }
 
-// kPolicyEach: neighbouring words of a thread.  A word is a long chain of instructions: those of a single workgroup have a thread each if they can (330 of them, in fp64
-// with a KL term, 4.9 us by four, 2.8 apart).
+// kPolicyEach: neighbouring words of a thread.  A word is a long chain of instructions: those of a single workgroup have a thread each if they can (405 of them with
+// a KL term 4.6 us by four, 2.9 apart).
 template <int kThreads, int kPolicyEach, bool kReference>
 __global__ __launch_bounds__(kThreads) void policy_kernel(PolicyArgs a) {
     constexpr int kChunk = kThreads * kPolicyEach;
